@@ -334,6 +334,75 @@ int cdgrab_reorder(cdgrab_handle *h, int64_t m, int64_t n, const int8_t *signs,
 int cdgrab_herding_bound(cdgrab_handle *h, int64_t m, int64_t n, int64_t d, const float *z,
                          const int32_t *perm, double *bound_out);
 
+/* ---- Per-example gradients of layers --------------------------------------------------
+ *
+ * What a model of layers needs to make the balancer's rows: the gradient of a layer's
+ * parameters for every example by itself, written to a stretch of the example's row.  Rows of
+ * several layers side by side make the [m][n][d] array that cdgrab_balance_epoch reads.
+ *
+ * Arrays of rows ("X", "Y", "D", ..) hold one element type, side by side within a row; their
+ * strides are counted in elements from row to row and are at least the row's width.
+ * Parameters and gradients are fp32.  Sums are taken in fp32 or double and in a fixed order: the
+ * same call gives the same bits.  These calls enqueue kernels only and may be captured once
+ * the call has run with the same sizes; captured calls of one handle share its workspace,
+ * so their replays must not overlap, like the handle's other calls.  Outputs must not overlap
+ * inputs.  The current device is left as it was. */
+#define CDGRAB_F32 0
+#define CDGRAB_BF16 1
+#define CDGRAB_F16 2
+
+/* Where the rows (tokens) of each example lie in the arrays of `rows` rows.
+ * Example e has count[e] rows (all `tokens` of them if count is NULL) starting at row first[e]
+ * (row e * tokens if first is NULL): NULL, NULL is a dense batch, count alone a padded one, first and
+ * count rows packed one after the other.  What of an example lies outside the arrays or
+ * beyond `tokens` rows is left out.  Rows of no example are neither read nor written, whatever they hold.  An
+ * example without rows has the gradient zero. */
+typedef struct cdgrab_token_rows {
+    int64_t examples;
+    int64_t rows;           /* of X and D (DY, DX); without `first` at least examples * tokens */
+    int64_t tokens;         /* rows an example has at most                                     */
+    const int64_t *first;   /* [examples] dev or NULL                                          */
+    const int32_t *count;   /* [examples] dev or NULL                                          */
+} cdgrab_token_rows;
+
+/* Layer norm of every row:  Y = gain * (X - mean) / sqrt(var + eps) + bias, mean and variance
+ * (over `width`, biased) of the row.
+ *   X, Y [rows][width] of `type` dev; gain, bias [width] fp32 dev, or NULL: one, zero.
+ * Statistics in fp32; a row with an element that is not finite becomes NaN.
+ * Errors: EINVAL (sizes, width > 16384, type, eps < 0, null, strides, overlap), EHIP. */
+int cdgrab_layernorm(cdgrab_handle *h, int64_t rows, int64_t width, int32_t type, const void *X,
+                     int64_t x_stride, const float *gain, const float *bias, float eps, void *Y,
+                     int64_t y_stride);
+
+/* Backward pass of cdgrab_layernorm, with the parameters' gradients of every example: with
+ * h = (X - mean) / sqrt(var + eps) and g = gain * DY, both of a row,
+ *     DX = (g - mean(g) - h mean(g h)) / sqrt(var + eps),
+ *     G[e][c] = sum over the example's rows of DY[c] h[c]          (gain),
+ *     G[e][width + c] = sum over the example's rows of DY[c]       (bias; only if with_bias).
+ * One example that holds all rows gives the ordinary gradient of the batch.
+ *   X (the forward pass's input), DY, DX [rows][width] of `type` dev, gain as there,
+ *   G: row e at G + e * g_stride, fp32 dev.  DX or G may be NULL: not wanted.
+ * Overlapping examples are allowed.
+ * Errors: EINVAL (as above; with_bias not 0 or 1; neither DX nor G), ENOMEM, EHIP. */
+int cdgrab_pergrad_layernorm(cdgrab_handle *h, const cdgrab_token_rows *t, int64_t width, int32_t type,
+                             const void *X, int64_t x_stride, const void *DY, int64_t dy_stride,
+                             const float *gain, float eps, void *DX, int64_t dx_stride,
+                             int32_t with_bias, float *G, int64_t g_stride);
+
+/* Gradient of a linear layer's weights (Y = X W + bias, W [in_dim][out_dim]) for every example:
+ *     G[e][r * out_dim + c] = sum over the example's rows of X[r] D[c],
+ *     G[e][in_dim * out_dim + c] = sum over the example's rows of D[c]     (only if with_bias):
+ * the layout of cdgrab_pergrad, which is this with one row per example and D = softmax - onehot.
+ *   X [rows][in_dim], D [rows][out_dim] (gradient of the layer's output) of `type` dev,
+ *   G: row e at G + e * g_stride, fp32 dev.
+ * Products of bf16 and fp16 elements are exact, those of fp32 elements good to 2^-23; sums in fp32.  An infinite fp32
+ * element (or one above 3.38e38) makes the sums it enters NaN.
+ * Errors: EINVAL (sizes, in_dim or out_dim > 2^20, type, with_bias not 0 or 1, null, strides, overlap),
+ * ENOMEM, EHIP. */
+int cdgrab_pergrad_linear(cdgrab_handle *h, const cdgrab_token_rows *t, int64_t in_dim, int64_t out_dim,
+                          int32_t type, const void *X, int64_t x_stride, const void *D, int64_t d_stride,
+                          int32_t with_bias, float *G, int64_t g_stride);
+
 /* Timings of the last cdgrab_balance_epoch on this handle (options.timing >= 1).
  * Synchronises the stream.  Errors: EINVAL (timing was off), EHIP. */
 int cdgrab_get_timing(cdgrab_handle *h, cdgrab_timing *out /*host*/);

@@ -59,6 +59,14 @@ class Plan(ctypes.Structure):
         return {name: getattr(self, name) for name, _ in self._fields_}
 
 
+class _TokenRows(ctypes.Structure):
+    _fields_ = [("examples", ctypes.c_int64), ("rows", ctypes.c_int64), ("tokens", ctypes.c_int64),
+                ("first", ctypes.c_void_p), ("count", ctypes.c_void_p)]
+
+
+_ELEM = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}  # CDGRAB_F32, _BF16, _F16
+
+
 def library_path() -> str:
     return _LIB_PATH
 
@@ -104,6 +112,13 @@ def load_library():
     lib.cdgrab_herding_bound.restype = ctypes.c_int
     lib.cdgrab_balance_epoch_static.argtypes = [P, i64, i64, i64, P, P, P, P, P, P, P]
     lib.cdgrab_balance_epoch_static.restype = ctypes.c_int
+    lib.cdgrab_layernorm.argtypes = [P, i64, i64, i32, P, i64, P, P, ctypes.c_float, P, i64]
+    lib.cdgrab_layernorm.restype = ctypes.c_int
+    lib.cdgrab_pergrad_layernorm.argtypes = [P, ctypes.POINTER(_TokenRows), i64, i32, P, i64, P, i64, P,
+                                             ctypes.c_float, P, i64, i32, P, i64]
+    lib.cdgrab_pergrad_layernorm.restype = ctypes.c_int
+    lib.cdgrab_pergrad_linear.argtypes = [P, ctypes.POINTER(_TokenRows), i64, i64, i32, P, i64, P, i64, i32, P, i64]
+    lib.cdgrab_pergrad_linear.restype = ctypes.c_int
     lib.cdgrab_get_timing.argtypes = [P, ctypes.POINTER(Timing)]
     lib.cdgrab_get_timing.restype = ctypes.c_int
     _lib = lib
@@ -358,3 +373,126 @@ def cdgrab_balance_epoch_randomized(h: Handle, grads: torch.Tensor, uniforms: to
         _ptr(perm_in, torch.int32, (m, n), "perm_in", dev),
         signs.data_ptr(), perm.data_ptr(), r64.data_ptr(), dots.data_ptr()))
     return {"signs": signs, "perm": perm, "r64": r64, "dots": dots}
+
+
+# ---- per-example gradients of layers --------------------------------------------------------
+
+def _rows(t: torch.Tensor, name: str, device, like: Optional[torch.Tensor] = None):
+    """(pointer, rows, width, stride) of an array of rows: [..., width] with elements side by side and one
+    distance from row to row."""
+    if t.dtype not in _ELEM:
+        raise TypeError("%s must be float32, bfloat16 or float16, got %s" % (name, t.dtype))
+    if t.device != device:
+        raise ValueError("%s must live on %s, got %s" % (name, device, t.device))
+    if t.dim() < 2:
+        raise ValueError("%s must have rows and a width, got shape %s" % (name, tuple(t.shape)))
+    if like is not None and (t.dtype != like.dtype or t.shape[:-1] != like.shape[:-1]):
+        raise ValueError("%s must be %s of rows %s, got %s %s" % (name, like.dtype, tuple(like.shape[:-1]), t.dtype,
+                                                                  tuple(t.shape)))
+    width, rows = t.shape[-1], 1
+    for n in t.shape[:-1]:
+        rows *= n
+    stride = max(width, 1)
+    if rows and width:
+        if t.stride(-1) != 1 and width > 1:
+            raise ValueError("%s: the elements of a row must lie side by side" % name)
+        steps = [(n, s) for n, s in zip(t.shape[:-1], t.stride()[:-1]) if n > 1]
+        if steps:
+            stride = steps[-1][1]
+            for (_, outer), (n, inner) in zip(steps, steps[1:]):
+                if outer != n * inner:
+                    raise ValueError("%s: rows must be one distance apart" % name)
+            if stride < width:
+                raise ValueError("%s: rows must not overlap" % name)
+    return t.data_ptr(), rows, width, stride
+
+
+def _token_rows(X: torch.Tensor, rows: int, first, count, tokens: Optional[int], device) -> _TokenRows:
+    """X is [examples][tokens][width], or [rows][width] with `first` and `tokens` (packed)."""
+    if first is None:
+        if X.dim() != 3:
+            raise ValueError("X must be [examples][tokens][width] unless `first` says where examples start")
+        if tokens is not None and tokens != X.shape[1]:
+            raise ValueError("tokens is %d, and X has %d per example" % (tokens, X.shape[1]))
+        examples, tokens = X.shape[0], X.shape[1]
+    else:
+        if tokens is None:
+            raise ValueError("`first` needs `tokens`, the rows that an example has at most")
+        examples = first.shape[0] if first.dim() == 1 else -1
+    return _TokenRows(examples, rows, tokens, _ptr(first, torch.int64, (examples,), "first", device),
+                      _ptr(count, torch.int32, (examples,), "count", device))
+
+
+def _grad_rows(G_out: Optional[torch.Tensor], examples: int, d: int, device):
+    """(G, stride): [examples][d] fp32, a stretch of longer rows if given so."""
+    if G_out is None:
+        G_out = torch.empty((examples, d), dtype=torch.float32, device=device)
+    if G_out.dtype != torch.float32:
+        raise TypeError("G_out must be float32, got %s" % G_out.dtype)
+    if tuple(G_out.shape) != (examples, d):
+        raise ValueError("G_out must have shape %s, got %s" % ((examples, d), tuple(G_out.shape)))
+    _, _, _, stride = _rows(G_out, "G_out", device)
+    return G_out, stride
+
+
+def cdgrab_layernorm(h: Handle, X: torch.Tensor, gain: Optional[torch.Tensor] = None,
+                     bias: Optional[torch.Tensor] = None, eps: float = 1e-5,
+                     Y: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Layer norm over the last axis of X[..., width]; gain and bias [width] float32."""
+    px, rows, width, sx = _rows(X, "X", h.device)
+    if Y is None:
+        Y = torch.empty(X.shape, dtype=X.dtype, device=h.device)
+    py, _, wy, sy = _rows(Y, "Y", h.device, X)
+    if wy != width:
+        raise ValueError("Y must have shape %s, got %s" % (tuple(X.shape), tuple(Y.shape)))
+    h._check(h._lib.cdgrab_layernorm(
+        h._h, rows, width, _ELEM[X.dtype], px, sx, _ptr(gain, torch.float32, (width,), "gain", h.device),
+        _ptr(bias, torch.float32, (width,), "bias", h.device), eps, py, sy))
+    return Y
+
+
+def cdgrab_pergrad_layernorm(h: Handle, X: torch.Tensor, dY: torch.Tensor, gain: Optional[torch.Tensor] = None,
+                             eps: float = 1e-5, first: Optional[torch.Tensor] = None,
+                             count: Optional[torch.Tensor] = None, tokens: Optional[int] = None,
+                             dX: Optional[torch.Tensor] = None, G_out: Optional[torch.Tensor] = None,
+                             with_bias: bool = True, want_dx: bool = True, want_grads: bool = True):
+    """Backward pass of cdgrab_layernorm: (dX, G), G[examples][gain's gradient | bias's gradient].
+
+    X and dY are [examples][tokens][width] (with `count` a padded batch), or [rows][width] with the examples' rows
+    packed: `first` [examples] int64, `count` int32, `tokens` at most.  Rows of no example keep what dX holds (zero
+    where the call makes dX).  G_out may be a stretch of columns of longer rows."""
+    px, rows, width, sx = _rows(X, "X", h.device)
+    py, _, wy, sy = _rows(dY, "dY", h.device, X)
+    if wy != width:
+        raise ValueError("dY must have shape %s, got %s" % (tuple(X.shape), tuple(dY.shape)))
+    t = _token_rows(X, rows, first, count, tokens, h.device)
+    pd, sd = None, width
+    if dX is not None or want_dx:
+        if dX is None:
+            whole = first is None and count is None
+            dX = (torch.empty if whole else torch.zeros)(X.shape, dtype=X.dtype, device=h.device)
+        pd, _, wd, sd = _rows(dX, "dX", h.device, X)
+        if wd != width:
+            raise ValueError("dX must have shape %s, got %s" % (tuple(X.shape), tuple(dX.shape)))
+    G, sg = None, 0
+    if G_out is not None or want_grads:
+        G, sg = _grad_rows(G_out, t.examples, (2 if with_bias else 1) * width, h.device)
+    h._check(h._lib.cdgrab_pergrad_layernorm(
+        h._h, ctypes.byref(t), width, _ELEM[X.dtype], px, sx, py, sy,
+        _ptr(gain, torch.float32, (width,), "gain", h.device), eps, pd, sd, 1 if with_bias else 0,
+        G.data_ptr() if G is not None else None, sg))
+    return dX, G
+
+
+def cdgrab_pergrad_linear(h: Handle, X: torch.Tensor, D: torch.Tensor, with_bias: bool = True,
+                          first: Optional[torch.Tensor] = None, count: Optional[torch.Tensor] = None,
+                          tokens: Optional[int] = None, G_out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Per-example gradients G[examples][(in + 1) * out] of a linear layer's weights (last `out`: the bias) from its
+    inputs X and its outputs' gradients D; rows of examples as in cdgrab_pergrad_layernorm."""
+    px, rows, n_in, sx = _rows(X, "X", h.device)
+    pd, _, n_out, sd = _rows(D, "D", h.device, X)
+    t = _token_rows(X, rows, first, count, tokens, h.device)
+    G, sg = _grad_rows(G_out, t.examples, (n_in + (1 if with_bias else 0)) * n_out, h.device)
+    h._check(h._lib.cdgrab_pergrad_linear(
+        h._h, ctypes.byref(t), n_in, n_out, _ELEM[X.dtype], px, sx, pd, sd, 1 if with_bias else 0, G.data_ptr(), sg))
+    return G

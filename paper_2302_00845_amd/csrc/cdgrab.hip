@@ -22,6 +22,8 @@
 #include "band_kernels.hpp"
 #include "narrow_kernels.hpp"
 #include "train_kernels.hpp"
+#include "norm_kernels.hpp"
+#include "linear_kernels.hpp"
 
 using namespace cdgrab;
 
@@ -79,6 +81,9 @@ struct cdgrab_handle {
     bool bands_in_graphs = false;                         // recorded launches hold its address ...
     double *bands_kept = nullptr;                         // ... or that of this one, which it has replaced
     float *staging = nullptr;  int64_t staging_cap = 0;   // floats: two staging chunks (the fused pass reads the previous block too)
+    char *layer_ws = nullptr;  int64_t layer_ws_cap = 0;  // bytes: sums in shares, matrices of the orthogonalised update
+    bool layer_ws_in_graphs = false;                      // recorded launches hold its address ...
+    std::vector<char *> layer_kept;                       // ... or that of one of these, which it has replaced
     bool fixed_workspace = false;                         // the workspace pointers are borrowed: never grow or free them
 
     hipStream_t side = nullptr;                           // chunks are balanced here while the next one is generated
@@ -786,6 +791,8 @@ int cdgrab_destroy(cdgrab_handle *h) {
     if (h->gram_parts) (void)hipFree(h->gram_parts);
     if (h->bands) (void)hipFree(h->bands);
     if (h->bands_kept) (void)hipFree(h->bands_kept);
+    if (h->layer_ws) (void)hipFree(h->layer_ws);
+    for (char *p : h->layer_kept) (void)hipFree(p);
     delete h;
     return CDGRAB_OK;
 }
@@ -1724,3 +1731,5 @@ int cdgrab_get_timing(cdgrab_handle *h, cdgrab_timing *out) {
 }
 
 }  // extern "C"
+
+#include "layer_entries.hpp"
