@@ -293,6 +293,18 @@ int cdgrab_train_epoch_softmax(cdgrab_handle *h, int64_t m, int64_t n, int64_t i
                                float momentum, int8_t *signs_out, int32_t *perm_out,
                                float *grads_out, float *loss_out);
 
+/* cdgrab_train_epoch_softmax with an orthogonalised update: after every step every worker applies
+ *     v <- momentum v + gbar,   W <- W - lr O(v),
+ * O(v) as cdgrab_orthogonalize (below) makes it of v as a matrix [in_dim+1][classes].  velocity is required (zeros
+ * before the first epoch), also for momentum 0; steps and coeffs as there; other arguments, outputs and the
+ * balancing as in cdgrab_train_epoch_softmax.  Errors: as there and there. */
+int cdgrab_train_epoch_softmax_orthogonal(cdgrab_handle *h, int64_t m, int64_t n, int64_t in_dim,
+                                          int64_t classes, const float *X, const int32_t *y,
+                                          const int32_t *perm_in, float *W, float *velocity, float lr,
+                                          float momentum, int32_t steps, const double *coeffs /*host*/,
+                                          int8_t *signs_out, int32_t *perm_out, float *grads_out,
+                                          float *loss_out);
+
 /* T training epochs with the permutations carried over (the outer loop of "CD-GraB
  * Workers" / "CD-GraB Parameter Server", Sec. 3.3: the order built while epoch t is
  * balanced is the order epoch t+1 visits).  Equivalent to `epochs` calls of
@@ -402,6 +414,21 @@ int cdgrab_pergrad_layernorm(cdgrab_handle *h, const cdgrab_token_rows *t, int64
 int cdgrab_pergrad_linear(cdgrab_handle *h, const cdgrab_token_rows *t, int64_t in_dim, int64_t out_dim,
                           int32_t type, const void *X, int64_t x_stride, const void *D, int64_t d_stride,
                           int32_t with_bias, float *G, int64_t g_stride);
+
+/* Orthogonalised update: M with its singular values brought near one and its singular vectors kept,
+ * by products alone (Newton-Schulz): X = M / ||M||_F, then `steps` times
+ *     A = X X^T,   X <- a X + (b A + c A^2) X          (the shorter side as rows), O = X.
+ *   M, O: `batch` matrices [rows][cols] of `type` dev, m_stride / o_stride elements from row to row, m_matrix / o_matrix from
+ *   matrix to matrix (any value if batch is 1); coeffs: {a, b, c} host, or NULL: 3.4445, -4.775, 2.0315
+ *   (about 0.7 .. 1.2 after five steps, from 0.01 of the norm on).
+ * Products with the error of fp32 ones whatever the type, or better; the result is rounded once.  A matrix of zeros stays
+ * zero, one with an element that is not finite becomes NaN.  Coefficients under which a singular value could pass 3.5
+ * within the steps are refused.  Like the calls above it may be captured once it has run with the same sizes.
+ * Errors: EINVAL (sizes, a shorter side > 16384, a side > 2^20, type, steps < 0 or > 64, coefficients, null,
+ * strides, overlap), ENOMEM, EHIP. */
+int cdgrab_orthogonalize(cdgrab_handle *h, int64_t batch, int64_t rows, int64_t cols, int32_t type,
+                         const void *M, int64_t m_stride, int64_t m_matrix, int32_t steps,
+                         const double *coeffs /*host*/, void *O, int64_t o_stride, int64_t o_matrix);
 
 /* Timings of the last cdgrab_balance_epoch on this handle (options.timing >= 1).
  * Synchronises the stream.  Errors: EINVAL (timing was off), EHIP. */

@@ -14,12 +14,14 @@ from .cdgrab import (  # noqa: F401
     cdgrab_balance_epoch_static,
     cdgrab_herding_bound,
     cdgrab_layernorm,
+    cdgrab_orthogonalize,
     cdgrab_pergrad,
     cdgrab_pergrad_layernorm,
     cdgrab_pergrad_linear,
     cdgrab_plan_epoch,
     cdgrab_reorder,
     cdgrab_train_epoch_softmax,
+    cdgrab_train_epoch_softmax_orthogonal,
     cdgrab_train_softmax,
     library_path,
     load_library,

@@ -112,6 +112,9 @@ def load_library():
     lib.cdgrab_herding_bound.restype = ctypes.c_int
     lib.cdgrab_balance_epoch_static.argtypes = [P, i64, i64, i64, P, P, P, P, P, P, P]
     lib.cdgrab_balance_epoch_static.restype = ctypes.c_int
+    lib.cdgrab_train_epoch_softmax_orthogonal.argtypes = [P, i64, i64, i64, i64, P, P, P, P, P, ctypes.c_float,
+                                                          ctypes.c_float, i32, P, P, P, P, P]
+    lib.cdgrab_train_epoch_softmax_orthogonal.restype = ctypes.c_int
     lib.cdgrab_layernorm.argtypes = [P, i64, i64, i32, P, i64, P, P, ctypes.c_float, P, i64]
     lib.cdgrab_layernorm.restype = ctypes.c_int
     lib.cdgrab_pergrad_layernorm.argtypes = [P, ctypes.POINTER(_TokenRows), i64, i32, P, i64, P, i64, P,
@@ -119,6 +122,8 @@ def load_library():
     lib.cdgrab_pergrad_layernorm.restype = ctypes.c_int
     lib.cdgrab_pergrad_linear.argtypes = [P, ctypes.POINTER(_TokenRows), i64, i64, i32, P, i64, P, i64, i32, P, i64]
     lib.cdgrab_pergrad_linear.restype = ctypes.c_int
+    lib.cdgrab_orthogonalize.argtypes = [P, i64, i64, i64, i32, P, i64, i64, i32, P, P, i64, i64]
+    lib.cdgrab_orthogonalize.restype = ctypes.c_int
     lib.cdgrab_get_timing.argtypes = [P, ctypes.POINTER(Timing)]
     lib.cdgrab_get_timing.restype = ctypes.c_int
     _lib = lib
@@ -496,3 +501,62 @@ def cdgrab_pergrad_linear(h: Handle, X: torch.Tensor, D: torch.Tensor, with_bias
     h._check(h._lib.cdgrab_pergrad_linear(
         h._h, ctypes.byref(t), n_in, n_out, _ELEM[X.dtype], px, sx, pd, sd, 1 if with_bias else 0, G.data_ptr(), sg))
     return G
+
+
+def _coeffs(coeffs):
+    if coeffs is None:
+        return None
+    a, b, c = (float(v) for v in coeffs)
+    return (ctypes.c_double * 3)(a, b, c)
+
+
+def cdgrab_orthogonalize(h: Handle, M: torch.Tensor, steps: int = 5, coeffs=None,
+                         out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """M[rows][cols] or [batch][rows][cols] with its singular values brought near one (Newton-Schulz products;
+    coeffs (a, b, c) of a x + b x^3 + c x^5)."""
+    if M.dim() not in (2, 3):
+        raise ValueError("M must be [rows][cols] or [batch][rows][cols], got %s" % (tuple(M.shape),))
+    if out is None:
+        out = torch.empty(M.shape, dtype=M.dtype, device=h.device)
+    at = []
+    for t, name in ((M, "M"), (out, "out")):
+        if t.dtype not in _ELEM:
+            raise TypeError("%s must be float32, bfloat16 or float16, got %s" % (name, t.dtype))
+        if t.device != h.device:
+            raise ValueError("%s must live on %s, got %s" % (name, h.device, t.device))
+        if t.dtype != M.dtype or t.shape != M.shape:
+            raise ValueError("out must be %s %s, got %s %s" % (M.dtype, tuple(M.shape), t.dtype, tuple(t.shape)))
+        if t.shape[-1] > 1 and t.stride(-1) != 1:
+            raise ValueError("%s: the elements of a row must lie side by side" % name)
+        row = t.stride(-2) if t.shape[-2] > 1 else t.shape[-1]
+        at.append((t.data_ptr(), row, t.stride(0) if t.dim() == 3 else 0))
+    batch = M.shape[0] if M.dim() == 3 else 1
+    h._check(h._lib.cdgrab_orthogonalize(h._h, batch, M.shape[-2], M.shape[-1], _ELEM[M.dtype], at[0][0], at[0][1], at[0][2],
+                                         steps, _coeffs(coeffs), at[1][0], at[1][1], at[1][2]))
+    return out
+
+
+def cdgrab_train_epoch_softmax_orthogonal(h: Handle, X: torch.Tensor, y: torch.Tensor, W: torch.Tensor,
+                                          velocity: torch.Tensor, perm_in: Optional[torch.Tensor] = None,
+                                          lr: float = 0.02, momentum: float = 0.95, steps: int = 5, coeffs=None,
+                                          want_grads: bool = False, want_loss: bool = True) -> dict:
+    """cdgrab_train_epoch_softmax with W <- W - lr O(velocity), O as cdgrab_orthogonalize makes it of the
+    velocity [(in_dim+1)*classes] as a matrix of the shape of W."""
+    m, n, in_dim = X.shape
+    classes = W.shape[1]
+    d = (in_dim + 1) * classes
+    dev = h.device
+    signs = torch.empty((m, n // 2), dtype=torch.int8, device=dev)
+    perm = torch.empty((m, n), dtype=torch.int32, device=dev)
+    grads = torch.empty((m, n, d), dtype=torch.float32, device=dev) if want_grads else None
+    loss = torch.empty((m, n), dtype=torch.float32, device=dev) if want_loss else None
+    h._check(h._lib.cdgrab_train_epoch_softmax_orthogonal(
+        h._h, m, n, in_dim, classes,
+        _ptr(X, torch.float32, (m, n, in_dim), "X", dev), _ptr(y, torch.int32, (m, n), "y", dev),
+        _ptr(perm_in, torch.int32, (m, n), "perm_in", dev),
+        _ptr(W, torch.float32, (in_dim + 1, classes), "W", dev),
+        _ptr(velocity, torch.float32, (d,), "velocity", dev), lr, momentum, steps, _coeffs(coeffs),
+        signs.data_ptr(), perm.data_ptr(),
+        grads.data_ptr() if grads is not None else None,
+        loss.data_ptr() if loss is not None else None))
+    return {"signs": signs, "perm": perm, "grads": grads, "loss": loss}

@@ -24,6 +24,7 @@
 #include "train_kernels.hpp"
 #include "norm_kernels.hpp"
 #include "linear_kernels.hpp"
+#include "ortho_kernels.hpp"
 
 using namespace cdgrab;
 
@@ -721,6 +722,8 @@ int launch_column_mean(cdgrab_handle *h, int64_t n, int64_t d, const float *rows
 }
 
 }  // namespace
+
+#include "layer_entries.hpp"
 
 extern "C" {
 
@@ -1430,6 +1433,8 @@ struct TrainCtx {
     float lr, momentum;
     int64_t block_steps;  // steps per block of train_kernels.hpp; 0: a launch pair per step
     int tiles, ksplit;    // Gram tiles per block of steps, workgroups per tile
+    int64_t orth_steps;   // -1: W <- W - lr v; else W <- W - lr O(v) after that many Newton-Schulz steps
+    OrthoCoeffs orth;
 };
 
 // Workers and classes that the blocks of steps are for: at least four steps per block and one MFMA column
@@ -1480,11 +1485,16 @@ int train_step_launches(TrainCtx *c, int64_t j, int64_t j_end, int64_t k_first, 
                            (int)c->classes);
         auto update = [&](auto kernel) {
             hipLaunchKernelGGL(kernel, dim3((unsigned)((c->d + 255) / 256)), dim3(256), 0, h->stream, c->X, c->perm_in,
-                               h->train_delta, c->W, c->velocity, staging, c->grads_out, c->m, c->n, j, k_first,
-                               (int)c->in_dim, (int)c->classes, c->lr, c->momentum);
+                               h->train_delta, c->orth_steps < 0 ? c->W : nullptr, c->velocity, staging, c->grads_out, c->m,
+                               c->n, j, k_first, (int)c->in_dim, (int)c->classes, c->lr, c->momentum);
         };
         if (c->perm_in) update(train_step_update<true>);
         else update(train_step_update<false>);
+        if (c->orth_steps >= 0) {
+            const int rc = run_ortho<float>(h, "cdgrab_train_epoch_softmax_orthogonal", 1, c->in_dim + 1, c->classes, c->velocity,
+                                            c->classes, 0, c->orth_steps, c->orth, nullptr, c->W, c->lr, c->classes, 0);
+            if (rc) return rc;
+        }
     }
     HIP_TRY(h, hipGetLastError());
     return CDGRAB_OK;
@@ -1541,27 +1551,28 @@ int train_generate(void *vctx, int64_t first_pair, int64_t count, float *staging
 }
 }  // namespace
 
-int cdgrab_train_epoch_softmax(cdgrab_handle *h, int64_t m, int64_t n, int64_t in_dim, int64_t classes,
-                               const float *X, const int32_t *y, const int32_t *perm_in, float *W,
-                               float *velocity, float lr, float momentum, int8_t *signs_out,
-                               int32_t *perm_out, float *grads_out, float *loss_out) {
-    if (!h) return CDGRAB_EINVAL;
+// (orth_steps, orth: as in TrainCtx)
+static int train_epoch_impl(cdgrab_handle *h, const char *who, int64_t m, int64_t n, int64_t in_dim, int64_t classes,
+                            const float *X, const int32_t *y, const int32_t *perm_in, float *W,
+                            float *velocity, float lr, float momentum, int64_t orth_steps, const OrthoCoeffs &orth,
+                            int8_t *signs_out, int32_t *perm_out, float *grads_out, float *loss_out) {
     if (m < 1 || n < 2 || (n & 1) || in_dim < 1 || classes < 1 || classes > 1024 || in_dim > (1 << 20))
-        return fail(h, CDGRAB_EINVAL, "cdgrab_train_epoch_softmax: bad sizes");
+        return fail(h, CDGRAB_EINVAL, "%s: bad sizes", who);
     if (!X || !y || !W || !signs_out || !perm_out)
-        return fail(h, CDGRAB_EINVAL, "cdgrab_train_epoch_softmax: null pointer");
+        return fail(h, CDGRAB_EINVAL, "%s: null pointer", who);
     if (ranges_overlap(perm_in, m * n * 4, perm_out, m * n * 4))
-        return fail(h, CDGRAB_EINVAL, "cdgrab_train_epoch_softmax: perm_in and perm_out must not overlap");
+        return fail(h, CDGRAB_EINVAL, "%s: perm_in and perm_out must not overlap", who);
     if (momentum != 0.0f && !velocity)
-        return fail(h, CDGRAB_EINVAL, "cdgrab_train_epoch_softmax: momentum needs a velocity buffer");
+        return fail(h, CDGRAB_EINVAL, "%s: momentum needs a velocity buffer", who);
     HIP_TRY(h, hipSetDevice(h->device));
     const int64_t chunk = train_chunk_pairs(h, m, n, (in_dim + 1) * classes);
     int64_t block_steps = std::min(train_block_steps(m, n, classes), 2 * (chunk / m));
-    if (block_steps < train_least_steps(m, in_dim, classes)) block_steps = 0;
+    // (a block of steps rests on an update that is linear in the gradients)
+    if (orth_steps >= 0 || block_steps < train_least_steps(m, in_dim, classes)) block_steps = 0;
     int rc = ensure(h, h->train_delta, h->train_delta_cap, block_steps > 0 ? block_steps * m * classes : m * classes);
     if (rc) return rc;
     TrainCtx ctx{h, m, n, in_dim, classes, (in_dim + 1) * classes, X, y, perm_in, W, velocity,
-                 grads_out, loss_out, lr, momentum, block_steps, 0, 1};
+                 grads_out, loss_out, lr, momentum, block_steps, 0, 1, orth_steps, orth};
     if (block_steps > 0) {
         const int64_t blocks = (std::min(2 * (chunk / m), n) + block_steps - 1) / block_steps;  // of a chunk
         const int64_t blk = (block_steps * m + kTilePairs - 1) / kTilePairs;
@@ -1577,6 +1588,29 @@ int cdgrab_train_epoch_softmax(cdgrab_handle *h, int64_t m, int64_t n, int64_t i
     }
     return balance_epoch_impl(h, m, n, ctx.d, nullptr, train_generate, &ctx, chunk, perm_in,
                               signs_out, perm_out, nullptr, nullptr, nullptr);
+}
+
+int cdgrab_train_epoch_softmax(cdgrab_handle *h, int64_t m, int64_t n, int64_t in_dim, int64_t classes,
+                               const float *X, const int32_t *y, const int32_t *perm_in, float *W,
+                               float *velocity, float lr, float momentum, int8_t *signs_out,
+                               int32_t *perm_out, float *grads_out, float *loss_out) {
+    if (!h) return CDGRAB_EINVAL;
+    return train_epoch_impl(h, "cdgrab_train_epoch_softmax", m, n, in_dim, classes, X, y, perm_in, W, velocity, lr, momentum, -1,
+                            OrthoCoeffs{}, signs_out, perm_out, grads_out, loss_out);
+}
+
+int cdgrab_train_epoch_softmax_orthogonal(cdgrab_handle *h, int64_t m, int64_t n, int64_t in_dim, int64_t classes,
+                                          const float *X, const int32_t *y, const int32_t *perm_in, float *W, float *velocity,
+                                          float lr, float momentum, int32_t steps, const double *coeffs, int8_t *signs_out,
+                                          int32_t *perm_out, float *grads_out, float *loss_out) {
+    if (!h) return CDGRAB_EINVAL;
+    static const char *who = "cdgrab_train_epoch_softmax_orthogonal";
+    OrthoCoeffs c{};
+    const int rc = ortho_coeffs(h, who, steps, coeffs, &c);
+    if (rc) return rc;
+    if (!velocity) return fail(h, CDGRAB_EINVAL, "%s: needs a velocity buffer", who);
+    return train_epoch_impl(h, who, m, n, in_dim, classes, X, y, perm_in, W, velocity, lr, momentum, steps, c, signs_out, perm_out,
+                            grads_out, loss_out);
 }
 
 int cdgrab_train_softmax(cdgrab_handle *h, int64_t m, int64_t n, int64_t in_dim, int64_t classes,
@@ -1731,5 +1765,3 @@ int cdgrab_get_timing(cdgrab_handle *h, cdgrab_timing *out) {
 }
 
 }  // extern "C"
-
-#include "layer_entries.hpp"

@@ -3,6 +3,10 @@
 
 namespace {
 
+constexpr int64_t kOrthoOneGroup = 4096;                     // columns that one workgroup of the narrow form takes by itself
+constexpr int64_t kOrthoBytes = (int64_t)4 << 30;            // workspace of the products' form: as many matrices at a time
+constexpr int64_t kOrthoMaxShort = 16384;
+constexpr int64_t kOrthoMaxSide = (int64_t)1 << 20;
 constexpr int64_t kMaxGroups = (int64_t)1 << 22;  // workgroups per launch (a grid dimension holds fewer than 2^32 threads)
 
 // Workspace of the layer operators.  What a recorded call has used is kept until the handle goes, also when a larger
@@ -149,6 +153,139 @@ int run_linear(cdgrab_handle *h, const TokenRows &tok, const T *X, int64_t x_str
     return CDGRAB_OK;
 }
 
+// The largest singular value that the steps can make of values up to 1: they are refused beyond what the kernels' scales
+// have room for (X up to 3.5, the factor b A + c A^2 up to 30).
+bool ortho_in_range(int64_t steps, const OrthoCoeffs &c) {
+    double most = 1.0001;
+    for (int64_t s = 0; s < steps; ++s) {
+        double next = 0.0;
+        for (int q = 0; q <= 2000; ++q) {
+            const double x = most * q / 2000, l = x * x, poly = c.b * l + c.c * l * l, y = std::abs(x * (c.a + poly));
+            if (!(std::abs(poly) <= 30.0 && y <= 3.5)) return false;  // (NaN is refused here too)
+            next = std::max(next, y);
+        }
+        most = 1.001 * next;
+        if (!(most <= 3.5)) return false;
+    }
+    return true;
+}
+
+template <int NT, typename T>
+int run_ortho_narrow(cdgrab_handle *h, const char *who, int64_t batch, OrthoIo<T> io, int64_t steps, const OrthoCoeffs &c) {
+    constexpr int64_t N = NT * 16;
+    // one workgroup per matrix while a matrix is short or there are enough of them
+    if (io.long_side <= kOrthoOneGroup || batch >= h->num_cu) {
+        hipLaunchKernelGGL((ortho_narrow<NT, T>), dim3((unsigned)batch), dim3(kOrthoThreads), 0, h->stream, io, (int)steps, c);
+        HIP_TRY(h, hipGetLastError());
+        return CDGRAB_OK;
+    }
+    const int64_t fill = std::max<int64_t>(1, h->num_cu / batch);
+    const int64_t per = round_up((io.long_side + std::min<int64_t>(fill, 128) - 1) / std::min<int64_t>(fill, 128), 256);
+    const int chunks = (int)((io.long_side + per - 1) / per);
+    double *parts = nullptr;
+    const int rc = layer_room(h, who, batch * (chunks + 1) * N * N, &parts);
+    if (rc) return rc;
+    double *P = parts + batch * chunks * N * N;
+    hipLaunchKernelGGL((ortho_narrow_gram<NT, T>), dim3((unsigned)(batch * chunks)), dim3(kOrthoThreads), 0, h->stream, io, chunks, per, parts);
+    hipLaunchKernelGGL((ortho_narrow_chain<NT>), dim3((unsigned)batch), dim3(kOrthoThreads), 0, h->stream, io.short_side, chunks, parts,
+                       (int)steps, c, P);
+    hipLaunchKernelGGL((ortho_narrow_apply<NT, T>), dim3((unsigned)(batch * chunks)), dim3(kOrthoThreads), 0, h->stream, io, chunks, per, P);
+    HIP_TRY(h, hipGetLastError());
+    return CDGRAB_OK;
+}
+
+template <int TILE, typename T>
+int run_ortho_products(cdgrab_handle *h, const char *who, int64_t batch, OrthoIo<T> io, int64_t steps, const OrthoCoeffs &c) {
+    const int64_t sp = round_up(io.short_side, TILE), lp = round_up(io.long_side, TILE);
+    const int64_t x_len = sp * lp, a_len = sp * sp, per_matrix = 4 * x_len + 4 * a_len + kOrthoSums * 4;  // fp16 elements
+    const int64_t tm = sp / TILE, tn = lp / TILE;
+    const int64_t most = std::max<int64_t>(1, std::min(kOrthoBytes / 2 / per_matrix,
+                                                       kMaxGroups / std::max(tm * tn, (sp / 32) * (lp / 32))));
+    const int64_t at_once = std::min(batch, most);
+    f16_t *ws = nullptr;
+    const int rc = layer_room(h, who, at_once * per_matrix, &ws);
+    if (rc) return rc;
+    double *sums = reinterpret_cast<double *>(ws);
+    f16_t *at = ws + at_once * kOrthoSums * 4;
+    const auto take = [&](int64_t len) {
+        const OrthoPair p{at, at + at_once * len};
+        at += 2 * at_once * len;
+        return p;
+    };
+    OrthoPair X = take(x_len), Y = take(x_len);
+    const OrthoPair A = take(a_len), B = take(a_len);
+    const int64_t rows = io.m_i < io.m_j ? io.long_side : io.short_side, cols = io.m_i < io.m_j ? io.short_side : io.long_side;
+    for (int64_t b0 = 0; b0 < batch; b0 += at_once) {
+        const int64_t n = std::min(at_once, batch - b0);
+        OrthoIo<T> part = io;
+        part.M += b0 * io.m_matrix;
+        if (part.O) part.O += b0 * io.o_matrix;
+        if (part.sub) part.sub += b0 * io.o_matrix;
+        hipLaunchKernelGGL((ortho_squares<T>), dim3((unsigned)(n * kOrthoSums)), dim3(256), 0, h->stream, part.M, io.m_matrix, rows, cols,
+                           std::max(io.m_i, io.m_j), sums);
+        hipLaunchKernelGGL((ortho_begin<T>), dim3((unsigned)(n * (sp / 32) * (lp / 32))), dim3(256), 0, h->stream, part, sums, X, (int)sp, (int)lp);
+        const auto go = [&](auto kernel, const OrthoProduct &p, int64_t tiles) {
+            hipLaunchKernelGGL(kernel, dim3((unsigned)(n * tiles)), dim3(256), 0, h->stream, p, part);
+        };
+        for (int64_t s = 0; s < steps; ++s) {
+            const int64_t half = tm * (tm + 1) / 2;
+            go(ortho_product_tile<TILE, kOrthoGram, T>,
+               OrthoProduct{X, X, A, A, lp, lp, sp, x_len, x_len, a_len, (int)lp, (int)tm, (int)tm, 0.f,
+                            kOrthoScaleA / (kOrthoScaleX * kOrthoScaleX)}, half);
+            go(ortho_product_tile<TILE, kOrthoPoly, T>,
+               OrthoProduct{A, A, A, B, sp, sp, sp, a_len, a_len, a_len, (int)sp, (int)tm, (int)tm, (float)c.b,
+                            (float)(c.c / kOrthoScaleA)}, half);
+            const OrthoProduct step{B, X, X, Y, sp, lp, lp, a_len, x_len, x_len, (int)sp, (int)tm, (int)tn, (float)c.a, 1.f / kOrthoScaleA};
+            if (s + 1 < steps) go(ortho_product_tile<TILE, kOrthoStep, T>, step, tm * tn);
+            else go(ortho_product_tile<TILE, kOrthoLast, T>, step, tm * tn);
+            std::swap(X, Y);
+        }
+    }
+    HIP_TRY(h, hipGetLastError());
+    return CDGRAB_OK;
+}
+
+// M and O (or `sub`) of `batch` matrices of rows x cols, `m_row` / `o_row` elements from row to row.
+template <typename T>
+int run_ortho(cdgrab_handle *h, const char *who, int64_t batch, int64_t rows, int64_t cols, const T *M, int64_t m_row, int64_t m_matrix,
+              int64_t steps, const OrthoCoeffs &c, T *O, float *sub, float rate, int64_t o_row, int64_t o_matrix) {
+    const bool wide = rows <= cols;
+    const OrthoIo<T> io{M, O, sub, rate, wide ? m_row : 1, wide ? 1 : m_row, m_matrix, wide ? o_row : 1, wide ? 1 : o_row, o_matrix,
+                        (int)std::min(rows, cols), (int)std::max(rows, cols)};
+    if (io.short_side <= 16) return run_ortho_narrow<1>(h, who, batch, io, steps, c);
+    if (io.short_side <= 32) return run_ortho_narrow<2>(h, who, batch, io, steps, c);
+    if (io.short_side <= kOrthoNarrow) return run_ortho_narrow<4>(h, who, batch, io, steps, c);
+    if (steps == 0) {
+        for (int64_t b0 = 0; b0 < batch; b0 += 32768) {
+            const int64_t n = std::min<int64_t>(32768, batch - b0);
+            double *sums = nullptr;
+            const int rc = layer_room(h, who, n * kOrthoSums, &sums);
+            if (rc) return rc;
+            OrthoIo<T> part = io;
+            part.M += b0 * io.m_matrix;
+            if (part.O) part.O += b0 * io.o_matrix;
+            if (part.sub) part.sub += b0 * io.o_matrix;
+            hipLaunchKernelGGL((ortho_squares<T>), dim3((unsigned)(n * kOrthoSums)), dim3(256), 0, h->stream, part.M, m_matrix, rows, cols,
+                               m_row, sums);
+            hipLaunchKernelGGL((ortho_scaled<T>), dim3((unsigned)std::min<int64_t>((rows * cols + 1023) / 1024, 4096), (unsigned)n), dim3(256),
+                               0, h->stream, part, sums);
+        }
+        HIP_TRY(h, hipGetLastError());
+        return CDGRAB_OK;
+    }
+    const int64_t s = io.short_side, tiles = batch * ((s + 127) / 128) * ((s + 127) / 128 + 1) / 2;
+    if (tiles >= h->num_cu / 2) return run_ortho_products<128>(h, who, batch, io, steps, c);
+    return run_ortho_products<64>(h, who, batch, io, steps, c);
+}
+
+int ortho_coeffs(cdgrab_handle *h, const char *who, int64_t steps, const double *coeffs, OrthoCoeffs *c) {
+    *c = coeffs ? OrthoCoeffs{coeffs[0], coeffs[1], coeffs[2]} : OrthoCoeffs{3.4445, -4.775, 2.0315};
+    if (steps < 0 || steps > 64) return fail(h, CDGRAB_EINVAL, "%s: steps=%lld (0 .. 64)", who, (long long)steps);
+    if (!ortho_in_range(steps, *c))
+        return fail(h, CDGRAB_EINVAL, "%s: with coefficients %g %g %g the steps can take a singular value beyond 3.5", who, c->a, c->b, c->c);
+    return CDGRAB_OK;
+}
+
 }  // namespace
 
 extern "C" int cdgrab_layernorm(cdgrab_handle *h, int64_t rows, int64_t width, int32_t type, const void *X, int64_t x_stride,
@@ -278,6 +415,40 @@ extern "C" int cdgrab_pergrad_linear(cdgrab_handle *h, const cdgrab_token_rows *
         if (in_dim <= 64 || out_dim <= 64 || tiles(128, 128) < h->num_cu)
             return run_linear<T, 64, 64, 2, 2>(h, tok, x, x_stride, dl, d_stride, in_dim, out_dim, with_bias, G, g_stride);
         return run_linear<T, 128, 128, 2, 2>(h, tok, x, x_stride, dl, d_stride, in_dim, out_dim, with_bias, G, g_stride);
+    };
+    if (type == CDGRAB_F32) return by_type(float{});
+    return type == CDGRAB_BF16 ? by_type(bf16_t{}) : by_type(f16_t{});
+}
+
+extern "C" int cdgrab_orthogonalize(cdgrab_handle *h, int64_t batch, int64_t rows, int64_t cols, int32_t type, const void *M,
+                                    int64_t m_stride, int64_t m_matrix, int32_t steps, const double *coeffs, void *O, int64_t o_stride,
+                                    int64_t o_matrix) {
+    if (!h) return CDGRAB_EINVAL;
+    static const char *who = "cdgrab_orthogonalize";
+    if (batch < 0 || batch > kMaxGroups || rows < 1 || cols < 1 || rows > kOrthoMaxSide || cols > kOrthoMaxSide || bad_type(type))
+        return fail(h, CDGRAB_EINVAL, "%s: bad arguments batch=%lld rows=%lld cols=%lld (1 .. 2^20) type=%d", who, (long long)batch,
+                    (long long)rows, (long long)cols, (int)type);
+    if (std::min(rows, cols) > kOrthoMaxShort)
+        return fail(h, CDGRAB_EINVAL, "%s: the shorter side is %lld, and at most %lld", who, (long long)std::min(rows, cols),
+                    (long long)kOrthoMaxShort);
+    OrthoCoeffs c{};
+    const int rc = ortho_coeffs(h, who, steps, coeffs, &c);
+    if (rc) return rc;
+    if (batch == 0) return CDGRAB_OK;
+    if (!M || !O) return fail(h, CDGRAB_EINVAL, "%s: null pointer", who);
+    const int64_t size = elem_size(type);
+    if (bad_rows(M, rows, cols, m_stride, size) || bad_rows(O, rows, cols, o_stride, size) ||
+        (batch > 1 && (m_matrix < (rows - 1) * m_stride + cols || o_matrix < (rows - 1) * o_stride + cols ||
+                       m_matrix > (INT64_MAX >> 4) / batch || o_matrix > (INT64_MAX >> 4) / batch)))
+        return fail(h, CDGRAB_EINVAL, "%s: a stride below the size, or a misaligned or too long array", who);
+    if (batch == 1) m_matrix = o_matrix = 0;
+    const int64_t m_len = (batch - 1) * m_matrix + (rows - 1) * m_stride + cols, o_len = (batch - 1) * o_matrix + (rows - 1) * o_stride + cols;
+    if (ranges_overlap(M, m_len * size, O, o_len * size)) return fail(h, CDGRAB_EINVAL, "%s: M and O must not overlap", who);
+    const OnDevice on(h->device);
+    HIP_TRY(h, on.err);
+    const auto by_type = [&](auto elem) {
+        typedef decltype(elem) T;
+        return run_ortho<T>(h, who, batch, rows, cols, (const T *)M, m_stride, m_matrix, steps, c, (T *)O, nullptr, 0.f, o_stride, o_matrix);
     };
     if (type == CDGRAB_F32) return by_type(float{});
     return type == CDGRAB_BF16 ? by_type(bf16_t{}) : by_type(f16_t{});

@@ -440,7 +440,7 @@ __global__ __launch_bounds__(kDeltaWaves * 64) void train_step_delta(const float
 // gradient row of this step into the staging chunk (pair-major: pair (k, i) of the
 // chunk holds rows [2q], [2q+1] with q = (k - k_first) m + i) and optionally into
 // grads_out[m][n][d], forms the average gradient and applies SGD with momentum
-// (v <- momentum v + gbar; w <- w - lr v).
+// (v <- momentum v + gbar; w <- w - lr v; without W the velocity only).
 template <bool PERM>
 __global__ __launch_bounds__(256) void train_step_update(const float *__restrict__ X,
                                                          const int32_t *__restrict__ perm,
@@ -487,7 +487,7 @@ __global__ __launch_bounds__(256) void train_step_update(const float *__restrict
         step = momentum * velocity[p] + gbar;
         velocity[p] = step;
     }
-    W[p] = W[p] - lr * step;
+    if (W) W[p] = W[p] - lr * step;
 }
 
 }  // namespace cdgrab
