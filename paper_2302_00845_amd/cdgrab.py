@@ -389,19 +389,23 @@ def _rows(t: torch.Tensor, name: str, device, like: Optional[torch.Tensor] = Non
         raise TypeError("%s must be float32, bfloat16 or float16, got %s" % (name, t.dtype))
     if t.device != device:
         raise ValueError("%s must live on %s, got %s" % (name, device, t.device))
-    if t.dim() < 2:
-        raise ValueError("%s must have rows and a width, got shape %s" % (name, tuple(t.shape)))
-    if like is not None and (t.dtype != like.dtype or t.shape[:-1] != like.shape[:-1]):
+    shape = t.shape
+    if len(shape) < 2:
+        raise ValueError("%s must have rows and a width, got shape %s" % (name, tuple(shape)))
+    if like is not None and (t.dtype != like.dtype or shape[:-1] != like.shape[:-1]):
         raise ValueError("%s must be %s of rows %s, got %s %s" % (name, like.dtype, tuple(like.shape[:-1]), t.dtype,
-                                                                  tuple(t.shape)))
-    width, rows = t.shape[-1], 1
-    for n in t.shape[:-1]:
+                                                                  tuple(shape)))
+    width = shape[-1]
+    if t.is_contiguous():
+        rows = t.numel() // width if width else 0
+        return t.data_ptr(), rows, width, max(width, 1)
+    rows, stride = 1, width
+    for n in shape[:-1]:
         rows *= n
-    stride = max(width, 1)
     if rows and width:
         if t.stride(-1) != 1 and width > 1:
             raise ValueError("%s: the elements of a row must lie side by side" % name)
-        steps = [(n, s) for n, s in zip(t.shape[:-1], t.stride()[:-1]) if n > 1]
+        steps = [(n, s) for n, s in zip(shape[:-1], t.stride()[:-1]) if n > 1]
         if steps:
             stride = steps[-1][1]
             for (_, outer), (n, inner) in zip(steps, steps[1:]):
@@ -409,7 +413,7 @@ def _rows(t: torch.Tensor, name: str, device, like: Optional[torch.Tensor] = Non
                     raise ValueError("%s: rows must be one distance apart" % name)
             if stride < width:
                 raise ValueError("%s: rows must not overlap" % name)
-    return t.data_ptr(), rows, width, stride
+    return t.data_ptr(), rows, width, max(stride, 1)
 
 
 def _token_rows(X: torch.Tensor, rows: int, first, count, tokens: Optional[int], device) -> _TokenRows:
@@ -431,7 +435,7 @@ def _token_rows(X: torch.Tensor, rows: int, first, count, tokens: Optional[int],
 def _grad_rows(G_out: Optional[torch.Tensor], examples: int, d: int, device):
     """(G, stride): [examples][d] fp32, a stretch of longer rows if given so."""
     if G_out is None:
-        G_out = torch.empty((examples, d), dtype=torch.float32, device=device)
+        return torch.empty((examples, d), dtype=torch.float32, device=device), max(d, 1)
     if G_out.dtype != torch.float32:
         raise TypeError("G_out must be float32, got %s" % G_out.dtype)
     if tuple(G_out.shape) != (examples, d):
@@ -446,10 +450,12 @@ def cdgrab_layernorm(h: Handle, X: torch.Tensor, gain: Optional[torch.Tensor] = 
     """Layer norm over the last axis of X[..., width]; gain and bias [width] float32."""
     px, rows, width, sx = _rows(X, "X", h.device)
     if Y is None:
-        Y = torch.empty(X.shape, dtype=X.dtype, device=h.device)
-    py, _, wy, sy = _rows(Y, "Y", h.device, X)
-    if wy != width:
-        raise ValueError("Y must have shape %s, got %s" % (tuple(X.shape), tuple(Y.shape)))
+        Y = torch.empty_like(X, memory_format=torch.contiguous_format)
+        py, sy = Y.data_ptr(), max(width, 1)
+    else:
+        py, _, wy, sy = _rows(Y, "Y", h.device, X)
+        if wy != width:
+            raise ValueError("Y must have shape %s, got %s" % (tuple(X.shape), tuple(Y.shape)))
     h._check(h._lib.cdgrab_layernorm(
         h._h, rows, width, _ELEM[X.dtype], px, sx, _ptr(gain, torch.float32, (width,), "gain", h.device),
         _ptr(bias, torch.float32, (width,), "bias", h.device), eps, py, sy))
@@ -475,7 +481,7 @@ def cdgrab_pergrad_layernorm(h: Handle, X: torch.Tensor, dY: torch.Tensor, gain:
     if dX is not None or want_dx:
         if dX is None:
             whole = first is None and count is None
-            dX = (torch.empty if whole else torch.zeros)(X.shape, dtype=X.dtype, device=h.device)
+            dX = (torch.empty_like if whole else torch.zeros_like)(X, memory_format=torch.contiguous_format)
         pd, _, wd, sd = _rows(dX, "dX", h.device, X)
         if wd != width:
             raise ValueError("dX must have shape %s, got %s" % (tuple(X.shape), tuple(dX.shape)))
@@ -517,7 +523,7 @@ def cdgrab_orthogonalize(h: Handle, M: torch.Tensor, steps: int = 5, coeffs=None
     if M.dim() not in (2, 3):
         raise ValueError("M must be [rows][cols] or [batch][rows][cols], got %s" % (tuple(M.shape),))
     if out is None:
-        out = torch.empty(M.shape, dtype=M.dtype, device=h.device)
+        out = torch.empty_like(M, memory_format=torch.contiguous_format)
     at = []
     for t, name in ((M, "M"), (out, "out")):
         if t.dtype not in _ELEM:

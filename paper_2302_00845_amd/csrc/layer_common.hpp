@@ -79,8 +79,8 @@ __device__ __forceinline__ float lanes_sum(float x) {
 
 // Workgroup b of `total` as the position in an order in which neighbours run on the same XCD (workgroups go round
 // the eight XCDs): what neighbouring tiles read in common then comes from one L2.
-__device__ __forceinline__ int64_t xcd_neighbours(int64_t b, int64_t total) {
-    const int64_t per = total / 8, rest = total - per * 8, x = b & 7, at = b >> 3;
+__device__ __forceinline__ uint32_t xcd_neighbours(uint32_t b, uint32_t total) {
+    const uint32_t per = total >> 3, rest = total & 7, x = b & 7, at = b >> 3;
     return x * per + (x < rest ? x : rest) + at;
 }
 

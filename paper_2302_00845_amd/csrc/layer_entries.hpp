@@ -122,6 +122,37 @@ void by_norm_type(int32_t type, int64_t width, F &&f) {
     else pick(f16_t{});
 }
 
+// Stores of four elements until they start at the same column again.
+int64_t flat_period(int64_t out_dim) { return out_dim / std::gcd<int64_t>(out_dim, 4); }
+
+// Floats of LDS that a stretch of linear_flat needs at most.
+int64_t flat_lds(int64_t tok, int64_t in_dim, int64_t out_dim, int64_t with_bias) {
+    return tok * (std::min<int64_t>(in_dim + with_bias, (kFlatElems + out_dim - 1) / out_dim + 1) + 1 + out_dim);
+}
+
+template <typename T, int TOK, int THREADS>
+int run_flat(cdgrab_handle *h, const TokenRows &tok, const T *X, int64_t x_stride, const T *D, int64_t d_stride, int64_t in_dim,
+             int64_t out_dim, int with_bias, float *G, int64_t g_stride) {
+    const int64_t d = (in_dim + with_bias) * out_dim, units = (d + 3 + kFlatElems - 1) / kFlatElems;
+    const int64_t per = std::max<int64_t>(1, kMaxGroups / units);
+    // threads whose stores of four elements make whole rows
+    const int period = (int)flat_period(out_dim), active = THREADS / period * period;
+    const auto launch = [&](auto kernel) {
+        for (int64_t e0 = 0; e0 < tok.examples; e0 += per) {
+            TokenRows part = tok;
+            part.examples = std::min(per, tok.examples - e0);
+            part.base = e0;
+            hipLaunchKernelGGL(kernel, dim3((unsigned)(part.examples * units)), dim3(THREADS),
+                               (size_t)flat_lds(TOK, in_dim, out_dim, with_bias) * sizeof(float), h->stream, part, (uint32_t)units, X, x_stride,
+                               D, d_stride, (int)in_dim, (int)out_dim, with_bias, active, G, g_stride);
+        }
+    };
+    if (out_dim < 4) launch(linear_flat<T, TOK, THREADS, true>);
+    else launch(linear_flat<T, TOK, THREADS, false>);
+    HIP_TRY(h, hipGetLastError());
+    return CDGRAB_OK;
+}
+
 template <typename T, int BM, int BN, int WM, int WN>
 int run_linear(cdgrab_handle *h, const TokenRows &tok, const T *X, int64_t x_stride, const T *D, int64_t d_stride, int64_t in_dim,
                int64_t out_dim, int with_bias, float *G, int64_t g_stride) {
@@ -408,6 +439,22 @@ extern "C" int cdgrab_pergrad_linear(cdgrab_handle *h, const cdgrab_token_rows *
         typedef decltype(elem) T;
         const T *x = (const T *)X, *dl = (const T *)D;
         const auto tiles = [&](int64_t bm, int64_t bn) { return ((in_dim + bm - 1) / bm) * ((out_dim + bn - 1) / bn) * tok.examples; };
+        // Few rows per example as outer products, us tiles -> stretches: one row, 784 -> 10, 60 000 examples 2496 -> 451, 768 -> 768, 500
+        // examples 244 -> 206; two rows, 768 -> 768 262 -> 268, 300 -> 250 173 -> 119; four rows, 300 -> 64 133 -> 113, 128 -> 128
+        // 76 -> 94; eight rows, 300 -> 40 115 -> 93, 50 -> 20 141 -> 36, 128 -> 128 76 -> 126.
+        const int64_t flat_tok = tok.tokens <= 2 ? tok.tokens : tok.tokens <= 4 ? 4 : 8;
+        if ((tok.tokens <= 2 || (tok.tokens <= 8 && tok.tokens * out_dim <= 384)) && d < ((int64_t)1 << 31) - 2 * kFlatElems &&
+            flat_period(out_dim) <= 256 && flat_lds(flat_tok, in_dim, out_dim, with_bias) <= kFlatLds) {
+            const auto flat = [&](auto t) {
+                constexpr int TOK = decltype(t)::value;
+                if (d <= 2048 && flat_period(out_dim) <= 64) return run_flat<T, TOK, 64>(h, tok, x, x_stride, dl, d_stride, in_dim, out_dim, with_bias, G, g_stride);
+                return run_flat<T, TOK, 256>(h, tok, x, x_stride, dl, d_stride, in_dim, out_dim, with_bias, G, g_stride);
+            };
+            if (flat_tok <= 1) return flat(std::integral_constant<int, 1>{});
+            if (flat_tok == 2) return flat(std::integral_constant<int, 2>{});
+            if (flat_tok == 4) return flat(std::integral_constant<int, 4>{});
+            return flat(std::integral_constant<int, 8>{});
+        }
         if (out_dim <= 32)
             return run_linear<T, 128, 32, 4, 1>(h, tok, x, x_stride, dl, d_stride, in_dim, out_dim, with_bias, G, g_stride);
         if (in_dim <= 32)

@@ -405,7 +405,8 @@ __global__ __launch_bounds__(256, 2) void ortho_product_tile(OrthoProduct p, Ort
     f16_t *stage = reinterpret_cast<f16_t *>(lds);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave >> 1, wn = wave & 1;
     const int per = SYM ? p.tiles_m * (p.tiles_m + 1) / 2 : p.tiles_m * p.tiles_n;
-    const int64_t id = xcd_neighbours(blockIdx.x, gridDim.x), b = id / per;
+    const uint32_t id = xcd_neighbours(blockIdx.x, gridDim.x);
+    const int64_t b = id / (uint32_t)per;
     int tm, tn;
     if constexpr (SYM) {  // tiles on or above the diagonal, column after column
         const int t = (int)(id - b * per);

@@ -200,7 +200,9 @@ def linear64(x, d, spans, dtype, shares=64):
     ("padded", [0, 5, 2], 5, 129, 33), ("packed", [7, 0, 40, 1], 40, 65, 31), ("padded", [33, 64, 0], 64, 300, 131),
     ("packed", [100, 37], 100, 257, 260), ("dense", [2100], 2100, 70, 90), ("padded", [1999, 4], 2000, 5, 200),
     ("dense", [2] * 300, 2, 150, 140), ("dense", [4] * 6, 4, 785, 10), ("dense", [1] * 9, 1, 20, 2049), ("packed", [31, 33], 33, 1, 500),
-    ("dense", [48] * 40, 48, 384, 256),
+    ("dense", [48] * 40, 48, 384, 256), ("padded", [1, 0, 1], 1, 9000, 3), ("padded", [2, 1, 0], 2, 700, 50), ("packed", [3, 1, 4], 4, 5001, 2),
+    ("padded", [8, 0, 5], 8, 900, 40), ("dense", [1] * 5, 1, 3, 255), ("dense", [1] * 3, 1, 33, 1021), ("padded", [6, 7], 7, 1300, 1),
+    ("dense", [2] * 3, 2, 8191, 1), ("packed", [0, 2], 2, 16, 514),
 ])
 def test_linear(lib, kind, counts, tokens, n_in, n_out, dtype):
     spans, rows, first, count = spans_of(kind, counts, tokens)
