@@ -258,17 +258,24 @@ int run_ortho_products(cdgrab_handle *h, const char *who, int64_t batch, OrthoIo
         const auto go = [&](auto kernel, const OrthoProduct &p, int64_t tiles) {
             hipLaunchKernelGGL(kernel, dim3((unsigned)(n * tiles)), dim3(256), 0, h->stream, p, part);
         };
+        // Stages of LDS: two leave room for two workgroups per CU, four for one, which is what there is when the tiles are few.  (24
+        // matrices of 768 x 768 945 us with two, 1030 with four; 12 of 768 x 2304, whose Gram matrices have 252 tiles, 1203 and 1194.)
         for (int64_t s = 0; s < steps; ++s) {
             const int64_t half = tm * (tm + 1) / 2;
-            go(ortho_product_tile<TILE, kOrthoGram, T>,
-               OrthoProduct{X, X, A, A, lp, lp, sp, x_len, x_len, a_len, (int)lp, (int)tm, (int)tm, 0.f,
-                            kOrthoScaleA / (kOrthoScaleX * kOrthoScaleX)}, half);
-            go(ortho_product_tile<TILE, kOrthoPoly, T>,
-               OrthoProduct{A, A, A, B, sp, sp, sp, a_len, a_len, a_len, (int)sp, (int)tm, (int)tm, (float)c.b,
-                            (float)(c.c / kOrthoScaleA)}, half);
+            const auto sym = [&](auto kernel2, auto kernel4, const OrthoProduct &p) {
+                if (TILE == 64 || n * half <= h->num_cu) go(kernel4, p, half);
+                else go(kernel2, p, half);
+            };
+            sym(ortho_product_tile<TILE, 2, kOrthoGram, T>, ortho_product_tile<TILE, 4, kOrthoGram, T>,
+                OrthoProduct{X, X, A, A, lp, lp, sp, x_len, x_len, a_len, (int)lp, (int)tm, (int)tm, 0.f,
+                             kOrthoScaleA / (kOrthoScaleX * kOrthoScaleX)});
+            sym(ortho_product_tile<TILE, 2, kOrthoPoly, T>, ortho_product_tile<TILE, 4, kOrthoPoly, T>,
+                OrthoProduct{A, A, A, B, sp, sp, sp, a_len, a_len, a_len, (int)sp, (int)tm, (int)tm, (float)c.b,
+                             (float)(c.c / kOrthoScaleA)});
             const OrthoProduct step{B, X, X, Y, sp, lp, lp, a_len, x_len, x_len, (int)sp, (int)tm, (int)tn, (float)c.a, 1.f / kOrthoScaleA};
-            if (s + 1 < steps) go(ortho_product_tile<TILE, kOrthoStep, T>, step, tm * tn);
-            else go(ortho_product_tile<TILE, kOrthoLast, T>, step, tm * tn);
+            constexpr int NS = TILE == 64 ? 4 : 2;
+            if (s + 1 < steps) go(ortho_product_tile<TILE, NS, kOrthoStep, T>, step, tm * tn);
+            else go(ortho_product_tile<TILE, NS, kOrthoLast, T>, step, tm * tn);
             std::swap(X, Y);
         }
     }

@@ -36,6 +36,22 @@ struct OrthoIo {
         if (sub) sub[p] = sub[p] - rate * v;
         else O[p] = (T)v;
     }
+    // Eight results side by side in memory, from element p on, of which the first n are there.
+    __device__ __forceinline__ void put8(int64_t p, const float (&v)[8], int n) const {
+        if (!sub && n >= 8) {
+            T x[8];
+#pragma unroll
+            for (int q = 0; q < 8; ++q) x[q] = (T)v[q];
+            store_any<T, 8>(O + p, x);
+        } else {
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+                if (q < n) {
+                    if (sub) sub[p + q] = sub[p + q] - rate * v[q];
+                    else O[p + q] = (T)v[q];
+                }
+        }
+    }
 };
 
 struct OrthoCoeffs { double a, b, c; };
@@ -347,45 +363,81 @@ enum OrthoWhat { kOrthoGram, kOrthoPoly, kOrthoStep, kOrthoLast };
 // along k), then
 //   Gram: A = X X^T;  Poly: B = b A + c A A;  Step: X' = a X + B X;  Last: O = (a X + B X) to the caller's array.
 // K is a multiple of 32, the tile's sides T of 32: nothing to clip but O.
-// Memory to LDS without registers, sixteen bytes a lane, the next 32 k while these are multiplied.  LDS rows are dense (a wave
+// Memory to LDS without registers, sixteen bytes a lane, NS stages of 32 k on their way or in use.  LDS rows are dense (a wave
 // fills 1 KB in a row); sixteen-byte pieces are swapped within a row by its number, so that the lanes of a read hit different banks.
 template <int T> struct OrthoTile {
-    static constexpr int KC = 32, PLANE = T * KC;  // elements
+    static constexpr int KC = 32, PLANE = T * KC, CALLS = PLANE / 8 / 64 / 4;  // elements; a wavefront's loads per plane
     // piece c of row r of an [T][KC] plane / of a [KC][T] plane (pairs of pieces stay together for the transposing read)
     static __device__ __forceinline__ int along(int r, int c) { return c ^ ((r >> 2) & 3); }
     static __device__ __forceinline__ int across(int r, int c) { return T == 128 ? c ^ ((r & 7) << 1) : c ^ (((r >> 1) & 3) << 1); }
 };
 
-template <int T, bool ACROSS>
-__device__ __forceinline__ void ortho_fetch(const f16_t *src, int64_t ld, f16_t *lds) {
-    typedef OrthoTile<T> O;
-    constexpr int PIECES = ACROSS ? T / 8 : O::KC / 8, ROWS = 64 / PIECES, CALLS = O::PLANE / 8 / 64 / 4;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-    for (int q = 0; q < CALLS; ++q) {
-        const int block = q * 4 + wave, row = block * ROWS + lane / PIECES, slot = lane % PIECES;
-        const int piece = ACROSS ? O::across(row, slot) : O::along(row, slot);
-        typedef __attribute__((address_space(3))) void *Lds;
-        typedef const __attribute__((address_space(1))) void *Mem;
-        __builtin_amdgcn_global_load_lds((Mem)(src + (int64_t)row * ld + piece * 8), (Lds)(lds + block * 512), 16, 0, 0);
-    }
+// Waits until at most LEFT of this wavefront's loads are on their way and its LDS reads are done, then for the workgroup.
+// (By builtins: the compiler then knows that the reads are done, and does not wait for the next ones instead.)
+template <int LEFT>
+__device__ __forceinline__ void ortho_barrier() {
+    static_assert(LEFT < 64, "six bits");
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_s_waitcnt((LEFT & 15) | (LEFT >> 4) << 14 | 7 << 4);  // vmcnt LEFT, lgkmcnt 0, expcnt any
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    __builtin_amdgcn_sched_barrier(0);
 }
 
+// A wavefront's share of a stage's loads of one plane: `from` is the same for all lanes, a lane adds `at[q]` bytes for its q-th load.
 template <int T, bool ACROSS>
-__device__ __forceinline__ f16x8 ortho_operand(const f16_t *lds, int at, int k, int lane) {
+struct OrthoFetch {
     typedef OrthoTile<T> O;
-    if constexpr (!ACROSS) {  // row at + lane % 32, elements k + 8 (lane / 32) ..
-        const int row = at + (lane & 31);
-        return *reinterpret_cast<const f16x8 *>(lds + row * O::KC + O::along(row, (k >> 3) + (lane >> 5)) * 8);
-    } else {
-        typedef __attribute__((address_space(3))) s16x4 *Ptr;
-        const int row = k + (lane >> 5) * 8 + ((lane & 15) >> 2), col = at + (lane & 16) + (lane & 3) * 4;
-        const f16_t *p0 = lds + row * T + O::across(row, col >> 3) * 8 + (col & 4);
-        const f16_t *p1 = lds + (row + 4) * T + O::across(row + 4, col >> 3) * 8 + (col & 4);
-        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Ptr)p0), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Ptr)p1);
-        return __builtin_bit_cast(f16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    uint32_t at[O::CALLS];
+    __device__ __forceinline__ OrthoFetch(int64_t ld, int wave, int lane) {
+        constexpr int PIECES = ACROSS ? T / 8 : O::KC / 8, ROWS = 64 / PIECES;
+#pragma unroll
+        for (int q = 0; q < O::CALLS; ++q) {
+            const int row = (q * 4 + wave) * ROWS + lane / PIECES, slot = lane % PIECES;
+            at[q] = (uint32_t)(row * (int)ld + (ACROSS ? O::across(row, slot) : O::along(row, slot)) * 8) * 2u;
+        }
     }
-}
+    __device__ __forceinline__ void operator()(const f16_t *from, f16_t *lds, int wave) const {
+        typedef __attribute__((address_space(3))) void *Lds;
+        typedef const __attribute__((address_space(1))) void *Mem;
+#pragma unroll
+        for (int q = 0; q < O::CALLS; ++q)
+            __builtin_amdgcn_global_load_lds((Mem)(reinterpret_cast<const char *>(from) + at[q]), (Lds)(lds + (q * 4 + wave) * 512), 16, 0, 0);
+    }
+};
+
+// A lane's operands of 32 x 32 x 16 MFMAs: `at[k / 16]` is where those of the tile's first 32 rows (columns) lie in a plane,
+// those of the i-th next are a constant further, as the planes and stages are.
+template <int T, bool ACROSS>
+struct OrthoRead {
+    typedef OrthoTile<T> O;
+    int at[2], at4[2];  // (in elements; at4: the second half of a transposing read)
+    __device__ __forceinline__ OrthoRead(int first, int lane) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            if constexpr (!ACROSS) {  // row first + lane % 32, elements 16 h + 8 (lane / 32) ..
+                const int row = first + (lane & 31);
+                at[h] = row * O::KC + O::along(row, 2 * h + (lane >> 5)) * 8;
+            } else {
+                const int row = 16 * h + (lane >> 5) * 8 + ((lane & 15) >> 2), col = first + (lane & 16) + (lane & 3) * 4;
+                at[h] = row * T + O::across(row, col >> 3) * 8 + (col & 4);
+                at4[h] = (row + 4) * T + O::across(row + 4, col >> 3) * 8 + (col & 4);
+            }
+        }
+    }
+    // (ACROSS: columns are swapped by exclusive or, and so are those 32 further, since `first` is a multiple of 64)
+    __device__ __forceinline__ f16x8 operator()(const f16_t *plane, int h, int i) const {
+        if constexpr (!ACROSS) {
+            return *reinterpret_cast<const f16x8 *>(plane + at[h] + i * 32 * O::KC);
+        } else {
+            typedef __attribute__((address_space(3))) s16x4 *Ptr;
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Ptr)(plane + (at[h] ^ (i * 32))));
+            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Ptr)(plane + (at4[h] ^ (i * 32))));
+            return __builtin_bit_cast(f16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        }
+    }
+};
 
 struct OrthoProduct {
     OrthoPair L, R, E, C;  // factors, what is added, the result
@@ -394,16 +446,16 @@ struct OrthoProduct {
     float alpha, beta;  // result = alpha E + beta (product as multiplied)
 };
 
-template <int T, int WHAT, typename U>
-__global__ __launch_bounds__(256, 2) void ortho_product_tile(OrthoProduct p, OrthoIo<U> io)
+template <int T, int NS, int WHAT, typename U>
+__global__ __launch_bounds__(256, NS * T * 256 > 80 * 1024 ? 1 : 2) void ortho_product_tile(OrthoProduct p, OrthoIo<U> io)
 {
     constexpr bool ACROSS = WHAT == kOrthoStep || WHAT == kOrthoLast, SYM = !ACROSS;
     typedef OrthoTile<T> O;
-    constexpr int MB = T / 64, LD = T + 4;
-    constexpr int STAGE = 4 * O::PLANE, BYTES = 2 * STAGE * 2, OUT = T / 2 * LD * 4;
+    constexpr int MB = T / 64, LD = T + 1;  // (eight rows further is eight banks further)
+    constexpr int STAGE = 4 * O::PLANE, BYTES = NS * STAGE * 2, OUT = T / 2 * LD * 4, LOADS = 4 * O::CALLS;
     __shared__ __align__(16) char lds[BYTES > OUT ? BYTES : OUT];
     f16_t *stage = reinterpret_cast<f16_t *>(lds);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave >> 1, wn = wave & 1;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave >> 1, wn = wave & 1;
     const int per = SYM ? p.tiles_m * (p.tiles_m + 1) / 2 : p.tiles_m * p.tiles_n;
     const uint32_t id = xcd_neighbours(blockIdx.x, gridDim.x);
     const int64_t b = id / (uint32_t)per;
@@ -431,44 +483,107 @@ __global__ __launch_bounds__(256, 2) void ortho_product_tile(OrthoProduct p, Ort
         for (int j = 0; j < MB; ++j)
 #pragma unroll
             for (int q = 0; q < 16; ++q) acc[i][j][q] = low[i][j][q] = 0.f;
-    const auto fetch = [&](int k, int buf) {
+    const OrthoFetch<T, false> fetch_l(p.l_ld, wave, lane);
+    const OrthoFetch<T, ACROSS> fetch_r(p.r_ld, wave, lane);
+    const auto fetch = [&](int q, int buf) {
         f16_t *s = stage + buf * STAGE;
-        ortho_fetch<T, false>(src[0] + k, p.l_ld, s);
-        ortho_fetch<T, false>(src[1] + k, p.l_ld, s + O::PLANE);
-        const int64_t off = ACROSS ? (int64_t)k * p.r_ld : k;
-        ortho_fetch<T, ACROSS>(src[2] + off, p.r_ld, s + 2 * O::PLANE);
-        ortho_fetch<T, ACROSS>(src[3] + off, p.r_ld, s + 3 * O::PLANE);
+        const int k = q * O::KC;
+        const int64_t off = ACROSS ? k * p.r_ld : k;
+        fetch_l(src[0] + k, s, wave);
+        fetch_l(src[1] + k, s + O::PLANE, wave);
+        fetch_r(src[2] + off, s + 2 * O::PLANE, wave);
+        fetch_r(src[3] + off, s + 3 * O::PLANE, wave);
     };
-    fetch(0, 0);
-    int buf = 0;
-    for (int k = 0; k < p.k; k += O::KC, buf ^= 1) {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wavefront's part of the stage is there; then everybody's
-        __syncthreads();
-        if (k + O::KC < p.k) fetch(k + O::KC, buf ^ 1);
+    struct Operands { f16x8 lh[MB], ll[MB], rh[MB], rl[MB]; };
+    const OrthoRead<T, false> read_l(wm * (T / 2), lane);
+    const OrthoRead<T, ACROSS> read_r(wn * (T / 2), lane);
+    const auto read = [&](Operands &o, int buf, int h) {
         const f16_t *s = stage + buf * STAGE;
 #pragma unroll
-        for (int kk = 0; kk < O::KC; kk += 16) {
-            f16x8 lh[MB], ll[MB], rh[MB], rl[MB];
-#pragma unroll
-            for (int i = 0; i < MB; ++i) {
-                lh[i] = ortho_operand<T, false>(s, wm * (T / 2) + i * 32, kk, lane);
-                ll[i] = ortho_operand<T, false>(s + O::PLANE, wm * (T / 2) + i * 32, kk, lane);
-                rh[i] = ortho_operand<T, ACROSS>(s + 2 * O::PLANE, wn * (T / 2) + i * 32, kk, lane);
-                rl[i] = ortho_operand<T, ACROSS>(s + 3 * O::PLANE, wn * (T / 2) + i * 32, kk, lane);
-            }
-#pragma unroll
-            for (int i = 0; i < MB; ++i)
-#pragma unroll
-                for (int j = 0; j < MB; ++j) {
-                    low[i][j] = mfma32(lh[i], rl[j], low[i][j]);
-                    acc[i][j] = mfma32(lh[i], rh[j], acc[i][j]);
-                    low[i][j] = mfma32(ll[i], rh[j], low[i][j]);
-                }
+        for (int i = 0; i < MB; ++i) {
+            o.lh[i] = read_l(s, h, i);
+            o.rl[i] = read_r(s + 3 * O::PLANE, h, i);
+            o.rh[i] = read_r(s + 2 * O::PLANE, h, i);
+            o.ll[i] = read_l(s + O::PLANE, h, i);
         }
-    }
+    };
+    const auto multiply = [&](const Operands &o) {  // (products that add to the same sum apart from each other)
+#pragma unroll
+        for (int i = 0; i < MB; ++i)
+#pragma unroll
+            for (int j = 0; j < MB; ++j) low[i][j] = mfma32(o.lh[i], o.rl[j], low[i][j]);
+#pragma unroll
+        for (int i = 0; i < MB; ++i)
+#pragma unroll
+            for (int j = 0; j < MB; ++j) acc[i][j] = mfma32(o.lh[i], o.rh[j], acc[i][j]);
+#pragma unroll
+        for (int i = 0; i < MB; ++i)
+#pragma unroll
+            for (int j = 0; j < MB; ++j) low[i][j] = mfma32(o.ll[i], o.rh[j], low[i][j]);
+    };
+    const auto interleave = [] {  // a few reads, a few products, and so on (left alone, the compiler puts the reads last)
+#pragma unroll
+        for (int q = 0; q < 6; ++q) {
+            __builtin_amdgcn_sched_group_barrier(0x100, ACROSS ? 3 : 2, 0);
+            __builtin_amdgcn_sched_group_barrier(0x8, MB, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    // Half a stage's operands are read while the other half's products run; between the halves the workgroup meets: the next
+    // stage is there, and everybody has read this one, whose place the next loads take.
+    const int stages = p.k / O::KC;
+    int sent = 0;
+    for (; sent < NS && sent < stages; ++sent) fetch(sent, sent);
+    if (sent == NS) ortho_barrier<(NS - 1) * LOADS>();
+    else ortho_barrier<0>();
+    Operands first, second;
+    read(first, 0, 0);
+    for (int q0 = 0; q0 + 1 < stages; q0 += NS)
+#pragma unroll
+        for (int buf = 0; buf < NS; ++buf) {  // (a constant: so are the places in LDS)
+            const int q = q0 + buf;
+            if (q + 1 >= stages) break;
+            read(second, buf, 1);
+            multiply(first);
+            interleave();
+            if (q + NS <= stages) ortho_barrier<(NS - 2) * LOADS>();
+            else ortho_barrier<0>();
+            if (sent < stages) fetch(sent++, buf);
+            read(first, (buf + 1) % NS, 0);
+            multiply(second);
+            interleave();
+        }
+    read(second, (stages - 1) % NS, 1);
+    multiply(first);
+    multiply(second);
     // The tile goes out through LDS, half its rows at a time, so that every thread stores eight neighbours of a row; a tile
-    // above the diagonal also to its mirror image.
+    // above the diagonal also to its mirror image.  What is added is requested before the first half is written.
+    constexpr int TASKS = T / 2 * T / 8 / 256;  // of a thread, per half
+    const int64_t c_tile = b * p.c_matrix + (int64_t)tm * T * p.c_ld + tn * T;
+    f16x8 e_hi[2][TASKS], e_lo[2][TASKS];
+    if constexpr (WHAT != kOrthoGram)
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int u = 0; u < TASKS; ++u) {
+                const int q = threadIdx.x + u * 256;
+                const int64_t at = c_tile + (int64_t)(half * (T / 2) + q / (T / 8)) * p.c_ld + q % (T / 8) * 8;
+                e_hi[half][u] = *reinterpret_cast<const f16x8 *>(p.E.hi + at);
+                e_lo[half][u] = *reinterpret_cast<const f16x8 *>(p.E.lo + at);
+            }
     float *out = reinterpret_cast<float *>(lds);
+    const auto store = [&](const float (&v)[8], int64_t at) {
+        f16x8 hi, lo;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            f16_t x, y;
+            ortho_split(v[j], x, y);
+            hi[j] = x;
+            lo[j] = y;
+        }
+        *reinterpret_cast<f16x8 *>(p.C.hi + at) = hi;
+        *reinterpret_cast<f16x8 *>(p.C.lo + at) = lo;
+    };
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
         __syncthreads();
@@ -479,59 +594,48 @@ __global__ __launch_bounds__(256, 2) void ortho_product_tile(OrthoProduct p, Ort
                 for (int j = 0; j < MB; ++j)
 #pragma unroll
                     for (int q = 0; q < 16; ++q)
-                        out[(i * 32 + 8 * (q >> 2) + 4 * (lane >> 5) + (q & 3)) * LD + wn * (T / 2) + j * 32 + (lane & 31)] = acc[i][j][q] + low[i][j][q];
+                        out[(i * 32 + 8 * (q >> 2) + 4 * (lane >> 5) + (q & 3)) * LD + wn * (T / 2) + j * 32 + (lane & 31)] =
+                            p.beta * (acc[i][j][q] + low[i][j][q]);
         __syncthreads();
+        // the values are read from LDS once more, along the other side
+        const bool turn = WHAT == kOrthoLast && io.o_i < io.o_j;  // (the caller's rows are the long side)
+        const bool again = turn || (SYM && tm != tn);
         const int m0 = tm * T + half * (T / 2), n0 = tn * T;
-        const auto put = [&](const float (&v)[8], int64_t row, int col) {
-            const int64_t at = b * p.c_matrix + row * p.c_ld + col;
-            f16x8 hi, lo, e_hi, e_lo;
-            if constexpr (WHAT != kOrthoGram) {
-                e_hi = *reinterpret_cast<const f16x8 *>(p.E.hi + at);
-                e_lo = *reinterpret_cast<const f16x8 *>(p.E.lo + at);
-            }
+#pragma unroll
+        for (int u = 0; u < TASKS; ++u) {
+            const int q = threadIdx.x + u * 256, r = q / (T / 8), c = q % (T / 8) * 8;
+            float v[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                float x = p.beta * v[j];
-                if constexpr (WHAT != kOrthoGram) x = fmaf(p.alpha, (float)e_hi[j] + (float)e_lo[j], x);
-                f16_t a, c;
-                ortho_split(x, a, c);
-                hi[j] = a;
-                lo[j] = c;
-            }
-            *reinterpret_cast<f16x8 *>(p.C.hi + at) = hi;
-            *reinterpret_cast<f16x8 *>(p.C.lo + at) = lo;
-        };
-        if constexpr (WHAT != kOrthoLast) {
-            for (int q = threadIdx.x; q < T / 2 * T / 8; q += 256) {
-                const int r = q / (T / 8), c = q % (T / 8) * 8;
-                float v[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = out[r * LD + c + j];
-                put(v, m0 + r, n0 + c);
-            }
-            if (SYM && tm != tn)
-                for (int q = threadIdx.x; q < T / 2 * T / 8; q += 256) {
-                    const int c = q / (T / 16), r = q % (T / 16) * 8;
-                    float v[8];
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) v[j] = out[(r + j) * LD + c];
-                    put(v, n0 + c, m0 + r);
+                v[j] = out[r * LD + c + j];
+                if constexpr (WHAT != kOrthoGram) {
+                    v[j] = fmaf(p.alpha, (float)e_hi[half][u][j] + (float)e_lo[half][u][j], v[j]);
+                    if (again) out[r * LD + c + j] = v[j];
                 }
-        } else {
-            for (int q = threadIdx.x; q < T / 2 * T / 8; q += 256) {
-                const int r = q / (T / 8), c = q % (T / 8) * 8;
-                const int64_t at = b * p.c_matrix + (int64_t)(m0 + r) * p.c_ld + n0 + c;
-                const f16x8 e_hi = *reinterpret_cast<const f16x8 *>(p.E.hi + at), e_lo = *reinterpret_cast<const f16x8 *>(p.E.lo + at);
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    out[r * LD + c + j] = fmaf(p.alpha, (float)e_hi[j] + (float)e_lo[j], p.beta * out[r * LD + c + j]);
             }
-            __syncthreads();
-            const bool turn = io.o_i < io.o_j;  // the caller's rows are the long side
-            for (int q = threadIdx.x; q < T / 2 * T; q += 256) {
-                const int r = turn ? q % (T / 2) : q / T, c = turn ? q / (T / 2) : q % T;
-                if (m0 + r < io.short_side && n0 + c < io.long_side)
-                    io.put(b, m0 + r, n0 + c, out[r * LD + c] * (1.f / kOrthoScaleX));
+            if constexpr (WHAT != kOrthoLast) {
+                store(v, c_tile + (int64_t)(half * (T / 2) + r) * p.c_ld + c);
+            } else if (!turn && m0 + r < io.short_side) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] *= 1.f / kOrthoScaleX;
+                io.put8(b * io.o_matrix + (m0 + r) * io.o_i + (n0 + c), v, io.long_side - n0 - c);
+            }
+        }
+        if (!again) continue;
+        __syncthreads();
+        const int64_t mirror = b * p.c_matrix + (int64_t)n0 * p.c_ld + m0;
+#pragma unroll
+        for (int u = 0; u < TASKS; ++u) {
+            const int q = threadIdx.x + u * 256, c = q / (T / 16), r = q % (T / 16) * 8;
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = out[(r + j) * LD + c];
+            if constexpr (WHAT != kOrthoLast) {
+                store(v, mirror + (int64_t)c * p.c_ld + r);
+            } else if (n0 + c < io.long_side) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] *= 1.f / kOrthoScaleX;
+                io.put8(b * io.o_matrix + (n0 + c) * io.o_j + (m0 + r), v, io.short_side - m0 - r);
             }
         }
     }
