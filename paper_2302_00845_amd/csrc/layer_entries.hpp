@@ -3,7 +3,7 @@
 
 namespace {
 
-constexpr int64_t kOrthoOneGroup = 4096;                     // columns that one workgroup of the narrow form takes by itself
+constexpr int64_t kOrthoSmallLds = 152 * 1024, kOrthoSmallLdsHalf = 76 * 1024;  // of a matrix that one workgroup holds
 constexpr int64_t kOrthoBytes = (int64_t)4 << 30;            // workspace of the products' form: as many matrices at a time
 constexpr int64_t kOrthoMaxShort = 16384;
 constexpr int64_t kOrthoMaxSide = (int64_t)1 << 20;
@@ -167,6 +167,9 @@ int run_linear(cdgrab_handle *h, const TokenRows &tok, const T *X, int64_t x_str
         const int rc = layer_room(h, "cdgrab_pergrad_linear", shares * tok.examples * d, &parts);
         if (rc) return rc;
     }
+    // Neighbouring tiles along G's rows write whole lines between them (200 examples of one token, 768 -> 2304: 319 -> 267 us); along
+    // the side of fewer tiles they read less, which counts with many tokens (32 of 1024: 236 -> 212).
+    const int down = tok.tokens >= 512 && in_dim < out_dim;
     const int64_t per = std::max<int64_t>(1, kMaxGroups / (tiles * shares));  // examples per launch
     for (int64_t e0 = 0; e0 < tok.examples; e0 += per) {
         const int64_t n = std::min(per, tok.examples - e0);
@@ -174,7 +177,7 @@ int run_linear(cdgrab_handle *h, const TokenRows &tok, const T *X, int64_t x_str
         part.examples = n;
         part.base = e0;
         hipLaunchKernelGGL((linear_grad<T, BM, BN, WM, WN>), dim3((unsigned)(n * tiles * shares)), dim3(kLinearThreads), 0, h->stream,
-                           part, (int)shares, X, x_stride, D, d_stride, (int)in_dim, (int)out_dim, with_bias,
+                           part, (int)shares, X, x_stride, D, d_stride, (int)in_dim, (int)out_dim, with_bias, down,
                            shares > 1 ? parts : G, shares > 1 ? d : g_stride, tok.examples * d);
     }
     if (shares > 1)
@@ -185,27 +188,42 @@ int run_linear(cdgrab_handle *h, const TokenRows &tok, const T *X, int64_t x_str
 }
 
 // The largest singular value that the steps can make of values up to 1: they are refused beyond what the kernels' scales
-// have room for (X up to 3.5, the factor b A + c A^2 up to 30).
+// have room for (X up to 3.5, the factor b A + c A^2 up to 30).  With l = s^2 a step takes s to s (a + b l + c l^2); both that
+// and the factor are largest at an end of 0 .. most^2 or where their slopes are zero.
 bool ortho_in_range(int64_t steps, const OrthoCoeffs &c) {
+    if (!std::isfinite(c.a) || !std::isfinite(c.b) || !std::isfinite(c.c)) return false;
     double most = 1.0001;
     for (int64_t s = 0; s < steps; ++s) {
+        const double end = most * most;
+        double at[4] = {end, end, end, end};
+        const double square = 9.0 * c.b * c.b - 20.0 * c.a * c.c;
+        if (c.c != 0.0) {
+            at[0] = -c.b / (2.0 * c.c);
+            if (square >= 0.0) {
+                at[1] = (-3.0 * c.b + std::sqrt(square)) / (10.0 * c.c);
+                at[2] = (-3.0 * c.b - std::sqrt(square)) / (10.0 * c.c);
+            }
+        } else if (c.b != 0.0) {
+            at[1] = -c.a / (3.0 * c.b);
+        }
         double next = 0.0;
-        for (int q = 0; q <= 2000; ++q) {
-            const double x = most * q / 2000, l = x * x, poly = c.b * l + c.c * l * l, y = std::abs(x * (c.a + poly));
-            if (!(std::abs(poly) <= 30.0 && y <= 3.5)) return false;  // (NaN is refused here too)
+        for (double l : at) {
+            l = std::max(0.0, std::min(l, end));
+            const double factor = c.b * l + c.c * l * l, y = std::abs(std::sqrt(l) * (c.a + factor));
+            if (!(std::abs(factor) <= 30.0 && y <= 3.5)) return false;
             next = std::max(next, y);
         }
         most = 1.001 * next;
-        if (!(most <= 3.5)) return false;
     }
-    return true;
+    return most <= 3.51;
 }
 
 template <int NT, typename T>
 int run_ortho_narrow(cdgrab_handle *h, const char *who, int64_t batch, OrthoIo<T> io, int64_t steps, const OrthoCoeffs &c) {
     constexpr int64_t N = NT * 16;
-    // one workgroup per matrix while a matrix is short or there are enough of them
-    if (io.long_side <= kOrthoOneGroup || batch >= h->num_cu) {
+    // one workgroup per matrix while a matrix is short or there are enough of them (us of one launch -> three: 12 x 4000 46 -> 27, 30 x
+    // 1000 37 -> 27, 64 x 512 111 -> 73)
+    if (io.long_side <= 1024 / (NT * NT) * 2 || batch >= h->num_cu) {
         hipLaunchKernelGGL((ortho_narrow<NT, T>), dim3((unsigned)batch), dim3(kOrthoThreads), 0, h->stream, io, (int)steps, c);
         HIP_TRY(h, hipGetLastError());
         return CDGRAB_OK;
@@ -283,6 +301,25 @@ int run_ortho_products(cdgrab_handle *h, const char *who, int64_t batch, OrthoIo
     return CDGRAB_OK;
 }
 
+// The padded sides of a matrix for ortho_small, and whether it takes one: a short side above 32 (below, the narrow form is as
+// fast) and at most 128, at most 32 blocks, LDS for all of it.  Blocks in units of one as long as there is a wavefront for each.
+struct OrthoSmall {
+    int64_t sp, lp, bytes;
+    int per;
+    bool fits;
+    OrthoSmall(int64_t s, int64_t l) {
+        sp = round_up(s, 32);
+        lp = round_up(l, 32);
+        per = sp * lp <= 8 * 1024 && sp <= 64 ? 1 : 2;
+        if (per == 2) {  // (whole units)
+            sp = round_up(s, 64);
+            lp = round_up(l, 64);
+        }
+        bytes = 4 * sp * (lp + 8 + sp + 8);
+        fits = s > 32 && s <= 128 && sp * lp <= 32 * 1024 && bytes <= kOrthoSmallLds;
+    }
+};
+
 // M and O (or `sub`) of `batch` matrices of rows x cols, `m_row` / `o_row` elements from row to row.
 template <typename T>
 int run_ortho(cdgrab_handle *h, const char *who, int64_t batch, int64_t rows, int64_t cols, const T *M, int64_t m_row, int64_t m_matrix,
@@ -292,7 +329,8 @@ int run_ortho(cdgrab_handle *h, const char *who, int64_t batch, int64_t rows, in
                         (int)std::min(rows, cols), (int)std::max(rows, cols)};
     if (io.short_side <= 16) return run_ortho_narrow<1>(h, who, batch, io, steps, c);
     if (io.short_side <= 32) return run_ortho_narrow<2>(h, who, batch, io, steps, c);
-    if (io.short_side <= kOrthoNarrow) return run_ortho_narrow<4>(h, who, batch, io, steps, c);
+    if (io.short_side <= kOrthoNarrow && (steps == 0 || !OrthoSmall(io.short_side, io.long_side).fits))
+        return run_ortho_narrow<4>(h, who, batch, io, steps, c);
     if (steps == 0) {
         for (int64_t b0 = 0; b0 < batch; b0 += 32768) {
             const int64_t n = std::min<int64_t>(32768, batch - b0);
@@ -308,6 +346,18 @@ int run_ortho(cdgrab_handle *h, const char *who, int64_t batch, int64_t rows, in
             hipLaunchKernelGGL((ortho_scaled<T>), dim3((unsigned)std::min<int64_t>((rows * cols + 1023) / 1024, 4096), (unsigned)n), dim3(256),
                                0, h->stream, part, sums);
         }
+        HIP_TRY(h, hipGetLastError());
+        return CDGRAB_OK;
+    }
+    const OrthoSmall small(io.short_side, io.long_side);
+    if (small.fits) {
+        const auto go = [&](auto kernel) {
+            hipLaunchKernelGGL(kernel, dim3((unsigned)batch), dim3(kOrthoSmallThreads), 0, h->stream, io, (int)small.sp, (int)small.lp,
+                               (int)steps, c);
+        };
+        if (small.per == 1) go(ortho_small<T, kOrthoSmallLdsHalf, 1>);
+        else if (small.bytes <= kOrthoSmallLdsHalf) go(ortho_small<T, kOrthoSmallLdsHalf, 2>);
+        else go(ortho_small<T, kOrthoSmallLds, 2>);
         HIP_TRY(h, hipGetLastError());
         return CDGRAB_OK;
     }

@@ -6,15 +6,9 @@
 // MFMA operand wants the tokens side by side: tiles go to LDS as they come, [token][feature], and ds_read_tr16 turns them
 // on the way to the registers.
 #pragma once
-#include "layer_common.hpp"
+#include "mfma_tiles.hpp"
 
 namespace cdgrab {
-
-typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef short s16x8 __attribute__((ext_vector_type(8)));
-typedef bf16_t bf16x8 __attribute__((ext_vector_type(8)));
-typedef f16_t f16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kLinearThreads = 256;
 constexpr int kLinearPad = 16;  // elements behind each LDS row: sixteen lanes of a transposing read then hit distinct banks
@@ -24,9 +18,6 @@ constexpr int kLinearPad = 16;  // elements behind each LDS row: sixteen lanes o
 // fp32 MFMA).
 template <typename T> struct LinearPlanes { static constexpr int N = 1, KC = 32; typedef T elem; };
 template <> struct LinearPlanes<float> { static constexpr int N = 3, KC = 16; typedef bf16_t elem; };
-
-__device__ __forceinline__ f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
-__device__ __forceinline__ f32x16 mfma32(f16x8 a, f16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 
 // Operand of a 32 x 32 x 16 MFMA from LDS [token][feature]: lane l holds feature l % 32 of tokens 8 (l / 32) .. + 7.
 // (A transposing read: sixteen lanes give four tokens' addresses, four lanes a token, and each receives one feature's four.)
@@ -106,12 +97,13 @@ struct LinearStage {
     }
 };
 
-// WAVES_M x WAVES_N wavefronts share the tile.  grid: (example, share of its tokens, tile); `shares` > 1: the sums of a share
+// WAVES_M x WAVES_N wavefronts share the tile.  grid: (example, share of its tokens, tile), neighbours down G's columns or along
+// its rows; `shares` > 1: the sums of a share
 // go to `to` + share * share_stride, which linear_grad_finish adds up in order.
 template <typename T, int BM, int BN, int WAVES_M, int WAVES_N>
 __global__ __launch_bounds__(kLinearThreads) void linear_grad(TokenRows tok, int shares, const T *__restrict__ X, int64_t x_stride,
                                                               const T *__restrict__ D, int64_t d_stride, int in_dim, int out_dim,
-                                                              int with_bias, float *__restrict__ to, int64_t to_stride,
+                                                              int with_bias, int down, float *__restrict__ to, int64_t to_stride,
                                                               int64_t share_stride)
 {
     typedef LinearPlanes<T> P;
@@ -127,7 +119,7 @@ __global__ __launch_bounds__(kLinearThreads) void linear_grad(TokenRows tok, int
     const uint32_t b = xcd_neighbours(blockIdx.x, gridDim.x), tiles = (uint32_t)(mt * nt), rest = b / tiles, tile = b - rest * tiles;
     const int share = (int)(rest % (uint32_t)shares);
     const int64_t e = tok.base + rest / (uint32_t)shares;
-    const int m0 = (int)(tile / nt) * BM, n0 = (int)(tile % nt) * BN;
+    const int m0 = (int)(down ? tile % mt : tile / nt) * BM, n0 = (int)(down ? tile / mt : tile % nt) * BN;
     const RowSpan span = rows_of(tok, e);
     int64_t per = (span.count + shares - 1) / shares;
     const int64_t begin = span.first + (share * per < span.count ? share * per : span.count);

@@ -14,7 +14,8 @@
 //     element, and a fixed power of two in front keeps the parts normal.  A and A^2 are symmetric: half of their tiles are
 //     computed.
 #pragma once
-#include "linear_kernels.hpp"
+#include "narrow_common.hpp"
+#include "mfma_tiles.hpp"
 
 namespace cdgrab {
 
@@ -63,82 +64,131 @@ __device__ __forceinline__ double ortho_root(double t) { return t == 0.0 ? 0.0 :
 constexpr int kOrthoNarrow = 64;
 constexpr int kOrthoThreads = 1024;
 
-// A product of NT x NT tiles of 16 x 16 in LDS (row-major, row length LD): wavefront w takes tile w, if there is one.  Lane l
-// holds entries (4 v + l / 16, l % 16), v = 0 .. 3, of its tile.
-template <int NT, int LD>
+// Symmetric matrices of NT x NT tiles of 16 x 16, a tile as a 16 x 16 x 4 MFMA leaves it: lane l holds entries (4 v + l / 16, l % 16),
+// v = 0 .. 3, and they lie in LDS in that order, [tile][v][lane].  Read as an operand, entry v of tile (k, i) is what the v-th
+// MFMA of a product wants of tile (i, k), its transpose, on the left and of tile (k, i) itself on the right: no other layout
+// is needed, and neither shuffles nor padding.
+template <int NT>
 struct OrthoTiles {
     static_assert(NT * NT <= kOrthoThreads / 64, "a wavefront per tile");
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    static constexpr int LEN = NT * NT * 256;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const bool mine = wave < NT * NT;
-    const int row = (wave / NT) * 16 + (lane >> 4), col = (wave % NT) * 16 + (lane & 15);  // of entry v = 0
+    const int ti = wave / NT, tj = wave % NT;
 
-    __device__ __forceinline__ f64x4 product(const double *A, const double *B) const {
-        f64x4 acc = {0.0, 0.0, 0.0, 0.0};
+    // this wavefront's tile of X Y, X and Y in LDS
+    __device__ __forceinline__ f64x4 product(const double *X, const double *Y) const {
+        f64x4 even = {0.0, 0.0, 0.0, 0.0}, odd = {0.0, 0.0, 0.0, 0.0};
         if (mine) {
-            const double *a = A + ((wave / NT) * 16 + (lane & 15)) * LD + (lane >> 4), *b = B + (lane >> 4) * LD + col;
+            const double *x = X + ti * 256 + lane, *y = Y + tj * 256 + lane;
 #pragma unroll
-            for (int q = 0; q < NT * 4; ++q)
-                acc = __builtin_amdgcn_mfma_f64_16x16x4f64(a[q * 4], b[q * 4 * LD], acc, 0, 0, 0);
+            for (int k = 0; k < NT; ++k)
+#pragma unroll
+                for (int v = 0; v < 4; v += 2) {
+                    even = __builtin_amdgcn_mfma_f64_16x16x4f64(x[k * NT * 256 + v * 64], y[k * NT * 256 + v * 64], even, 0, 0, 0);
+                    odd = __builtin_amdgcn_mfma_f64_16x16x4f64(x[k * NT * 256 + v * 64 + 64], y[k * NT * 256 + v * 64 + 64], odd, 0, 0, 0);
+                }
         }
-        return acc;
+        return even + odd;
     }
-    __device__ __forceinline__ void store(double *C, f64x4 x) const {
+    static __device__ __forceinline__ f64x4 product(f64x4 x, f64x4 y) {  // (of single tiles in registers)
+        f64x4 even = {0.0, 0.0, 0.0, 0.0}, odd = {0.0, 0.0, 0.0, 0.0};
+        even = __builtin_amdgcn_mfma_f64_16x16x4f64(x[0], y[0], even, 0, 0, 0);
+        odd = __builtin_amdgcn_mfma_f64_16x16x4f64(x[1], y[1], odd, 0, 0, 0);
+        even = __builtin_amdgcn_mfma_f64_16x16x4f64(x[2], y[2], even, 0, 0, 0);
+        odd = __builtin_amdgcn_mfma_f64_16x16x4f64(x[3], y[3], odd, 0, 0, 0);
+        return even + odd;
+    }
+    __device__ __forceinline__ f64x4 load(const double *X) const {
+        f64x4 x = {0.0, 0.0, 0.0, 0.0};
         if (mine)
 #pragma unroll
-            for (int v = 0; v < 4; ++v) C[(row + 4 * v) * LD + col] = x[v];
+            for (int v = 0; v < 4; ++v) x[v] = X[wave * 256 + v * 64 + lane];
+        return x;
+    }
+    __device__ __forceinline__ void store(double *X, f64x4 x) const {
+        if (mine)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) X[wave * 256 + v * 64 + lane] = x[v];
+    }
+    // s on the diagonal, for the first n rows
+    __device__ __forceinline__ f64x4 diagonal(double s, int n) const {
+        f64x4 x;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) x[v] = ti == tj && 4 * v + (lane >> 4) == (lane & 15) && ti * 16 + (lane & 15) < n ? s : 0.0;
+        return x;
+    }
+    // where entry (i, j) lies
+    static __device__ __forceinline__ int at(int i, int j) {
+        return ((i >> 4) * NT + (j >> 4)) * 256 + ((i & 15) >> 2) * 64 + (i & 3) * 16 + (j & 15);
     }
 };
 
 // P (in LDS) from the Gram matrix of M in A (in LDS), entries beyond the short side zero:
 //   A <- A / trace(A), P <- I / sqrt(trace); steps times: Q = a I + b A + c A^2, P <- Q P, A <- Q A Q.
-// Everything commutes and is symmetric, so that the order of factors does not matter.
+// Everything commutes and is symmetric, so that the order of factors does not matter.  A single tile stays in one wavefront's
+// registers; more go through LDS, three rounds per step.
 template <int NT>
 struct OrthoChain {
-    static constexpr int N = NT * 16, LD = N + 2;  // (rows an even number of banks apart would share them)
-    double A[N * LD], Q[N * LD], P[N * LD];
+    typedef OrthoTiles<NT> Tiles;
+    double A[Tiles::LEN], Q[Tiles::LEN], P[Tiles::LEN];
     double trace;
 
     __device__ __forceinline__ void run(int n, int steps, OrthoCoeffs c) {
-        const int tid = threadIdx.x;
-        const OrthoTiles<NT, LD> tiles;
+        const Tiles tiles;
         __syncthreads();
-        if (tid < 64) {
-            double t = 0.0;
-            for (int i = tid; i < n; i += 64) t += A[i * LD + i];
-#pragma unroll
-            for (int off = 32; off > 0; off >>= 1) t += __shfl_xor(t, off, 64);
-            if (tid == 0) trace = t;
+        if (threadIdx.x < 64) {
+            double t = (int)threadIdx.x < n ? A[Tiles::at(threadIdx.x, threadIdx.x)] : 0.0;
+            t = sum_across_32(sum_across_16(dpp_add<0x140>(sum_of_eight(t))));
+            if (threadIdx.x == 0) trace = t;
         }
         __syncthreads();
-        const double t = trace, inv = t == 0.0 ? 0.0 : 1.0 / t, root = ortho_root(t);
-        for (int q = tid; q < N * N; q += kOrthoThreads) {
-            const int i = q / N, j = q % N;
-            A[i * LD + j] = A[i * LD + j] * inv;
-            P[i * LD + j] = i == j && i < n ? root : 0.0;
-        }
-        __syncthreads();
-        for (int s = 0; s < steps; ++s) {
-            f64x4 x = tiles.product(A, A);
-            if (tiles.mine)
+        const double t = trace, inv = t == 0.0 ? 0.0 : 1.0 / t;
+        f64x4 a = tiles.load(A), p = tiles.diagonal(ortho_root(t), n);
+        const f64x4 one = tiles.diagonal(c.a, NT * 16);
 #pragma unroll
-                for (int v = 0; v < 4; ++v) {
-                    const int i = tiles.row + 4 * v, j = tiles.col;
-                    Q[i * LD + j] = (i == j ? c.a : 0.0) + c.b * A[i * LD + j] + c.c * x[v];
+        for (int v = 0; v < 4; ++v) a[v] = a[v] * inv;
+        if constexpr (NT == 1) {
+            if (tiles.wave == 0)
+                for (int s = 0; s < steps; ++s) {
+                    f64x4 q = Tiles::product(a, a);
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) q[v] = one[v] + c.b * a[v] + c.c * q[v];
+                    p = Tiles::product(q, p);
+                    a = Tiles::product(Tiles::product(q, a), q);
                 }
+            tiles.store(P, p);
+        } else {
+            tiles.store(A, a);
+            tiles.store(P, p);
             __syncthreads();
-            x = tiles.product(Q, P);
-            const f64x4 y = tiles.product(Q, A);
-            __syncthreads();
-            tiles.store(P, x);
-            tiles.store(A, y);
-            __syncthreads();
-            if (s + 1 < steps) {  // (the last step's A is for nobody)
-                x = tiles.product(A, Q);
+            for (int s = 0; s < steps; ++s) {
+                f64x4 q = tiles.product(A, A);
+#pragma unroll
+                for (int v = 0; v < 4; ++v) q[v] = one[v] + c.b * a[v] + c.c * q[v];
+                tiles.store(Q, q);
                 __syncthreads();
-                tiles.store(A, x);
+                if (s == 0) {  // (P is a multiple of I)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) p[v] = q[v] * ortho_root(t);
+                } else {
+                    p = tiles.product(Q, P);
+                }
+                const bool more = s + 1 < steps;  // (the last step's A is for nobody)
+                if (more) a = tiles.product(Q, A);
+                __syncthreads();
+                tiles.store(P, p);
+                if (more) {
+                    tiles.store(A, a);
+                    __syncthreads();
+                    a = tiles.product(A, Q);
+                    __syncthreads();
+                    tiles.store(A, a);
+                }
                 __syncthreads();
             }
         }
+        __syncthreads();
     }
 };
 
@@ -147,11 +197,12 @@ struct OrthoChain {
 template <int NT, typename T, typename F>
 __device__ __forceinline__ void ortho_gram(const OrthoIo<T> &io, int64_t b, int64_t j0, int64_t j1, double *lds, F &&to) {
     constexpr int TILES = NT * (NT + 1) / 2, WAVES = kOrthoThreads / 64, UN = 4;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, k = lane >> 4;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, k = lane >> 4;
     f64x4 acc[TILES];
 #pragma unroll
     for (int t = 0; t < TILES; ++t) acc[t] = f64x4{0.0, 0.0, 0.0, 0.0};
-    for (int64_t j = j0 + wave * 4 + k; __any(j < j1); j += 4 * WAVES * UN) {
+    for (int64_t jw = j0 + wave * 4; jw < j1; jw += 4 * WAVES * UN) {  // (the same for all lanes)
+        const int64_t j = jw + k;
         T raw[UN][NT];
 #pragma unroll
         for (int u = 0; u < UN; ++u)  // (clamped, not branched: all loads on their way together)
@@ -198,26 +249,39 @@ __device__ __forceinline__ void ortho_gram(const OrthoIo<T> &io, int64_t b, int6
         }
 }
 
-// O = P X for columns j0 .. j1 - 1, in double (P's large entries cancel): a thread takes a column and ROWS rows.
+// O = P X for columns j0 .. j1 - 1, in double (P's large entries cancel): a wavefront takes sixteen columns at a time.
 template <int NT, typename T>
-__device__ __forceinline__ void ortho_apply(const OrthoIo<T> &io, int64_t b, int64_t j0, int64_t j1, const double *P, int ld) {
-    constexpr int ROWS = NT == 1 ? 2 : 8;
-    const int n = io.short_side, parts = (n + ROWS - 1) / ROWS;
-    for (int64_t q = threadIdx.x; q < (j1 - j0) * parts; q += kOrthoThreads) {
-        // neighbouring threads take what lies side by side in memory
-        const int64_t j = io.o_j < io.o_i ? j0 + q % (j1 - j0) : j0 + q / parts;
-        const int i0 = (int)(io.o_j < io.o_i ? q / (j1 - j0) : q % parts) * ROWS;
-        double acc[ROWS];
+__device__ __forceinline__ void ortho_apply(const OrthoIo<T> &io, int64_t b, int64_t j0, int64_t j1, const double *P) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, k = lane >> 4;
+    for (int64_t jw = j0 + wave * 16; jw < j1; jw += 16 * (kOrthoThreads / 64)) {
+        const int64_t j = jw + r;
+        T raw[NT][4];
 #pragma unroll
-        for (int u = 0; u < ROWS; ++u) acc[u] = 0.0;
-        for (int k = 0; k < n; ++k) {
-            const double x = io.at(b, k, j);
+        for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int u = 0; u < ROWS; ++u) acc[u] = __builtin_fma(P[(i0 + u) * ld + k], x, acc[u]);
+            for (int v = 0; v < 4; ++v) {
+                const int i = t * 16 + 4 * v + k;
+                raw[t][v] = io.M[b * io.m_matrix + (i < io.short_side ? i : 0) * io.m_i + (j < j1 ? j : j0) * io.m_j];
+            }
+#pragma unroll
+        for (int ti = 0; ti < NT; ++ti) {
+            f64x4 even = {0.0, 0.0, 0.0, 0.0}, odd = {0.0, 0.0, 0.0, 0.0};
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int v = 0; v < 4; v += 2) {
+                    const double *p = P + (t * NT + ti) * 256 + v * 64 + lane;
+                    const bool here = t * 16 + 4 * v + k < io.short_side, next = t * 16 + 4 * v + 4 + k < io.short_side;
+                    even = __builtin_amdgcn_mfma_f64_16x16x4f64(p[0], here ? (double)(float)raw[t][v] : 0.0, even, 0, 0, 0);
+                    odd = __builtin_amdgcn_mfma_f64_16x16x4f64(p[64], next ? (double)(float)raw[t][v + 1] : 0.0, odd, 0, 0, 0);
+                }
+            const f64x4 sum = even + odd;
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                const int i = ti * 16 + 4 * v + k;
+                if (i < io.short_side && j < j1) io.put(b, i, j, (float)sum[v]);
+            }
         }
-#pragma unroll
-        for (int u = 0; u < ROWS; ++u)
-            if (i0 + u < n) io.put(b, i0 + u, j, (float)acc[u]);
     }
 }
 
@@ -229,11 +293,11 @@ __global__ __launch_bounds__(kOrthoThreads) void ortho_narrow(OrthoIo<T> io, int
     __shared__ double lds[kOrthoThreads * 4];
     const int64_t b = blockIdx.x;
     ortho_gram<NT>(io, b, 0, io.long_side, lds, [&](int i, int j, double v) {
-        s.A[i * s.LD + j] = v;
-        s.A[j * s.LD + i] = v;
+        s.A[OrthoTiles<NT>::at(i, j)] = v;
+        s.A[OrthoTiles<NT>::at(j, i)] = v;
     });
     s.run(io.short_side, steps, c);
-    ortho_apply<NT>(io, b, 0, io.long_side, s.P, s.LD);
+    ortho_apply<NT>(io, b, 0, io.long_side, s.P);
 }
 
 // Long matrices: chunks of columns for the Gram matrix, then the recurrence, then chunks of columns for the product.
@@ -241,40 +305,39 @@ template <int NT, typename T>
 __global__ __launch_bounds__(kOrthoThreads) void ortho_narrow_gram(OrthoIo<T> io, int chunks, int64_t per, double *__restrict__ parts)
 {
     __shared__ double lds[kOrthoThreads * 4];
-    constexpr int N = NT * 16;
     const int64_t b = blockIdx.x / chunks, c = blockIdx.x % chunks;
     const int64_t j1 = (c + 1) * per < io.long_side ? (c + 1) * per : io.long_side;
-    double *to = parts + (int64_t)blockIdx.x * N * N;
-    ortho_gram<NT>(io, b, c * per, j1, lds, [&](int i, int j, double v) { to[i * N + j] = v; });
+    double *to = parts + (int64_t)blockIdx.x * OrthoTiles<NT>::LEN;
+    ortho_gram<NT>(io, b, c * per, j1, lds, [&](int i, int j, double v) { to[OrthoTiles<NT>::at(i, j)] = v; });
 }
 template <int NT>
 __global__ __launch_bounds__(kOrthoThreads) void ortho_narrow_chain(int n, int chunks, const double *__restrict__ parts, int steps,
                                                                     OrthoCoeffs c, double *__restrict__ out)
 {
     __shared__ OrthoChain<NT> s;
-    constexpr int N = NT * 16;
-    const double *from = parts + (int64_t)blockIdx.x * chunks * N * N;
-    for (int q = threadIdx.x; q < N * N; q += kOrthoThreads) {
-        const int i = q / N, j = q % N;
-        if (i / 16 > j / 16) continue;
+    typedef OrthoTiles<NT> Tiles;
+    const double *from = parts + (int64_t)blockIdx.x * chunks * Tiles::LEN;
+    for (int q = threadIdx.x; q < Tiles::LEN; q += kOrthoThreads) {
+        const int ti = q / 256 / NT, tj = q / 256 % NT;
+        if (ti > tj) continue;
         double sum = 0.0;
 #pragma unroll 8
-        for (int p = 0; p < chunks; ++p) sum += from[(int64_t)p * N * N + q];
-        s.A[i * s.LD + j] = sum;
-        if (i / 16 < j / 16) s.A[j * s.LD + i] = sum;
+        for (int p = 0; p < chunks; ++p) sum += from[(int64_t)p * Tiles::LEN + q];
+        s.A[q] = sum;
+        const int i = ti * 16 + (q % 256 / 64) * 4 + q % 64 / 16, j = tj * 16 + q % 16;
+        if (ti < tj) s.A[Tiles::at(j, i)] = sum;
     }
     s.run(n, steps, c);
-    for (int q = threadIdx.x; q < N * N; q += kOrthoThreads) out[(int64_t)blockIdx.x * N * N + q] = s.P[(q / N) * s.LD + q % N];
+    for (int q = threadIdx.x; q < Tiles::LEN; q += kOrthoThreads) out[(int64_t)blockIdx.x * Tiles::LEN + q] = s.P[q];
 }
 template <int NT, typename T>
 __global__ __launch_bounds__(kOrthoThreads) void ortho_narrow_apply(OrthoIo<T> io, int chunks, int64_t per, const double *__restrict__ P)
 {
-    constexpr int N = NT * 16, LD = N + 2;
-    __shared__ double p[N * LD];
+    __shared__ double p[OrthoTiles<NT>::LEN];
     const int64_t b = blockIdx.x / chunks, c = blockIdx.x % chunks;
-    for (int q = threadIdx.x; q < N * N; q += kOrthoThreads) p[(q / N) * LD + q % N] = P[b * N * N + q];
+    for (int q = threadIdx.x; q < OrthoTiles<NT>::LEN; q += kOrthoThreads) p[q] = P[b * OrthoTiles<NT>::LEN + q];
     __syncthreads();
-    ortho_apply<NT>(io, b, c * per, (c + 1) * per < io.long_side ? (c + 1) * per : io.long_side, p, LD);
+    ortho_apply<NT>(io, b, c * per, (c + 1) * per < io.long_side ? (c + 1) * per : io.long_side, p);
 }
 
 // ---- longer sides: products of pairs of fp16 --------------------------------------------------------------------------------
@@ -363,82 +426,6 @@ enum OrthoWhat { kOrthoGram, kOrthoPoly, kOrthoStep, kOrthoLast };
 // along k), then
 //   Gram: A = X X^T;  Poly: B = b A + c A A;  Step: X' = a X + B X;  Last: O = (a X + B X) to the caller's array.
 // K is a multiple of 32, the tile's sides T of 32: nothing to clip but O.
-// Memory to LDS without registers, sixteen bytes a lane, NS stages of 32 k on their way or in use.  LDS rows are dense (a wave
-// fills 1 KB in a row); sixteen-byte pieces are swapped within a row by its number, so that the lanes of a read hit different banks.
-template <int T> struct OrthoTile {
-    static constexpr int KC = 32, PLANE = T * KC, CALLS = PLANE / 8 / 64 / 4;  // elements; a wavefront's loads per plane
-    // piece c of row r of an [T][KC] plane / of a [KC][T] plane (pairs of pieces stay together for the transposing read)
-    static __device__ __forceinline__ int along(int r, int c) { return c ^ ((r >> 2) & 3); }
-    static __device__ __forceinline__ int across(int r, int c) { return T == 128 ? c ^ ((r & 7) << 1) : c ^ (((r >> 1) & 3) << 1); }
-};
-
-// Waits until at most LEFT of this wavefront's loads are on their way and its LDS reads are done, then for the workgroup.
-// (By builtins: the compiler then knows that the reads are done, and does not wait for the next ones instead.)
-template <int LEFT>
-__device__ __forceinline__ void ortho_barrier() {
-    static_assert(LEFT < 64, "six bits");
-    __builtin_amdgcn_sched_barrier(0);
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_s_waitcnt((LEFT & 15) | (LEFT >> 4) << 14 | 7 << 4);  // vmcnt LEFT, lgkmcnt 0, expcnt any
-    __builtin_amdgcn_s_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-    __builtin_amdgcn_sched_barrier(0);
-}
-
-// A wavefront's share of a stage's loads of one plane: `from` is the same for all lanes, a lane adds `at[q]` bytes for its q-th load.
-template <int T, bool ACROSS>
-struct OrthoFetch {
-    typedef OrthoTile<T> O;
-    uint32_t at[O::CALLS];
-    __device__ __forceinline__ OrthoFetch(int64_t ld, int wave, int lane) {
-        constexpr int PIECES = ACROSS ? T / 8 : O::KC / 8, ROWS = 64 / PIECES;
-#pragma unroll
-        for (int q = 0; q < O::CALLS; ++q) {
-            const int row = (q * 4 + wave) * ROWS + lane / PIECES, slot = lane % PIECES;
-            at[q] = (uint32_t)(row * (int)ld + (ACROSS ? O::across(row, slot) : O::along(row, slot)) * 8) * 2u;
-        }
-    }
-    __device__ __forceinline__ void operator()(const f16_t *from, f16_t *lds, int wave) const {
-        typedef __attribute__((address_space(3))) void *Lds;
-        typedef const __attribute__((address_space(1))) void *Mem;
-#pragma unroll
-        for (int q = 0; q < O::CALLS; ++q)
-            __builtin_amdgcn_global_load_lds((Mem)(reinterpret_cast<const char *>(from) + at[q]), (Lds)(lds + (q * 4 + wave) * 512), 16, 0, 0);
-    }
-};
-
-// A lane's operands of 32 x 32 x 16 MFMAs: `at[k / 16]` is where those of the tile's first 32 rows (columns) lie in a plane,
-// those of the i-th next are a constant further, as the planes and stages are.
-template <int T, bool ACROSS>
-struct OrthoRead {
-    typedef OrthoTile<T> O;
-    int at[2], at4[2];  // (in elements; at4: the second half of a transposing read)
-    __device__ __forceinline__ OrthoRead(int first, int lane) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            if constexpr (!ACROSS) {  // row first + lane % 32, elements 16 h + 8 (lane / 32) ..
-                const int row = first + (lane & 31);
-                at[h] = row * O::KC + O::along(row, 2 * h + (lane >> 5)) * 8;
-            } else {
-                const int row = 16 * h + (lane >> 5) * 8 + ((lane & 15) >> 2), col = first + (lane & 16) + (lane & 3) * 4;
-                at[h] = row * T + O::across(row, col >> 3) * 8 + (col & 4);
-                at4[h] = (row + 4) * T + O::across(row + 4, col >> 3) * 8 + (col & 4);
-            }
-        }
-    }
-    // (ACROSS: columns are swapped by exclusive or, and so are those 32 further, since `first` is a multiple of 64)
-    __device__ __forceinline__ f16x8 operator()(const f16_t *plane, int h, int i) const {
-        if constexpr (!ACROSS) {
-            return *reinterpret_cast<const f16x8 *>(plane + at[h] + i * 32 * O::KC);
-        } else {
-            typedef __attribute__((address_space(3))) s16x4 *Ptr;
-            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Ptr)(plane + (at[h] ^ (i * 32))));
-            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Ptr)(plane + (at4[h] ^ (i * 32))));
-            return __builtin_bit_cast(f16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-        }
-    }
-};
-
 struct OrthoProduct {
     OrthoPair L, R, E, C;  // factors, what is added, the result
     int64_t l_ld, r_ld, c_ld, l_matrix, r_matrix, c_matrix;  // (E lies as C does)
@@ -450,7 +437,7 @@ template <int T, int NS, int WHAT, typename U>
 __global__ __launch_bounds__(256, NS * T * 256 > 80 * 1024 ? 1 : 2) void ortho_product_tile(OrthoProduct p, OrthoIo<U> io)
 {
     constexpr bool ACROSS = WHAT == kOrthoStep || WHAT == kOrthoLast, SYM = !ACROSS;
-    typedef OrthoTile<T> O;
+    typedef LdsTile<T> O;
     constexpr int MB = T / 64, LD = T + 1;  // (eight rows further is eight banks further)
     constexpr int STAGE = 4 * O::PLANE, BYTES = NS * STAGE * 2, OUT = T / 2 * LD * 4, LOADS = 4 * O::CALLS;
     __shared__ __align__(16) char lds[BYTES > OUT ? BYTES : OUT];
@@ -483,8 +470,8 @@ __global__ __launch_bounds__(256, NS * T * 256 > 80 * 1024 ? 1 : 2) void ortho_p
         for (int j = 0; j < MB; ++j)
 #pragma unroll
             for (int q = 0; q < 16; ++q) acc[i][j][q] = low[i][j][q] = 0.f;
-    const OrthoFetch<T, false> fetch_l(p.l_ld, wave, lane);
-    const OrthoFetch<T, ACROSS> fetch_r(p.r_ld, wave, lane);
+    const TileFetch<f16_t, T, false> fetch_l(p.l_ld, wave, lane);
+    const TileFetch<f16_t, T, ACROSS> fetch_r(p.r_ld, wave, lane);
     const auto fetch = [&](int q, int buf) {
         f16_t *s = stage + buf * STAGE;
         const int k = q * O::KC;
@@ -495,8 +482,8 @@ __global__ __launch_bounds__(256, NS * T * 256 > 80 * 1024 ? 1 : 2) void ortho_p
         fetch_r(src[3] + off, s + 3 * O::PLANE, wave);
     };
     struct Operands { f16x8 lh[MB], ll[MB], rh[MB], rl[MB]; };
-    const OrthoRead<T, false> read_l(wm * (T / 2), lane);
-    const OrthoRead<T, ACROSS> read_r(wn * (T / 2), lane);
+    const TileRead<f16_t, T, false> read_l(wm * (T / 2), lane);
+    const TileRead<f16_t, T, ACROSS> read_r(wn * (T / 2), lane);
     const auto read = [&](Operands &o, int buf, int h) {
         const f16_t *s = stage + buf * STAGE;
 #pragma unroll
@@ -534,8 +521,8 @@ __global__ __launch_bounds__(256, NS * T * 256 > 80 * 1024 ? 1 : 2) void ortho_p
     const int stages = p.k / O::KC;
     int sent = 0;
     for (; sent < NS && sent < stages; ++sent) fetch(sent, sent);
-    if (sent == NS) ortho_barrier<(NS - 1) * LOADS>();
-    else ortho_barrier<0>();
+    if (sent == NS) stage_barrier<(NS - 1) * LOADS>();
+    else stage_barrier<0>();
     Operands first, second;
     read(first, 0, 0);
     for (int q0 = 0; q0 + 1 < stages; q0 += NS)
@@ -546,8 +533,8 @@ __global__ __launch_bounds__(256, NS * T * 256 > 80 * 1024 ? 1 : 2) void ortho_p
             read(second, buf, 1);
             multiply(first);
             interleave();
-            if (q + NS <= stages) ortho_barrier<(NS - 2) * LOADS>();
-            else ortho_barrier<0>();
+            if (q + NS <= stages) stage_barrier<(NS - 2) * LOADS>();
+            else stage_barrier<0>();
             if (sent < stages) fetch(sent++, buf);
             read(first, (buf + 1) % NS, 0);
             multiply(second);
@@ -639,6 +626,194 @@ __global__ __launch_bounds__(256, NS * T * 256 > 80 * 1024 ? 1 : 2) void ortho_p
             }
         }
     }
+}
+
+// A matrix that fits in LDS as pairs, with its Gram matrix: all steps in one workgroup.  Launches and what lies between them are
+// what the products of such matrices take else: 8 matrices of 128 x 128 in 17 launches 76 us, like this 60 us; 64 x 64 in double 64
+// us, like this 20.  A wavefront
+// computes 32 x 32 blocks, PER of them with the same left rows, holds them while others still read what they replace, and writes
+// them in pairs.  (All blocks of A and A^2: those below the diagonal would be written two bytes at a time, and eight wavefronts
+// have two blocks each either way.)  X and A have rows of lp and sp elements and eight more, so that the sixteen lanes of a read
+// hit different banks.
+constexpr int kOrthoSmallThreads = 512;
+
+template <typename T, int BYTES, int PER>
+__global__ __launch_bounds__(kOrthoSmallThreads) void ortho_small(OrthoIo<T> io, int sp, int lp, int steps, OrthoCoeffs c)
+{
+    constexpr int WAVES = kOrthoSmallThreads / 64, MOST = PER == 1 ? 1 : 2;  // units of PER blocks of a wavefront at most
+    __shared__ __align__(16) f16_t lds[BYTES / 2];
+    __shared__ double part[WAVES];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t b = blockIdx.x;
+    const int xs = lp + 8, as = sp + 8, s = io.short_side, l = io.long_side;
+    f16_t *const Xh = lds, *const Xl = Xh + sp * xs, *const Ah = Xl + sp * xs, *const Al = Ah + sp * as;
+
+    // The caller's rows, whatever side they are: a wavefront takes every eighth, and eight of its rows at a time.
+    constexpr int UN = 8;
+    const bool turn = io.m_i < io.m_j;  // the rows of M are the long side
+    const int inner = turn ? s : l, outer = turn ? l : s, inner_p = turn ? sp : lp, outer_p = turn ? lp : sp;
+    const T *from = io.M + b * io.m_matrix;
+    const int64_t m_row = turn ? io.m_j : io.m_i;
+    const auto each = [&](int rows, int cols, auto &&use) {  // use(row, column, element), rows beyond the matrix: zero
+        for (int o = wave; o < rows; o += WAVES * UN)
+            for (int q = lane; q < cols; q += 64) {
+                T raw[UN];
+#pragma unroll
+                for (int u = 0; u < UN; ++u) {
+                    const int row = o + u * WAVES;
+                    raw[u] = from[(row < outer ? row : 0) * m_row + (q < inner ? q : 0)];
+                }
+#pragma unroll
+                for (int u = 0; u < UN; ++u) {
+                    const int row = o + u * WAVES;
+                    if (row < rows) use(row, q, row < outer && q < inner ? (double)(float)raw[u] : 0.0);
+                }
+            }
+    };
+    double sum = 0.0;
+    each(outer, inner, [&](int, int, double x) { sum = __builtin_fma(x, x, sum); });
+    sum = sum_across_32(sum_across_16(dpp_add<0x140>(sum_of_eight(sum))));
+    if (lane == 0) part[wave] = sum;
+    __syncthreads();
+    sum = 0.0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) sum += part[w];
+    const double norm = ortho_root(sum) * (double)kOrthoScaleX;
+    each(outer_p, inner_p, [&](int o, int q, double x) {
+        f16_t hi, lo;
+        ortho_split((float)(x * norm), hi, lo);
+        const int at = turn ? q * xs + o : o * xs + q;
+        Xh[at] = hi;
+        Xl[at] = lo;
+    });
+    __syncthreads();
+
+    // Blocks (i0, j0), (i0, j0 + 32), .. of a product, turned: a lane's sixteen entries of each are in row lane % 32, at columns
+    // 8 (q / 4) + 4 (lane / 32) + q % 4.  left: rows along k; right: rows along k (its transpose is the factor), or across.
+    const int row = lane & 31, quad = 4 * (lane >> 5);
+    typedef __attribute__((ext_vector_type(4))) f16_t f16x4;
+    struct Blocks { f32x16 v[PER]; };
+    const auto along = [&](const f16_t *m, int stride, int first, int k) {
+        return *reinterpret_cast<const f16x8 *>(m + (first + row) * stride + k + 8 * (lane >> 5));
+    };
+    const auto across = [&](const f16_t *m, int stride, int first, int k) {  // rows k .., columns first ..
+        typedef __attribute__((address_space(3))) s16x4 *Ptr;
+        const f16_t *p = m + (k + (lane >> 5) * 8 + ((lane & 15) >> 2)) * stride + first + (lane & 16) + (lane & 3) * 4;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Ptr)p), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Ptr)(p + 4 * stride));
+        return __builtin_bit_cast(f16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    const auto product = [&](const f16_t *lh_, const f16_t *ll_, int ls, int i0, auto &&right, const f16_t *rh_, const f16_t *rl_, int rs,
+                             int j0, int length) {
+        Blocks out;
+        f32x16 low[PER];
+#pragma unroll
+        for (int u = 0; u < PER; ++u)
+#pragma unroll
+            for (int q = 0; q < 16; ++q) out.v[u][q] = low[u][q] = 0.f;
+        struct Operands { f16x8 lh, ll, rh[PER], rl[PER]; };
+        const auto read = [&](Operands &o, int k) {
+            o.lh = along(lh_, ls, i0, k);
+            o.ll = along(ll_, ls, i0, k);
+#pragma unroll
+            for (int u = 0; u < PER; ++u) {
+                o.rl[u] = right(rl_, rs, j0 + 32 * u, k);
+                o.rh[u] = right(rh_, rs, j0 + 32 * u, k);
+            }
+        };
+        const auto multiply = [&](const Operands &o) {
+#pragma unroll
+            for (int u = 0; u < PER; ++u) low[u] = mfma32(o.rl[u], o.lh, low[u]);
+#pragma unroll
+            for (int u = 0; u < PER; ++u) out.v[u] = mfma32(o.rh[u], o.lh, out.v[u]);
+#pragma unroll
+            for (int u = 0; u < PER; ++u) low[u] = mfma32(o.rh[u], o.ll, low[u]);
+        };
+#pragma unroll 2
+        for (int k = 0; k < length; k += 16) {
+            Operands o;
+            read(o, k);
+            multiply(o);
+        }
+#pragma unroll
+        for (int u = 0; u < PER; ++u) out.v[u] += low[u];
+        return out;
+    };
+    const auto put = [&](f16_t *mh, f16_t *ml, int stride, int i0, int j0, const Blocks &x) {
+#pragma unroll
+        for (int u = 0; u < PER; ++u)
+#pragma unroll
+            for (int q = 0; q < 16; q += 4) {
+                f16x4 hi, lo;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    f16_t y, z;
+                    ortho_split(x.v[u][q + e], y, z);
+                    hi[e] = y;
+                    lo[e] = z;
+                }
+                const int at = (i0 + row) * stride + j0 + 32 * u + 2 * q + quad;
+                *reinterpret_cast<f16x4 *>(mh + at) = hi;
+                *reinterpret_cast<f16x4 *>(ml + at) = lo;
+            }
+    };
+    const auto plus = [&](const f16_t *mh, const f16_t *ml, int stride, int i0, int j0, float alpha, float beta, Blocks &x) {
+#pragma unroll
+        for (int u = 0; u < PER; ++u)
+#pragma unroll
+            for (int q = 0; q < 16; q += 4) {
+                const int at = (i0 + row) * stride + j0 + 32 * u + 2 * q + quad;
+                const f16x4 hi = *reinterpret_cast<const f16x4 *>(mh + at), lo = *reinterpret_cast<const f16x4 *>(ml + at);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x.v[u][q + e] = fmaf(alpha, (float)hi[e] + (float)lo[e], beta * x.v[u][q + e]);
+            }
+    };
+    const int nb = sp / 32, units = nb * (lp / 32 / PER);
+    const bool sym = wave < nb * nb / PER;  // this wavefront's blocks of A and A^2
+    const int si = wave % nb * 32, sj = wave / nb * 32 * PER;
+    for (int step = 0; step < steps; ++step) {
+        Blocks y;
+        if (sym) {
+            y = product(Xh, Xl, xs, si, along, Xh, Xl, xs, sj, lp);
+#pragma unroll
+            for (int u = 0; u < PER; ++u)
+#pragma unroll
+                for (int q = 0; q < 16; ++q) y.v[u][q] *= kOrthoScaleA / (kOrthoScaleX * kOrthoScaleX);
+            put(Ah, Al, as, si, sj, y);
+        }
+        __syncthreads();
+        if (sym) {
+            y = product(Ah, Al, as, si, along, Ah, Al, as, sj, sp);
+            plus(Ah, Al, as, si, sj, (float)c.b, (float)(c.c / kOrthoScaleA), y);
+        }
+        __syncthreads();
+        if (sym) put(Ah, Al, as, si, sj, y);
+        __syncthreads();
+        Blocks x[MOST];
+#pragma unroll
+        for (int u = 0; u < MOST; ++u) {
+            const int t = wave + u * WAVES, i0 = t % nb * 32, j0 = t / nb * 32 * PER;
+            if (t < units) {
+                x[u] = product(Ah, Al, as, i0, across, Xh, Xl, xs, j0, sp);
+                plus(Xh, Xl, xs, i0, j0, (float)c.a, 1.f / kOrthoScaleA, x[u]);
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < MOST; ++u) {
+            const int t = wave + u * WAVES, i0 = t % nb * 32, j0 = t / nb * 32 * PER;
+            if (t < units) put(Xh, Xl, xs, i0, j0, x[u]);
+        }
+        __syncthreads();
+    }
+    const int64_t o_row = turn ? io.o_j : io.o_i;
+    for (int o = wave; o < outer; o += WAVES)
+        for (int q = lane; q < inner; q += 64) {
+            const int at = turn ? q * xs + o : o * xs + q;
+            const float v = ((float)Xh[at] + (float)Xl[at]) * (1.f / kOrthoScaleX);
+            const int64_t p = b * io.o_matrix + o * o_row + q;
+            if (io.sub) io.sub[p] = io.sub[p] - io.rate * v;
+            else io.O[p] = (T)v;
+        }
 }
 
 // No step at all: O = X_0.
