@@ -14,12 +14,18 @@ template <typename T, int N>
 struct AnyVec {
     typedef T type __attribute__((ext_vector_type(N), aligned(sizeof(T))));
 };
-template <typename T, int N>
+template <typename T, int N, bool ONCE = false>  // ONCE: not to be kept in the caches
 __device__ __forceinline__ void load_any(const T *p, T (&v)[N]) {
     if constexpr (N == 1) {
         v[0] = *p;
     } else {
-        const typename AnyVec<T, N>::type x = *reinterpret_cast<const typename AnyVec<T, N>::type *>(p);
+        typename AnyVec<T, N>::type x;
+        if constexpr (ONCE && N * sizeof(T) == 16) {
+            typedef uint32_t words __attribute__((ext_vector_type(4), aligned(2)));
+            x = __builtin_bit_cast(typename AnyVec<T, N>::type, __builtin_nontemporal_load(reinterpret_cast<const words *>(p)));
+        } else {
+            x = *reinterpret_cast<const typename AnyVec<T, N>::type *>(p);
+        }
 #pragma unroll
         for (int j = 0; j < N; ++j) v[j] = x[j];
     }

@@ -80,8 +80,17 @@ int check_tokens(cdgrab_handle *h, const char *who, const cdgrab_token_rows *t) 
     return CDGRAB_OK;
 }
 
-// f(threads per row, groups of VEC per thread): the fewest threads that hold the row in few groups.
-template <int VEC, typename F>
+// Rows that the caches do not hold anyway are read past them, if their pieces are whole (a line that two rows share would be read
+// twice).  65 536 rows of 768 fp32: forward 79 -> 66 us, backward 127 -> 106; in bf16 47 and 79 -> 77; 51 400 rows of 515 fp16,
+// which are not, forward 35 -> 43.
+bool norm_once(int64_t rows, int64_t width, int64_t size, const void *p, int64_t stride) {
+    return rows * width * size >= ((int64_t)64 << 20) && reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride * size % 16 == 0;
+}
+
+// f(threads per row, groups of VEC per thread): the fewest threads that hold the row in few groups.  The backward pass, which has
+// two reductions and twice the arithmetic per row, takes narrower ones where its rows then fill them: two rows of 768 bf16 a
+// wavefront instead of one 74 -> 68 us (65 536 rows), the forward pass 45 -> 59.
+template <int VEC, bool BACKWARD, typename F>
 void by_norm_shape(int64_t width, F &&f) {
     const int64_t groups = (width + VEC - 1) / VEC;
     const auto go = [&](auto lanes, auto k) { f(lanes, k); };
@@ -89,10 +98,12 @@ void by_norm_shape(int64_t width, F &&f) {
     if constexpr (VEC == 1) {
         NORM_SHAPE(8, 1);
     } else {
+        constexpr int HALF = BACKWARD ? 2 : 1;
         if (groups <= 8) NORM_SHAPE(8, 1);
         else if (groups <= 16) NORM_SHAPE(16, 1);
-        else if (groups <= 32) NORM_SHAPE(32, 1);
-        else if (groups <= 64) NORM_SHAPE(64, 1);
+        else if (groups <= 32) NORM_SHAPE(32 / HALF, HALF);
+        else if (groups <= 64) NORM_SHAPE(64 / HALF, HALF);
+        else if (groups <= 96 && BACKWARD) NORM_SHAPE(32, 3);
         else if (groups <= 128) NORM_SHAPE(64, 2);
         else if (groups <= 192) NORM_SHAPE(64, 3);
         else if (groups <= 256) NORM_SHAPE(64, 4);
@@ -392,15 +403,22 @@ extern "C" int cdgrab_layernorm(cdgrab_handle *h, int64_t rows, int64_t width, i
         return fail(h, CDGRAB_EINVAL, "%s: X and Y must not overlap", who);
     const OnDevice on(h->device);
     HIP_TRY(h, on.err);
+    const bool once = norm_once(rows, width, size, X, x_stride);
     by_norm_type(type, width, [&](auto elem, auto vec) {
         typedef decltype(elem) T;
         constexpr int VEC = decltype(vec)::value;
-        by_norm_shape<VEC>(width, [&](auto lanes, auto k) {
+        by_norm_shape<VEC, false>(width, [&](auto lanes, auto k) {
             constexpr int LANES = decltype(lanes)::value, K = decltype(k)::value;
             constexpr int THREADS = LANES > kNormThreads ? LANES : kNormThreads, PER = THREADS / LANES;
             const int64_t groups = std::min<int64_t>((rows + PER - 1) / PER, (int64_t)h->num_cu * (2048 / THREADS));
-            hipLaunchKernelGGL((norm_forward<T, VEC, LANES, K>), dim3((unsigned)groups), dim3(THREADS), 0, h->stream,
-                               (const T *)X, x_stride, gain, bias, (T *)Y, y_stride, rows, (int)width, eps);
+            const auto launch = [&](auto kernel) {
+                hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(THREADS), 0, h->stream, (const T *)X, x_stride, gain, bias, (T *)Y,
+                                   y_stride, rows, (int)width, eps);
+            };
+            if constexpr (VEC > 1) {
+                if (once) return launch(norm_forward<T, VEC, LANES, K, true>);
+            }
+            launch(norm_forward<T, VEC, LANES, K, false>);
         });
     });
     HIP_TRY(h, hipGetLastError());
@@ -435,10 +453,11 @@ extern "C" int cdgrab_pergrad_layernorm(cdgrab_handle *h, const cdgrab_token_row
     HIP_TRY(h, on.err);
     const TokenRows tok{t->examples, t->rows, t->tokens, t->first, t->count, 0};
     rc = CDGRAB_OK;
+    const bool once = norm_once(t->rows, width, size, X, x_stride) && norm_once(t->rows, width, size, DY, dy_stride);
     by_norm_type(type, width, [&](auto elem, auto vec) {
         typedef decltype(elem) T;
         constexpr int VEC = decltype(vec)::value;
-        by_norm_shape<VEC>(width, [&](auto lanes, auto k) {
+        by_norm_shape<VEC, true>(width, [&](auto lanes, auto k) {
             constexpr int LANES = decltype(lanes)::value, K = decltype(k)::value;
             constexpr int THREADS = LANES > kNormThreads ? LANES : kNormThreads, PER = THREADS / LANES;
             // an example's rows in chunks until the chip is full, of eight rows per group of threads at least
@@ -452,9 +471,18 @@ extern "C" int cdgrab_pergrad_layernorm(cdgrab_handle *h, const cdgrab_token_row
                 TokenRows part = tok;
                 part.examples = std::min(per, tok.examples - e0);
                 part.base = e0;
-                hipLaunchKernelGGL((norm_backward<T, VEC, LANES, K>), dim3((unsigned)(part.examples * chunks)), dim3(THREADS), 0,
-                                   h->stream, part, (int)chunks, (const T *)X, x_stride, (const T *)DY, dy_stride, gain, (T *)DX,
-                                   dx_stride, G, g_stride, (int)with_bias, partial, (int)width, eps);
+                const auto launch = [&](auto kernel) {
+                    hipLaunchKernelGGL(kernel, dim3((unsigned)(part.examples * chunks)), dim3(THREADS), 0, h->stream, part, (int)chunks,
+                                       (const T *)X, x_stride, (const T *)DY, dy_stride, gain, (T *)DX, dx_stride, G, g_stride,
+                                       (int)with_bias, partial, (int)width, eps);
+                };
+                if constexpr (VEC > 1) {
+                    if (once) {
+                        launch(norm_backward<T, VEC, LANES, K, true>);
+                        continue;
+                    }
+                }
+                launch(norm_backward<T, VEC, LANES, K, false>);
             }
             if (partial) {
                 const int64_t groups = (cols + 31) / 32;
@@ -516,7 +544,10 @@ extern "C" int cdgrab_pergrad_linear(cdgrab_handle *h, const cdgrab_token_rows *
             return run_linear<T, 128, 32, 4, 1>(h, tok, x, x_stride, dl, d_stride, in_dim, out_dim, with_bias, G, g_stride);
         if (in_dim <= 32)
             return run_linear<T, 32, 128, 1, 4>(h, tok, x, x_stride, dl, d_stride, in_dim, out_dim, with_bias, G, g_stride);
-        if (in_dim <= 64 || out_dim <= 64 || tiles(128, 128) < h->num_cu)
+        // Small tiles where large ones, even in shares of the tokens, would not fill the chip, and where small ones fill it without
+        // shares (64 examples of 1024 tokens, 128 -> 384: 26 us against 33; one of 65 536, 768 -> 2304: large ones in shares 414, small 800).
+        const bool few = tiles(128, 128) * std::max<int64_t>(1, tok.tokens / 256) < 2 * h->num_cu;
+        if (in_dim <= 64 || out_dim <= 64 || few || (tiles(128, 128) < h->num_cu && tiles(64, 64) >= 2 * h->num_cu))
             return run_linear<T, 64, 64, 2, 2>(h, tok, x, x_stride, dl, d_stride, in_dim, out_dim, with_bias, G, g_stride);
         return run_linear<T, 128, 128, 2, 2>(h, tok, x, x_stride, dl, d_stride, in_dim, out_dim, with_bias, G, g_stride);
     };

@@ -112,8 +112,9 @@ __global__ __launch_bounds__(kLinearThreads) void linear_grad(TokenRows tok, int
     typedef LinearStage<T, BN> SD;
     static_assert(WAVES_M * WAVES_N * 64 == kLinearThreads, "");
     constexpr int MB = BM / WAVES_M / 32, NB = BN / WAVES_N / 32, STAGE = P::N * (SX::PLANE + SD::PLANE);
-    __shared__ E lds[2][STAGE];
-    __shared__ float bias_part[SD::GROUPS * 8 <= kLinearThreads ? kLinearThreads * 8 : 1];
+    static_assert(2 * STAGE * sizeof(E) >= kLinearThreads * 8 * sizeof(float), "the bias's sums take the stages' place");
+    __shared__ __align__(16) E lds[2][STAGE];
+    float *bias_part = reinterpret_cast<float *>(lds);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / WAVES_N, wn = wave % WAVES_N;
     const int mt = (in_dim + BM - 1) / BM, nt = (out_dim + BN - 1) / BN;
     const uint32_t b = xcd_neighbours(blockIdx.x, gridDim.x), tiles = (uint32_t)(mt * nt), rest = b / tiles, tile = b - rest * tiles;
@@ -199,6 +200,7 @@ __global__ __launch_bounds__(kLinearThreads) void linear_grad(TokenRows tok, int
     if (sums) {  // uniform: column sums of the delta tile, over the threads that staged the same columns
         constexpr int ROWS = kLinearThreads / SD::GROUPS;
         float mine[8];
+        __syncthreads();  // (the last stage has been read)
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             mine[j] = 0.f;

@@ -63,9 +63,10 @@ struct NormSlice {
 template <typename T, int VEC, int K>
 struct NormRow {
     T v[K][VEC];
+    template <bool ONCE>
     __device__ __forceinline__ void load(const T *row, const int (&pos)[K]) {
 #pragma unroll
-        for (int k = 0; k < K; ++k) load_any<T, VEC>(row + pos[k], v[k]);
+        for (int k = 0; k < K; ++k) load_any<T, VEC, ONCE>(row + pos[k], v[k]);
     }
 };
 
@@ -82,7 +83,7 @@ __device__ __forceinline__ float norm_mean(const NormRow<T, VEC, K> &x, const No
     return s[0] * inv_width;
 }
 
-template <typename T, int VEC, int LANES, int K>
+template <typename T, int VEC, int LANES, int K, bool ONCE>
 __global__ __launch_bounds__(LANES > kNormThreads ? LANES : kNormThreads) void norm_forward(
     const T *__restrict__ X, int64_t x_stride, const float *__restrict__ gain, const float *__restrict__ bias, T *__restrict__ Y,
     int64_t y_stride, int64_t rows, int width, float eps)
@@ -103,10 +104,10 @@ __global__ __launch_bounds__(LANES > kNormThreads ? LANES : kNormThreads) void n
     const int64_t step = (int64_t)gridDim.x * PER;
     int64_t row = (int64_t)blockIdx.x * PER + mine;
     NormRow<T, VEC, K> next;
-    next.load(X + (row < rows ? row : rows - 1) * x_stride, sl.pos);
+    next.template load<ONCE>(X + (row < rows ? row : rows - 1) * x_stride, sl.pos);
     for (int64_t base = (int64_t)blockIdx.x * PER; base < rows; base += step, row += step) {  // (uniform: rows beyond the last are not written)
         const NormRow<T, VEC, K> x = next;
-        if (base + step < rows) next.load(X + (row + step < rows ? row + step : rows - 1) * x_stride, sl.pos);
+        if (base + step < rows) next.template load<ONCE>(X + (row + step < rows ? row + step : rows - 1) * x_stride, sl.pos);
         const float mu = norm_mean<T, VEC, LANES, K>(x, sl, inv_width, lds);
         float s[2] = {0.f, 0.f};
 #pragma unroll
@@ -136,7 +137,7 @@ __global__ __launch_bounds__(LANES > kNormThreads ? LANES : kNormThreads) void n
 // Workgroup b takes chunk b % chunks of the rows of example b / chunks; a thread adds up its columns' gradients in registers,
 // the workgroup's groups of threads add theirs through LDS in order.  One chunk: to the example's row of G; else to `partial`
 // [examples][chunks][1 or 2][width], which norm_grad_finish adds up in order.  So the sums do not depend on what else runs.
-template <typename T, int VEC, int LANES, int K>
+template <typename T, int VEC, int LANES, int K, bool ONCE>
 __global__ __launch_bounds__(LANES > kNormThreads ? LANES : kNormThreads) void norm_backward(
     TokenRows tok, int chunks, const T *__restrict__ X, int64_t x_stride, const T *__restrict__ DY, int64_t dy_stride,
     const float *__restrict__ gain, T *__restrict__ DX, int64_t dx_stride, float *__restrict__ G, int64_t g_stride, int with_bias,
@@ -165,8 +166,8 @@ __global__ __launch_bounds__(LANES > kNormThreads ? LANES : kNormThreads) void n
         NormRow<T, VEC, K> next_x, next_y;
         const auto fetch = [&](int64_t at) {
             const int64_t row = span.first + (at < t1 ? at : t1 - 1);
-            next_x.load(X + row * x_stride, sl.pos);
-            next_y.load(DY + row * dy_stride, sl.pos);
+            next_x.template load<ONCE>(X + row * x_stride, sl.pos);
+            next_y.template load<ONCE>(DY + row * dy_stride, sl.pos);
         };
         fetch(t0 + mine);
         for (int64_t base = t0; base < t1; base += PER) {
