@@ -409,8 +409,8 @@ int cdgrab_pergrad_layernorm(cdgrab_handle *h, const cdgrab_token_rows *t, int64
  *   G: row e at G + e * g_stride, fp32 dev.
  * Products of bf16 and fp16 elements are exact, those of fp32 elements good to 2^-23; sums in fp32.  An infinite fp32
  * element (or one above 3.38e38) makes the sums it enters NaN.
- * Errors: EINVAL (sizes, in_dim or out_dim > 2^20, type, with_bias not 0 or 1, null, strides, overlap),
- * ENOMEM, EHIP. */
+ * Errors: EINVAL (sizes, in_dim or out_dim > 2^20, more than 2^32 elements per row, type, with_bias not 0 or 1,
+ * null, strides, overlap), ENOMEM, EHIP. */
 int cdgrab_pergrad_linear(cdgrab_handle *h, const cdgrab_token_rows *t, int64_t in_dim, int64_t out_dim,
                           int32_t type, const void *X, int64_t x_stride, const void *D, int64_t d_stride,
                           int32_t with_bias, float *G, int64_t g_stride);
@@ -424,8 +424,8 @@ int cdgrab_pergrad_linear(cdgrab_handle *h, const cdgrab_token_rows *t, int64_t 
  * Products with the error of fp32 ones whatever the type, or better; the result is rounded once.  A matrix of zeros stays
  * zero, one with an element that is not finite becomes NaN.  Coefficients under which a singular value could pass 3.5
  * within the steps are refused.  Like the calls above it may be captured once it has run with the same sizes.
- * Errors: EINVAL (sizes, a shorter side > 16384, a side > 2^20, type, steps < 0 or > 64, coefficients, null,
- * strides, overlap), ENOMEM, EHIP. */
+ * Errors: EINVAL (sizes, a shorter side > 16384, a side > 2^20, more than 2^32 elements, a batch > 2^21, type, steps < 0
+ * or > 64, coefficients, null, strides, overlap), ENOMEM, EHIP. */
 int cdgrab_orthogonalize(cdgrab_handle *h, int64_t batch, int64_t rows, int64_t cols, int32_t type,
                          const void *M, int64_t m_stride, int64_t m_matrix, int32_t steps,
                          const double *coeffs /*host*/, void *O, int64_t o_stride, int64_t o_matrix);

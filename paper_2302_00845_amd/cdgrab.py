@@ -480,8 +480,10 @@ def cdgrab_pergrad_layernorm(h: Handle, X: torch.Tensor, dY: torch.Tensor, gain:
     pd, sd = None, width
     if dX is not None or want_dx:
         if dX is None:
-            whole = first is None and count is None
-            dX = (torch.empty_like if whole else torch.zeros_like)(X, memory_format=torch.contiguous_format)
+            dX = torch.empty_like(X, memory_format=torch.contiguous_format)
+            if first is not None or count is not None:
+                with torch.cuda.stream(h.stream):  # before the call's kernels, wherever they run
+                    dX.zero_()
         pd, _, wd, sd = _rows(dX, "dX", h.device, X)
         if wd != width:
             raise ValueError("dX must have shape %s, got %s" % (tuple(X.shape), tuple(dX.shape)))

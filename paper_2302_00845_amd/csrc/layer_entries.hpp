@@ -7,7 +7,8 @@ constexpr int64_t kOrthoSmallLds = 152 * 1024, kOrthoSmallLdsHalf = 76 * 1024;  
 constexpr int64_t kOrthoBytes = (int64_t)4 << 30;            // workspace of the products' form: as many matrices at a time
 constexpr int64_t kOrthoMaxShort = 16384;
 constexpr int64_t kOrthoMaxSide = (int64_t)1 << 20;
-constexpr int64_t kMaxGroups = (int64_t)1 << 22;  // workgroups per launch (a grid dimension holds fewer than 2^32 threads)
+constexpr int64_t kMaxGroups = (int64_t)1 << 21;  // workgroups per launch, of up to 1024 threads (a grid dimension holds fewer than 2^32)
+constexpr int64_t kMaxCells = (int64_t)1 << 32;   // elements of a matrix, of a gradient row: 2^22 workgroups of 256 threads at the most
 
 // Workspace of the layer operators.  What a recorded call has used is kept until the handle goes, also when a larger
 // buffer takes its place: the recording holds its address.  A recorded call allocates nothing.
@@ -257,7 +258,7 @@ int run_ortho_narrow(cdgrab_handle *h, const char *who, int64_t batch, OrthoIo<T
 template <int TILE, typename T>
 int run_ortho_products(cdgrab_handle *h, const char *who, int64_t batch, OrthoIo<T> io, int64_t steps, const OrthoCoeffs &c) {
     const int64_t sp = round_up(io.short_side, TILE), lp = round_up(io.long_side, TILE);
-    const int64_t x_len = sp * lp, a_len = sp * sp, per_matrix = 4 * x_len + 4 * a_len + kOrthoSums * 4;  // fp16 elements
+    const int64_t x_len = 2 * sp * lp, a_len = 2 * sp * sp, per_matrix = 2 * x_len + 2 * a_len + kOrthoSums * 4;  // fp16 elements
     const int64_t tm = sp / TILE, tn = lp / TILE;
     const int64_t most = std::max<int64_t>(1, std::min(kOrthoBytes / 2 / per_matrix,
                                                        kMaxGroups / std::max(tm * tn, (sp / 32) * (lp / 32))));
@@ -268,12 +269,11 @@ int run_ortho_products(cdgrab_handle *h, const char *who, int64_t batch, OrthoIo
     double *sums = reinterpret_cast<double *>(ws);
     f16_t *at = ws + at_once * kOrthoSums * 4;
     const auto take = [&](int64_t len) {
-        const OrthoPair p{at, at + at_once * len};
-        at += 2 * at_once * len;
+        f16_t *p = at;
+        at += at_once * len;
         return p;
     };
-    OrthoPair X = take(x_len), Y = take(x_len);
-    const OrthoPair A = take(a_len), B = take(a_len);
+    f16_t *X = take(x_len), *Y = take(x_len), *const A = take(a_len), *const B = take(a_len);
     const int64_t rows = io.m_i < io.m_j ? io.long_side : io.short_side, cols = io.m_i < io.m_j ? io.short_side : io.long_side;
     for (int64_t b0 = 0; b0 < batch; b0 += at_once) {
         const int64_t n = std::min(at_once, batch - b0);
@@ -410,7 +410,9 @@ extern "C" int cdgrab_layernorm(cdgrab_handle *h, int64_t rows, int64_t width, i
         by_norm_shape<VEC, false>(width, [&](auto lanes, auto k) {
             constexpr int LANES = decltype(lanes)::value, K = decltype(k)::value;
             constexpr int THREADS = LANES > kNormThreads ? LANES : kNormThreads, PER = THREADS / LANES;
-            const int64_t groups = std::min<int64_t>((rows + PER - 1) / PER, (int64_t)h->num_cu * (2048 / THREADS));
+            // (at least four rows per group of threads, which reads its columns' parameters once, if that leaves two workgroups per CU)
+            const int64_t all = (rows + PER - 1) / PER, most = (int64_t)h->num_cu * (2048 / THREADS);
+            const int64_t groups = std::min(std::min(all, most), std::max<int64_t>(2 * (int64_t)h->num_cu, all / 4));
             const auto launch = [&](auto kernel) {
                 hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(THREADS), 0, h->stream, (const T *)X, x_stride, gain, bias, (T *)Y,
                                    y_stride, rows, (int)width, eps);
@@ -509,6 +511,7 @@ extern "C" int cdgrab_pergrad_linear(cdgrab_handle *h, const cdgrab_token_rows *
         return fail(h, CDGRAB_EINVAL, "%s: bad arguments in_dim=%lld out_dim=%lld (1 .. 2^20) type=%d with_bias=%d", who,
                     (long long)in_dim, (long long)out_dim, (int)type, (int)with_bias);
     const int64_t size = elem_size(type), d = (in_dim + with_bias) * out_dim;
+    if (d > kMaxCells) return fail(h, CDGRAB_EINVAL, "%s: %lld elements per gradient row, and at most 2^32", who, (long long)d);
     if (t->examples == 0) return CDGRAB_OK;
     if (!G || (t->rows > 0 && t->tokens > 0 && (!X || !D))) return fail(h, CDGRAB_EINVAL, "%s: null pointer", who);
     if (bad_rows(X, t->rows, in_dim, x_stride, size) || bad_rows(D, t->rows, out_dim, d_stride, size) ||
@@ -563,9 +566,9 @@ extern "C" int cdgrab_orthogonalize(cdgrab_handle *h, int64_t batch, int64_t row
     if (batch < 0 || batch > kMaxGroups || rows < 1 || cols < 1 || rows > kOrthoMaxSide || cols > kOrthoMaxSide || bad_type(type))
         return fail(h, CDGRAB_EINVAL, "%s: bad arguments batch=%lld rows=%lld cols=%lld (1 .. 2^20) type=%d", who, (long long)batch,
                     (long long)rows, (long long)cols, (int)type);
-    if (std::min(rows, cols) > kOrthoMaxShort)
-        return fail(h, CDGRAB_EINVAL, "%s: the shorter side is %lld, and at most %lld", who, (long long)std::min(rows, cols),
-                    (long long)kOrthoMaxShort);
+    if (std::min(rows, cols) > kOrthoMaxShort || rows * cols > kMaxCells)
+        return fail(h, CDGRAB_EINVAL, "%s: a shorter side of %lld (at most %lld) or %lld elements (2^32)", who,
+                    (long long)std::min(rows, cols), (long long)kOrthoMaxShort, (long long)(rows * cols));
     OrthoCoeffs c{};
     const int rc = ortho_coeffs(h, who, steps, coeffs, &c);
     if (rc) return rc;

@@ -344,9 +344,6 @@ __global__ __launch_bounds__(kOrthoThreads) void ortho_narrow_apply(OrthoIo<T> i
 constexpr float kOrthoScaleX = 8192.f, kOrthoScaleA = 2048.f;  // X up to 7.9, A and b A + c A^2 up to 31 (the host sees to it)
 constexpr int kOrthoSums = 64;  // sums of squares per matrix
 
-// A matrix as pairs of fp16: hi and lo planes, `ld` elements from row to row.
-struct OrthoPair { f16_t *hi, *lo; };
-
 // Sums of squares of matrix b of `rows` x `cols` as it lies in memory; a wavefront takes every 256th row.
 template <typename T>
 __global__ __launch_bounds__(256) void ortho_squares(const T *__restrict__ M, int64_t matrix, int64_t rows, int64_t cols, int64_t stride,
@@ -380,7 +377,7 @@ __device__ __forceinline__ void ortho_split(float v, f16_t &hi, f16_t &lo) {
 // X_0 as pairs, [short][long] padded with zeros to sp x lp: 32 x 32 elements a workgroup, turned through LDS where the rows
 // of M are the long side.
 template <typename T>
-__global__ __launch_bounds__(256) void ortho_begin(OrthoIo<T> io, const double *__restrict__ sums, OrthoPair X, int sp, int lp)
+__global__ __launch_bounds__(256) void ortho_begin(OrthoIo<T> io, const double *__restrict__ sums, f16_t *__restrict__ X, int sp, int lp)
 {
     __shared__ float tile[32][33];
     __shared__ double norm;
@@ -409,14 +406,13 @@ __global__ __launch_bounds__(256) void ortho_begin(OrthoIo<T> io, const double *
         else tile[y + 8 * q][x] = n;
     }
     __syncthreads();
-    const int64_t base = b * sp * (int64_t)lp;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-        const int64_t p = base + (int64_t)(i0 + y + 8 * q) * lp + j0 + x;
+        const int64_t p = b * 2 * sp * (int64_t)lp + pair_at(i0 + y + 8 * q, j0 + x, lp);
         f16_t hi, lo;
         ortho_split(tile[y + 8 * q][x] * kOrthoScaleX, hi, lo);
-        X.hi[p] = hi;
-        X.lo[p] = lo;
+        X[p] = hi;
+        X[p + 32] = lo;
     }
 }
 
@@ -427,8 +423,9 @@ enum OrthoWhat { kOrthoGram, kOrthoPoly, kOrthoStep, kOrthoLast };
 //   Gram: A = X X^T;  Poly: B = b A + c A A;  Step: X' = a X + B X;  Last: O = (a X + B X) to the caller's array.
 // K is a multiple of 32, the tile's sides T of 32: nothing to clip but O.
 struct OrthoProduct {
-    OrthoPair L, R, E, C;  // factors, what is added, the result
-    int64_t l_ld, r_ld, c_ld, l_matrix, r_matrix, c_matrix;  // (E lies as C does)
+    const f16_t *L, *R, *E;  // factors, what is added: matrices of pairs
+    f16_t *C;                // the result
+    int64_t l_ld, r_ld, c_ld, l_matrix, r_matrix, c_matrix;  // (E lies as C does; fp16 from matrix to matrix)
     int k, tiles_m, tiles_n;
     float alpha, beta;  // result = alpha E + beta (product as multiplied)
 };
@@ -437,9 +434,9 @@ template <int T, int NS, int WHAT, typename U>
 __global__ __launch_bounds__(256, NS * T * 256 > 80 * 1024 ? 1 : 2) void ortho_product_tile(OrthoProduct p, OrthoIo<U> io)
 {
     constexpr bool ACROSS = WHAT == kOrthoStep || WHAT == kOrthoLast, SYM = !ACROSS;
-    typedef LdsTile<T> O;
+    typedef PairTile<T> O;
     constexpr int MB = T / 64, LD = T + 1;  // (eight rows further is eight banks further)
-    constexpr int STAGE = 4 * O::PLANE, BYTES = NS * STAGE * 2, OUT = T / 2 * LD * 4, LOADS = 4 * O::CALLS;
+    constexpr int STAGE = 2 * O::LEN, BYTES = NS * STAGE * 2, OUT = T / 2 * LD * 4, LOADS = 2 * O::CALLS;
     __shared__ __align__(16) char lds[BYTES > OUT ? BYTES : OUT];
     f16_t *stage = reinterpret_cast<f16_t *>(lds);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave >> 1, wn = wave & 1;
@@ -458,9 +455,8 @@ __global__ __launch_bounds__(256, NS * T * 256 > 80 * 1024 ? 1 : 2) void ortho_p
         tm = t % p.tiles_m;
         tn = t / p.tiles_m;
     }
-    const f16_t *src[4] = {p.L.hi + b * p.l_matrix + (int64_t)tm * T * p.l_ld, p.L.lo + b * p.l_matrix + (int64_t)tm * T * p.l_ld,
-                           p.R.hi + b * p.r_matrix + (ACROSS ? (int64_t)tn * T : (int64_t)tn * T * p.r_ld),
-                           p.R.lo + b * p.r_matrix + (ACROSS ? (int64_t)tn * T : (int64_t)tn * T * p.r_ld)};
+    const f16_t *const left = p.L + b * p.l_matrix + (int64_t)tm * T * 2 * p.l_ld;
+    const f16_t *const right = p.R + b * p.r_matrix + (ACROSS ? (int64_t)tn * T * 2 : (int64_t)tn * T * 2 * p.r_ld);
     // (the products with the small parts in sums of their own: as parts of one sum each would round it once more, 2468
     // columns 3.3e-6 off instead of 1.9e-6)
     f32x16 acc[MB][MB], low[MB][MB];
@@ -470,28 +466,24 @@ __global__ __launch_bounds__(256, NS * T * 256 > 80 * 1024 ? 1 : 2) void ortho_p
         for (int j = 0; j < MB; ++j)
 #pragma unroll
             for (int q = 0; q < 16; ++q) acc[i][j][q] = low[i][j][q] = 0.f;
-    const TileFetch<f16_t, T, false> fetch_l(p.l_ld, wave, lane);
-    const TileFetch<f16_t, T, ACROSS> fetch_r(p.r_ld, wave, lane);
+    const PairFetch<T, false> fetch_l(p.l_ld, wave, lane);
+    const PairFetch<T, ACROSS> fetch_r(p.r_ld, wave, lane);
     const auto fetch = [&](int q, int buf) {
         f16_t *s = stage + buf * STAGE;
-        const int k = q * O::KC;
-        const int64_t off = ACROSS ? k * p.r_ld : k;
-        fetch_l(src[0] + k, s, wave);
-        fetch_l(src[1] + k, s + O::PLANE, wave);
-        fetch_r(src[2] + off, s + 2 * O::PLANE, wave);
-        fetch_r(src[3] + off, s + 3 * O::PLANE, wave);
+        fetch_l(left + q * 64, s, wave);
+        fetch_r(right + (ACROSS ? q * O::KC * 2 * p.r_ld : q * 64), s + O::LEN, wave);
     };
     struct Operands { f16x8 lh[MB], ll[MB], rh[MB], rl[MB]; };
-    const TileRead<f16_t, T, false> read_l(wm * (T / 2), lane);
-    const TileRead<f16_t, T, ACROSS> read_r(wn * (T / 2), lane);
+    const PairRead<T, false> read_l(wm * (T / 2), lane);
+    const PairRead<T, ACROSS> read_r(wn * (T / 2), lane);
     const auto read = [&](Operands &o, int buf, int h) {
         const f16_t *s = stage + buf * STAGE;
 #pragma unroll
         for (int i = 0; i < MB; ++i) {
-            o.lh[i] = read_l(s, h, i);
-            o.rl[i] = read_r(s + 3 * O::PLANE, h, i);
-            o.rh[i] = read_r(s + 2 * O::PLANE, h, i);
-            o.ll[i] = read_l(s + O::PLANE, h, i);
+            o.lh[i] = read_l.high(s, h, i);
+            o.rl[i] = read_r.low(s + O::LEN, h, i);
+            o.rh[i] = read_r.high(s + O::LEN, h, i);
+            o.ll[i] = read_l.low(s, h, i);
         }
     };
     const auto multiply = [&](const Operands &o) {  // (products that add to the same sum apart from each other)
@@ -546,7 +538,7 @@ __global__ __launch_bounds__(256, NS * T * 256 > 80 * 1024 ? 1 : 2) void ortho_p
     // The tile goes out through LDS, half its rows at a time, so that every thread stores eight neighbours of a row; a tile
     // above the diagonal also to its mirror image.  What is added is requested before the first half is written.
     constexpr int TASKS = T / 2 * T / 8 / 256;  // of a thread, per half
-    const int64_t c_tile = b * p.c_matrix + (int64_t)tm * T * p.c_ld + tn * T;
+    const auto place = [&](int64_t row, int64_t col) { return b * p.c_matrix + pair_at(row, col, p.c_ld); };
     f16x8 e_hi[2][TASKS], e_lo[2][TASKS];
     if constexpr (WHAT != kOrthoGram)
 #pragma unroll
@@ -554,9 +546,9 @@ __global__ __launch_bounds__(256, NS * T * 256 > 80 * 1024 ? 1 : 2) void ortho_p
 #pragma unroll
             for (int u = 0; u < TASKS; ++u) {
                 const int q = threadIdx.x + u * 256;
-                const int64_t at = c_tile + (int64_t)(half * (T / 2) + q / (T / 8)) * p.c_ld + q % (T / 8) * 8;
-                e_hi[half][u] = *reinterpret_cast<const f16x8 *>(p.E.hi + at);
-                e_lo[half][u] = *reinterpret_cast<const f16x8 *>(p.E.lo + at);
+                const int64_t at = place(tm * T + half * (T / 2) + q / (T / 8), tn * T + q % (T / 8) * 8);
+                e_hi[half][u] = *reinterpret_cast<const f16x8 *>(p.E + at);
+                e_lo[half][u] = *reinterpret_cast<const f16x8 *>(p.E + at + 32);
             }
     float *out = reinterpret_cast<float *>(lds);
     const auto store = [&](const float (&v)[8], int64_t at) {
@@ -568,8 +560,8 @@ __global__ __launch_bounds__(256, NS * T * 256 > 80 * 1024 ? 1 : 2) void ortho_p
             hi[j] = x;
             lo[j] = y;
         }
-        *reinterpret_cast<f16x8 *>(p.C.hi + at) = hi;
-        *reinterpret_cast<f16x8 *>(p.C.lo + at) = lo;
+        *reinterpret_cast<f16x8 *>(p.C + at) = hi;
+        *reinterpret_cast<f16x8 *>(p.C + at + 32) = lo;
     };
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
@@ -601,7 +593,7 @@ __global__ __launch_bounds__(256, NS * T * 256 > 80 * 1024 ? 1 : 2) void ortho_p
                 }
             }
             if constexpr (WHAT != kOrthoLast) {
-                store(v, c_tile + (int64_t)(half * (T / 2) + r) * p.c_ld + c);
+                store(v, place(m0 + r, n0 + c));
             } else if (!turn && m0 + r < io.short_side) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[j] *= 1.f / kOrthoScaleX;
@@ -610,7 +602,6 @@ __global__ __launch_bounds__(256, NS * T * 256 > 80 * 1024 ? 1 : 2) void ortho_p
         }
         if (!again) continue;
         __syncthreads();
-        const int64_t mirror = b * p.c_matrix + (int64_t)n0 * p.c_ld + m0;
 #pragma unroll
         for (int u = 0; u < TASKS; ++u) {
             const int q = threadIdx.x + u * 256, c = q / (T / 16), r = q % (T / 16) * 8;
@@ -618,7 +609,7 @@ __global__ __launch_bounds__(256, NS * T * 256 > 80 * 1024 ? 1 : 2) void ortho_p
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] = out[(r + j) * LD + c];
             if constexpr (WHAT != kOrthoLast) {
-                store(v, mirror + (int64_t)c * p.c_ld + r);
+                store(v, place(n0 + c, m0 + r));
             } else if (n0 + c < io.long_side) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[j] *= 1.f / kOrthoScaleX;

@@ -259,6 +259,23 @@ def test_strided_rows_and_a_stretch_of_longer_gradient_rows(lib, dtype):
     assert (y_all[..., :5] == 9.0).all() and (y_all[..., 5 + width:] == 9.0).all()
 
 
+@pytest.mark.parametrize("tokens,n_in,n_out", [(1, 70, 10), (1, 900, 33), (2, 40, 3), (4, 5000, 7), (5, 40, 50), (40, 130, 140)])
+def test_gradient_rows_at_any_element(lib, tokens, n_in, n_out):
+    """Rows of G that start at any multiple of four bytes, one after the other or with room between them."""
+    x, d = rand(1, 5, tokens, n_in), rand(2, 5, tokens, n_out)
+    h = lib.Handle()
+    want = lib.cdgrab_pergrad_linear(h, x, d)
+    size = want.shape[1]
+    for gap in (0, 1, 2, 3, 6):
+        for start in (0, 1, 2, 3):
+            whole = torch.full((start + 5 * (size + gap) + 8,), 9.0, device="cuda")
+            G = torch.as_strided(whole, (5, size), (size + gap, 1), start)
+            lib.cdgrab_pergrad_linear(h, x, d, G_out=G)
+            assert torch.equal(G, want)
+            G.fill_(9.0)
+            assert (whole == 9.0).all()
+
+
 def test_spans_that_leave_the_arrays_are_cut(lib):
     x, d = rand(1, 20, 40), rand(2, 20, 50)
     first = torch.tensor([-5, 18, 25, 0, 3, 20, 19], dtype=torch.int64, device="cuda")
@@ -350,6 +367,23 @@ def test_refusals(lib):
         with pytest.raises(lib.CdgrabError) as err:
             call()
         assert err.value.code == -1 and "cdgrab_" in str(err.value)
+    # sizes and addresses that the binding would not make
+    import ctypes
+    from paper_2302_00845_amd.cdgrab import _TokenRows
+    big = torch.zeros(4000, device="cuda")
+    p, q = x.data_ptr(), big.data_ptr()
+    lib_h, ok = h._lib, _TokenRows(2, 6, 3, None, None)
+    assert lib_h.cdgrab_layernorm(h._h, 6, 8, 7, p, 8, None, None, 1e-5, q, 8) == -1  # no such type
+    assert lib_h.cdgrab_layernorm(h._h, 6, 8, 0, p, 7, None, None, 1e-5, q, 8) == -1  # rows overlap
+    assert lib_h.cdgrab_layernorm(h._h, 6, 8, 0, p + 1, 8, None, None, 1e-5, q, 8) == -1  # between elements
+    assert lib_h.cdgrab_layernorm(h._h, -1, 8, 0, p, 8, None, None, 1e-5, q, 8) == -1
+    assert lib_h.cdgrab_layernorm(h._h, 6, 8, 0, None, 8, None, None, 1e-5, q, 8) == -1
+    for t in (None, _TokenRows(3, 6, 3, None, None), _TokenRows(-1, 6, 3, None, None), _TokenRows(2, 6, -3, None, None)):
+        t = ctypes.byref(t) if t is not None else None
+        assert lib_h.cdgrab_pergrad_linear(h._h, t, 8, 5, 0, p, 8, d.data_ptr(), 5, 1, q, 45) == -1
+        assert lib_h.cdgrab_pergrad_layernorm(h._h, t, 8, 0, p, 8, q, 8, None, 1e-5, None, 8, 1, q + 400, 16) == -1
+    for n_in, n_out, bias, g_stride in ((0, 5, 1, 45), (8, 2 ** 20 + 1, 1, 2 ** 30), (2 ** 20, 2 ** 13, 1, 2 ** 40), (8, 5, 2, 45), (8, 5, 1, 44)):
+        assert lib_h.cdgrab_pergrad_linear(h._h, ctypes.byref(ok), n_in, n_out, 0, p, 2 ** 20, d.data_ptr(), 2 ** 20, bias, q, g_stride) == -1
     whole = torch.zeros(6, 100, device="cuda")
     with pytest.raises(lib.CdgrabError):  # the gradients' rows lie in the input's
         lib.cdgrab_pergrad_linear(h, whole[:, :4].unsqueeze(0), torch.zeros(1, 6, 3, device="cuda"), G_out=whole[:1, 2:17])

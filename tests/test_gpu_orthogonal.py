@@ -64,7 +64,8 @@ def test_matches_the_definition(lib, rows, cols, dtype):
 
 
 @pytest.mark.parametrize("batch,rows,cols", [(3, 20, 7), (300, 5, 6), (2, 3, 10000), (3, 130, 70), (40, 128, 192), (5, 100, 800),
-                                             (260, 12, 5000)])
+                                             (260, 12, 5000), (24, 300, 500), (24, 500, 300), (60, 300, 260), (3, 33, 250), (2, 64, 500),
+                                             (2, 250, 33), (5, 128, 120), (2, 60, 700), (300, 40, 90)])
 def test_batches(lib, batch, rows, cols):
     m = rand(batch, batch, rows, cols)
     m[batch // 2] *= 1e-12  # each matrix has its own norm
@@ -198,6 +199,14 @@ def test_refusals(lib):
         with pytest.raises(lib.CdgrabError) as err:
             call()
         assert err.value.code == -1
+    p, lim = m.data_ptr(), 2 ** 21 + 1  # sizes that no array here has: refused before anything is looked at
+    for b, r, c in ((lim, 20, 30), (1, 2 ** 20 + 1, 1), (1, 16385, 16385), (1, 8192, 2 ** 20), (-1, 2, 2)):
+        assert h._lib.cdgrab_orthogonalize(h._h, b, r, c, 0, p, c, r * c, 5, None, p, c, r * c) == -1
+    assert h._lib.cdgrab_orthogonalize(h._h, 1, 20, 30, 3, p, 30, 0, 5, None, p, 30, 0) == -1  # no such type
+    assert h._lib.cdgrab_orthogonalize(h._h, 1, 20, 30, 0, p, 29, 0, 5, None, whole.data_ptr(), 30, 0) == -1  # rows overlap
+    assert h._lib.cdgrab_orthogonalize(h._h, 2, 20, 30, 0, p, 30, 599, 5, None, whole.data_ptr(), 30, 600) == -1  # matrices do
+    assert h._lib.cdgrab_orthogonalize(h._h, 1, 20, 30, 0, p + 2, 30, 0, 5, None, whole.data_ptr(), 30, 0) == -1  # between elements
+    assert h._lib.cdgrab_orthogonalize(h._h, 1, 20, 30, 0, None, 30, 0, 5, None, whole.data_ptr(), 30, 0) == -1
     for call in (lambda: lib.cdgrab_orthogonalize(h, m.double()), lambda: lib.cdgrab_orthogonalize(h, m[0]),
                  lambda: lib.cdgrab_orthogonalize(h, m.t()), lambda: lib.cdgrab_orthogonalize(h, m, out=torch.empty(20, 31, device="cuda"))):
         with pytest.raises((TypeError, ValueError)):
