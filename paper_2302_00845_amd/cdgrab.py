@@ -384,21 +384,19 @@ def cdgrab_balance_epoch_randomized(h: Handle, grads: torch.Tensor, uniforms: to
 
 def _rows(t: torch.Tensor, name: str, device, like: Optional[torch.Tensor] = None):
     """(pointer, rows, width, stride) of an array of rows: [..., width] with elements side by side and one
-    distance from row to row."""
+    distance from row to row.  `like`: of the same type and shape."""
     if t.dtype not in _ELEM:
         raise TypeError("%s must be float32, bfloat16 or float16, got %s" % (name, t.dtype))
     if t.device != device:
         raise ValueError("%s must live on %s, got %s" % (name, device, t.device))
     shape = t.shape
+    if like is not None and (shape != like.shape or t.dtype != like.dtype):
+        raise ValueError("%s must be %s %s, got %s %s" % (name, like.dtype, tuple(like.shape), t.dtype, tuple(shape)))
     if len(shape) < 2:
         raise ValueError("%s must have rows and a width, got shape %s" % (name, tuple(shape)))
-    if like is not None and (t.dtype != like.dtype or shape[:-1] != like.shape[:-1]):
-        raise ValueError("%s must be %s of rows %s, got %s %s" % (name, like.dtype, tuple(like.shape[:-1]), t.dtype,
-                                                                  tuple(shape)))
     width = shape[-1]
     if t.is_contiguous():
-        rows = t.numel() // width if width else 0
-        return t.data_ptr(), rows, width, max(width, 1)
+        return t.data_ptr(), t.numel() // width if width else 0, width, width or 1
     rows, stride = 1, width
     for n in shape[:-1]:
         rows *= n
@@ -416,14 +414,26 @@ def _rows(t: torch.Tensor, name: str, device, like: Optional[torch.Tensor] = Non
     return t.data_ptr(), rows, width, max(stride, 1)
 
 
+def _vector(t: Optional[torch.Tensor], n: int, name: str, device) -> Optional[int]:
+    """Pointer of a contiguous float32 [n], or None."""
+    if t is None:
+        return None
+    if t.dtype is torch.float32 and t.dim() == 1 and t.shape[0] == n and t.is_contiguous() and t.device == device:
+        return t.data_ptr()
+    return _ptr(t, torch.float32, (n,), name, device)  # (says what is wrong)
+
+
 def _token_rows(X: torch.Tensor, rows: int, first, count, tokens: Optional[int], device) -> _TokenRows:
     """X is [examples][tokens][width], or [rows][width] with `first` and `tokens` (packed)."""
     if first is None:
         if X.dim() != 3:
             raise ValueError("X must be [examples][tokens][width] unless `first` says where examples start")
-        if tokens is not None and tokens != X.shape[1]:
-            raise ValueError("tokens is %d, and X has %d per example" % (tokens, X.shape[1]))
-        examples, tokens = X.shape[0], X.shape[1]
+        examples, own, _ = X.shape
+        if tokens is not None and tokens != own:
+            raise ValueError("tokens is %d, and X has %d per example" % (tokens, own))
+        tokens = own
+        if count is None:
+            return _TokenRows(examples, rows, tokens, None, None)
     else:
         if tokens is None:
             raise ValueError("`first` needs `tokens`, the rows that an example has at most")
@@ -435,7 +445,7 @@ def _token_rows(X: torch.Tensor, rows: int, first, count, tokens: Optional[int],
 def _grad_rows(G_out: Optional[torch.Tensor], examples: int, d: int, device):
     """(G, stride): [examples][d] fp32, a stretch of longer rows if given so."""
     if G_out is None:
-        return torch.empty((examples, d), dtype=torch.float32, device=device), max(d, 1)
+        return torch.empty((examples, d), dtype=torch.float32, device=device), d or 1
     if G_out.dtype != torch.float32:
         raise TypeError("G_out must be float32, got %s" % G_out.dtype)
     if tuple(G_out.shape) != (examples, d):
@@ -448,17 +458,15 @@ def cdgrab_layernorm(h: Handle, X: torch.Tensor, gain: Optional[torch.Tensor] = 
                      bias: Optional[torch.Tensor] = None, eps: float = 1e-5,
                      Y: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Layer norm over the last axis of X[..., width]; gain and bias [width] float32."""
-    px, rows, width, sx = _rows(X, "X", h.device)
+    dev = h.device
+    px, rows, width, sx = _rows(X, "X", dev)
     if Y is None:
         Y = torch.empty_like(X, memory_format=torch.contiguous_format)
-        py, sy = Y.data_ptr(), max(width, 1)
+        py, sy = Y.data_ptr(), width or 1
     else:
-        py, _, wy, sy = _rows(Y, "Y", h.device, X)
-        if wy != width:
-            raise ValueError("Y must have shape %s, got %s" % (tuple(X.shape), tuple(Y.shape)))
-    h._check(h._lib.cdgrab_layernorm(
-        h._h, rows, width, _ELEM[X.dtype], px, sx, _ptr(gain, torch.float32, (width,), "gain", h.device),
-        _ptr(bias, torch.float32, (width,), "bias", h.device), eps, py, sy))
+        py, _, _, sy = _rows(Y, "Y", dev, X)
+    h._check(h._lib.cdgrab_layernorm(h._h, rows, width, _ELEM[X.dtype], px, sx, _vector(gain, width, "gain", dev),
+                                     _vector(bias, width, "bias", dev), eps, py, sy))
     return Y
 
 
@@ -472,28 +480,25 @@ def cdgrab_pergrad_layernorm(h: Handle, X: torch.Tensor, dY: torch.Tensor, gain:
     X and dY are [examples][tokens][width] (with `count` a padded batch), or [rows][width] with the examples' rows
     packed: `first` [examples] int64, `count` int32, `tokens` at most.  Rows of no example keep what dX holds (zero
     where the call makes dX).  G_out may be a stretch of columns of longer rows."""
-    px, rows, width, sx = _rows(X, "X", h.device)
-    py, _, wy, sy = _rows(dY, "dY", h.device, X)
-    if wy != width:
-        raise ValueError("dY must have shape %s, got %s" % (tuple(X.shape), tuple(dY.shape)))
-    t = _token_rows(X, rows, first, count, tokens, h.device)
+    dev = h.device
+    px, rows, width, sx = _rows(X, "X", dev)
+    py, _, _, sy = _rows(dY, "dY", dev, X)
+    t = _token_rows(X, rows, first, count, tokens, dev)
     pd, sd = None, width
-    if dX is not None or want_dx:
-        if dX is None:
-            dX = torch.empty_like(X, memory_format=torch.contiguous_format)
-            if first is not None or count is not None:
-                with torch.cuda.stream(h.stream):  # before the call's kernels, wherever they run
-                    dX.zero_()
-        pd, _, wd, sd = _rows(dX, "dX", h.device, X)
-        if wd != width:
-            raise ValueError("dX must have shape %s, got %s" % (tuple(X.shape), tuple(dX.shape)))
-    G, sg = None, 0
+    if dX is not None:
+        pd, _, _, sd = _rows(dX, "dX", dev, X)
+    elif want_dx:
+        dX = torch.empty_like(X, memory_format=torch.contiguous_format)
+        if first is not None or count is not None:
+            with torch.cuda.stream(h.stream):  # before the call's kernels, wherever they run
+                dX.zero_()
+        pd, sd = dX.data_ptr(), width or 1
+    G, pg, sg = None, None, 0
     if G_out is not None or want_grads:
-        G, sg = _grad_rows(G_out, t.examples, (2 if with_bias else 1) * width, h.device)
-    h._check(h._lib.cdgrab_pergrad_layernorm(
-        h._h, ctypes.byref(t), width, _ELEM[X.dtype], px, sx, py, sy,
-        _ptr(gain, torch.float32, (width,), "gain", h.device), eps, pd, sd, 1 if with_bias else 0,
-        G.data_ptr() if G is not None else None, sg))
+        G, sg = _grad_rows(G_out, t.examples, (2 if with_bias else 1) * width, dev)
+        pg = G.data_ptr()
+    h._check(h._lib.cdgrab_pergrad_layernorm(h._h, ctypes.byref(t), width, _ELEM[X.dtype], px, sx, py, sy,
+                                             _vector(gain, width, "gain", dev), eps, pd, sd, 1 if with_bias else 0, pg, sg))
     return dX, G
 
 
@@ -502,12 +507,15 @@ def cdgrab_pergrad_linear(h: Handle, X: torch.Tensor, D: torch.Tensor, with_bias
                           tokens: Optional[int] = None, G_out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Per-example gradients G[examples][(in + 1) * out] of a linear layer's weights (last `out`: the bias) from its
     inputs X and its outputs' gradients D; rows of examples as in cdgrab_pergrad_layernorm."""
-    px, rows, n_in, sx = _rows(X, "X", h.device)
-    pd, _, n_out, sd = _rows(D, "D", h.device, X)
-    t = _token_rows(X, rows, first, count, tokens, h.device)
-    G, sg = _grad_rows(G_out, t.examples, (n_in + (1 if with_bias else 0)) * n_out, h.device)
-    h._check(h._lib.cdgrab_pergrad_linear(
-        h._h, ctypes.byref(t), n_in, n_out, _ELEM[X.dtype], px, sx, pd, sd, 1 if with_bias else 0, G.data_ptr(), sg))
+    dev = h.device
+    px, rows, n_in, sx = _rows(X, "X", dev)
+    pd, _, n_out, sd = _rows(D, "D", dev)
+    if D.dtype != X.dtype or D.shape[:-1] != X.shape[:-1]:
+        raise ValueError("D must be %s of rows %s, got %s %s" % (X.dtype, tuple(X.shape[:-1]), D.dtype, tuple(D.shape)))
+    t = _token_rows(X, rows, first, count, tokens, dev)
+    G, sg = _grad_rows(G_out, t.examples, (n_in + (1 if with_bias else 0)) * n_out, dev)
+    h._check(h._lib.cdgrab_pergrad_linear(h._h, ctypes.byref(t), n_in, n_out, _ELEM[X.dtype], px, sx, pd, sd,
+                                          1 if with_bias else 0, G.data_ptr(), sg))
     return G
 
 
@@ -526,21 +534,21 @@ def cdgrab_orthogonalize(h: Handle, M: torch.Tensor, steps: int = 5, coeffs=None
         raise ValueError("M must be [rows][cols] or [batch][rows][cols], got %s" % (tuple(M.shape),))
     if out is None:
         out = torch.empty_like(M, memory_format=torch.contiguous_format)
+    elif out.dtype != M.dtype or out.shape != M.shape:
+        raise ValueError("out must be %s %s, got %s %s" % (M.dtype, tuple(M.shape), out.dtype, tuple(out.shape)))
+    if M.dtype not in _ELEM:
+        raise TypeError("M must be float32, bfloat16 or float16, got %s" % M.dtype)
+    rows, cols = M.shape[-2:]
     at = []
     for t, name in ((M, "M"), (out, "out")):
-        if t.dtype not in _ELEM:
-            raise TypeError("%s must be float32, bfloat16 or float16, got %s" % (name, t.dtype))
         if t.device != h.device:
             raise ValueError("%s must live on %s, got %s" % (name, h.device, t.device))
-        if t.dtype != M.dtype or t.shape != M.shape:
-            raise ValueError("out must be %s %s, got %s %s" % (M.dtype, tuple(M.shape), t.dtype, tuple(t.shape)))
-        if t.shape[-1] > 1 and t.stride(-1) != 1:
+        strides = t.stride()
+        if cols > 1 and strides[-1] != 1:
             raise ValueError("%s: the elements of a row must lie side by side" % name)
-        row = t.stride(-2) if t.shape[-2] > 1 else t.shape[-1]
-        at.append((t.data_ptr(), row, t.stride(0) if t.dim() == 3 else 0))
-    batch = M.shape[0] if M.dim() == 3 else 1
-    h._check(h._lib.cdgrab_orthogonalize(h._h, batch, M.shape[-2], M.shape[-1], _ELEM[M.dtype], at[0][0], at[0][1], at[0][2],
-                                         steps, _coeffs(coeffs), at[1][0], at[1][1], at[1][2]))
+        at.append((t.data_ptr(), strides[-2] if rows > 1 else cols, strides[0]))
+    h._check(h._lib.cdgrab_orthogonalize(h._h, M.shape[0] if M.dim() == 3 else 1, rows, cols, _ELEM[M.dtype], *at[0], steps,
+                                         _coeffs(coeffs), *at[1]))
     return out
 
 
