@@ -1610,6 +1610,9 @@ int cdgrab_train_epoch_softmax_orthogonal(cdgrab_handle *h, int64_t m, int64_t n
     const int rc = ortho_coeffs(h, who, steps, coeffs, &c);
     if (rc) return rc;
     if (!velocity) return fail(h, CDGRAB_EINVAL, "%s: needs a velocity buffer", who);
+    if (in_dim > 0 && in_dim <= (1 << 20) && classes > 0 && classes <= 1024 &&
+        ranges_overlap(W, (in_dim + 1) * classes * 4, velocity, (in_dim + 1) * classes * 4))
+        return fail(h, CDGRAB_EINVAL, "%s: W and velocity must not overlap", who);
     return train_epoch_impl(h, who, m, n, in_dim, classes, X, y, perm_in, W, velocity, lr, momentum, steps, c, signs_out, perm_out,
                             grads_out, loss_out);
 }

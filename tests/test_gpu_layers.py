@@ -443,3 +443,26 @@ def test_a_block_of_layers_makes_the_balancers_rows(lib):
     from parity import check_epoch
     got = {k: (v.cpu().numpy() if v is not None else None) for k, v in out.items()}
     check_epoch(rows.view(m, n, d).cpu().numpy(), got)
+
+
+@pytest.mark.parametrize("tokens,n_in,n_out", [(2, 50, 20), (6, 300, 40), (90, 140, 150), (1200, 40, 70)])
+def test_the_same_rows_in_several_examples(lib, tokens, n_in, n_out):
+    """Examples may share rows, all of them too: each has its own sums, and dX is the row's whoever it belongs to."""
+    rows = tokens + 7
+    x, d, dy = rand(1, rows, n_in), rand(2, rows, n_out), rand(3, rows, n_in)
+    spans = [(3, tokens), (3, tokens), (0, tokens), (5, tokens - 1), (3, tokens)]
+    first, count = device_spans(*zip(*spans))
+    h = lib.Handle()
+    want, tol = linear64(x, d, spans, torch.float32)
+    g = lib.cdgrab_pergrad_linear(h, x, d, first=first, count=count, tokens=tokens)
+    close(g, want, tol, "linear")
+    assert torch.equal(g[0], g[1]) and torch.equal(g[0], g[4])
+    want_dx, tol_dx, want_g, tol_g = grad64(x, dy, torch.ones(n_in, device="cuda"), 1e-5, spans, torch.float32)
+    dx, g = lib.cdgrab_pergrad_layernorm(h, x, dy, first=first, count=count, tokens=tokens)
+    close(g, want_g, tol_g, "norm")
+    assert torch.equal(g[0], g[1]) and torch.equal(g[0], g[4])
+    inside = torch.zeros(rows, dtype=torch.bool, device="cuda")
+    for a, c in spans:
+        inside[a:a + c] = True
+    close(dx[inside], want_dx[inside], tol_dx[inside], "dX")
+    assert (dx[~inside] == 0).all()

@@ -270,3 +270,78 @@ def test_training_epoch_refusals_and_steps(lib):
     # each step of an update of norm one moves the weights by lr at the most
     lib.cdgrab_train_epoch_softmax_orthogonal(h, X, y, W, v, lr=0.5, steps=0)
     assert (W.cpu() - torch.from_numpy(W0)).norm().item() <= 4 * 0.5 * (1 + 100 * U)
+
+
+def test_training_epoch_velocity_apart_from_the_weights(lib):
+    X, y, W0 = workloads.softmax_problem(0, 8, 6, 3)
+    X, y = torch.from_numpy(X).cuda().view(2, 4, 6), torch.from_numpy(y).cuda().view(2, 4)
+    h = lib.Handle()
+    for at in (0, 9, 20):  # 21 elements each
+        with pytest.raises(lib.CdgrabError) as err:
+            big = torch.zeros(45, device="cuda")
+            lib.cdgrab_train_epoch_softmax_orthogonal(h, X, y, big[:21].view(7, 3), big[at:at + 21])
+        assert err.value.code == -1 and "overlap" in str(err.value)
+    both = torch.zeros(42, device="cuda")
+    lib.cdgrab_train_epoch_softmax_orthogonal(h, X, y, both[:21].view(7, 3), both[21:])
+    assert torch.isfinite(both).all()
+
+
+@pytest.mark.parametrize("m,n,in_dim,classes", [(3, 10, 7, 5), (5, 6, 90, 80), (2, 4, 300, 200)])
+def test_training_epoch_recorded(lib, m, n, in_dim, classes):
+    X, y, W0 = workloads.softmax_problem(m + n, m * n, in_dim, classes)
+    X, y, W0 = torch.from_numpy(X).cuda().view(m, n, in_dim), torch.from_numpy(y).cuda().view(m, n), torch.from_numpy(W0).cuda()
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(stream):
+        h = lib.Handle(stream=stream)
+        W, v = W0.clone(), torch.zeros(W0.numel(), device="cuda")
+        want = lib.cdgrab_train_epoch_softmax_orthogonal(h, X, y, W, v)
+        stream.synchronize()
+        want_W, want_v = W.clone(), v.clone()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            got = lib.cdgrab_train_epoch_softmax_orthogonal(h, X, y, W, v)
+        lib.cdgrab_orthogonalize(h, rand(1, 2, 500, 400))  # a larger workspace in between
+        for _ in range(3):
+            W.copy_(W0)
+            v.zero_()
+            graph.replay()
+            stream.synchronize()
+            assert torch.equal(W, want_W) and torch.equal(v, want_v)
+            for key in ("signs", "perm", "loss"):
+                assert torch.equal(got[key], want[key])
+            lib.cdgrab_orthogonalize(h, rand(2, 300, 100))
+
+
+def test_two_recordings_and_two_handles(lib):
+    """Recordings of one handle share its workspace and follow one another; another handle's call runs beside them."""
+    a, b, c = rand(1, 3, 200, 300), rand(2, 150, 260), rand(3, 4, 140, 200)
+    base = lib.Handle()
+    want = [lib.cdgrab_orthogonalize(base, t) for t in (a, b, c)]
+    torch.cuda.synchronize()
+    stream, beside = torch.cuda.Stream(), torch.cuda.Stream()
+    with torch.cuda.stream(beside):
+        other = lib.Handle(stream=beside)
+        out_c = torch.empty_like(c)
+    with torch.cuda.stream(stream):
+        h = lib.Handle(stream=stream)
+        out_a, out_b = torch.empty_like(a), torch.empty_like(b)
+        graphs = []
+        for t, o in ((b, out_b), (a, out_a)):  # (the second takes a larger workspace than the first one has recorded)
+            lib.cdgrab_orthogonalize(h, t, out=o)
+            stream.synchronize()
+            graphs.append(torch.cuda.CUDAGraph())
+            with torch.cuda.graph(graphs[-1], stream=stream):
+                lib.cdgrab_orthogonalize(h, t, out=o)
+    for _ in range(4):
+        for o in (out_a, out_b, out_c):
+            o.fill_(float("nan"))
+        torch.cuda.synchronize()
+        with torch.cuda.stream(beside):
+            lib.cdgrab_orthogonalize(other, c, out=out_c)
+        with torch.cuda.stream(stream):
+            for g in graphs:
+                g.replay()
+        torch.cuda.synchronize()
+        for o, w in zip((out_a, out_b, out_c), want):
+            assert torch.equal(o, w)
