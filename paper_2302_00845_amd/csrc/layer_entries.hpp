@@ -263,9 +263,15 @@ int run_ortho_products(cdgrab_handle *h, const char *who, int64_t batch, OrthoIo
     const int64_t most = std::max<int64_t>(1, std::min(kOrthoBytes / 2 / per_matrix,
                                                        kMaxGroups / std::max(tm * tn, (sp / 32) * (lp / 32))));
     const int64_t at_once = std::min(batch, most);
+    // Few tiles and a long side: the Gram matrix in shares of it, of 24 stages at least, until there is a workgroup for every CU (us,
+    // whole -> in shares: 2 x 200 x 12000 542 -> 251, 1 x 768 x 2304 251 -> 233)
+    const int64_t half = tm * (tm + 1) / 2;
+    const int64_t shares = TILE == 64 ? std::max<int64_t>(1, std::min(h->num_cu / (at_once * half), lp / (24 * 32))) : 1;
+    const int64_t shares_len = shares > 1 ? at_once * half * shares * TILE * TILE * 2 : 0;  // (in fp16 elements)
     f16_t *ws = nullptr;
-    const int rc = layer_room(h, who, at_once * per_matrix, &ws);
+    const int rc = layer_room(h, who, at_once * per_matrix + shares_len, &ws);
     if (rc) return rc;
+    float *const parts = reinterpret_cast<float *>(ws + at_once * per_matrix);
     double *sums = reinterpret_cast<double *>(ws);
     f16_t *at = ws + at_once * kOrthoSums * 4;
     const auto take = [&](int64_t len) {
@@ -287,24 +293,44 @@ int run_ortho_products(cdgrab_handle *h, const char *who, int64_t batch, OrthoIo
         const auto go = [&](auto kernel, const OrthoProduct &p, int64_t tiles) {
             hipLaunchKernelGGL(kernel, dim3((unsigned)(n * tiles)), dim3(256), 0, h->stream, p, part);
         };
+        constexpr int Q = TILE == 64 ? 2 : 1;
+        // Tiles that leave CUs idle are computed by eight wavefronts, from ten stages on (768 x 768 201 -> 179 us, 512 x 512 150 -> 135; with
+        // four to six stages 130 x 70 81 -> 89).
+        const auto wide = [&](const OrthoProduct &p, int64_t tiles) { return Q == 2 && p.k >= 320 && n * tiles <= h->num_cu; };
+        const auto go2 = [&](auto kernel, const OrthoProduct &p, int64_t tiles) {
+            hipLaunchKernelGGL(kernel, dim3((unsigned)(n * tiles)), dim3(256 * Q), 0, h->stream, p, part);
+        };
         // Stages of LDS: two leave room for two workgroups per CU, four for one, which is what there is when the tiles are few.  (24
         // matrices of 768 x 768 945 us with two, 1030 with four; 12 of 768 x 2304, whose Gram matrices have 252 tiles, 1203 and 1194.)
         for (int64_t s = 0; s < steps; ++s) {
-            const int64_t half = tm * (tm + 1) / 2;
-            const auto sym = [&](auto kernel2, auto kernel4, const OrthoProduct &p) {
-                if (TILE == 64 || n * half <= h->num_cu) go(kernel4, p, half);
+            const auto sym = [&](auto kernel2, auto kernel4, auto kernel8, const OrthoProduct &p) {
+                if (wide(p, half)) go2(kernel8, p, half);
+                else if (TILE == 64 || n * half <= h->num_cu) go(kernel4, p, half);
                 else go(kernel2, p, half);
             };
-            sym(ortho_product_tile<TILE, 2, kOrthoGram, T>, ortho_product_tile<TILE, 4, kOrthoGram, T>,
-                OrthoProduct{X, X, A, A, lp, lp, sp, x_len, x_len, a_len, (int)lp, (int)tm, (int)tm, 0.f,
-                             kOrthoScaleA / (kOrthoScaleX * kOrthoScaleX)});
-            sym(ortho_product_tile<TILE, 2, kOrthoPoly, T>, ortho_product_tile<TILE, 4, kOrthoPoly, T>,
+            const OrthoProduct gram{X, X, A, A, lp, lp, sp, x_len, x_len, a_len, (int)lp, (int)tm, (int)tm, 0.f,
+                                    kOrthoScaleA / (kOrthoScaleX * kOrthoScaleX), (int)shares, parts};
+            if constexpr (TILE == 64) {
+                if (shares > 1) {
+                    go2(ortho_product_tile<TILE, 4, Q, kOrthoShare, T>, gram, half * shares);
+                    hipLaunchKernelGGL((ortho_gram_finish<TILE>), dim3((unsigned)(n * half)), dim3(256), 0, h->stream, gram);
+                }
+            }
+            if (shares == 1)
+                sym(ortho_product_tile<TILE, 2, 1, kOrthoGram, T>, ortho_product_tile<TILE, 4, 1, kOrthoGram, T>,
+                    ortho_product_tile<TILE, 4, Q, kOrthoGram, T>, gram);
+            sym(ortho_product_tile<TILE, 2, 1, kOrthoPoly, T>, ortho_product_tile<TILE, 4, 1, kOrthoPoly, T>,
+                ortho_product_tile<TILE, 4, Q, kOrthoPoly, T>,
                 OrthoProduct{A, A, A, B, sp, sp, sp, a_len, a_len, a_len, (int)sp, (int)tm, (int)tm, (float)c.b,
-                             (float)(c.c / kOrthoScaleA)});
-            const OrthoProduct step{B, X, X, Y, sp, lp, lp, a_len, x_len, x_len, (int)sp, (int)tm, (int)tn, (float)c.a, 1.f / kOrthoScaleA};
+                             (float)(c.c / kOrthoScaleA), 1, nullptr});
+            const OrthoProduct step{B, X, X, Y, sp, lp, lp, a_len, x_len, x_len, (int)sp, (int)tm, (int)tn, (float)c.a, 1.f / kOrthoScaleA,
+                                    1, nullptr};
             constexpr int NS = TILE == 64 ? 4 : 2;
-            if (s + 1 < steps) go(ortho_product_tile<TILE, NS, kOrthoStep, T>, step, tm * tn);
-            else go(ortho_product_tile<TILE, NS, kOrthoLast, T>, step, tm * tn);
+            if (wide(step, tm * tn)) {
+                if (s + 1 < steps) go2(ortho_product_tile<TILE, NS, Q, kOrthoStep, T>, step, tm * tn);
+                else go2(ortho_product_tile<TILE, NS, Q, kOrthoLast, T>, step, tm * tn);
+            } else if (s + 1 < steps) go(ortho_product_tile<TILE, NS, 1, kOrthoStep, T>, step, tm * tn);
+            else go(ortho_product_tile<TILE, NS, 1, kOrthoLast, T>, step, tm * tn);
             std::swap(X, Y);
         }
     }

@@ -416,11 +416,11 @@ __global__ __launch_bounds__(256) void ortho_begin(OrthoIo<T> io, const double *
     }
 }
 
-enum OrthoWhat { kOrthoGram, kOrthoPoly, kOrthoStep, kOrthoLast };
+enum OrthoWhat { kOrthoGram, kOrthoShare, kOrthoPoly, kOrthoStep, kOrthoLast };
 
 // One tile of a product of pairs, L R^T (Gram, Poly: R's rows, both with their elements along k) or L R (Step, Last: R's rows
 // along k), then
-//   Gram: A = X X^T;  Poly: B = b A + c A A;  Step: X' = a X + B X;  Last: O = (a X + B X) to the caller's array.
+//   Gram: A = X X^T;  Share: the sums of a share of k, for ortho_gram_finish;  Poly: B = b A + c A A;  Step: X' = a X + B X;  Last: O = (a X + B X) to the caller's array.
 // K is a multiple of 32, the tile's sides T of 32: nothing to clip but O.
 struct OrthoProduct {
     const f16_t *L, *R, *E;  // factors, what is added: matrices of pairs
@@ -428,35 +428,66 @@ struct OrthoProduct {
     int64_t l_ld, r_ld, c_ld, l_matrix, r_matrix, c_matrix;  // (E lies as C does; fp16 from matrix to matrix)
     int k, tiles_m, tiles_n;
     float alpha, beta;  // result = alpha E + beta (product as multiplied)
+    int shares;         // Share: of k, and where their sums go: [matrix][share][tile][T][T]
+    float *sums;
 };
 
-template <int T, int NS, int WHAT, typename U>
-__global__ __launch_bounds__(256, NS * T * 256 > 80 * 1024 ? 1 : 2) void ortho_product_tile(OrthoProduct p, OrthoIo<U> io)
+// The t-th of the tiles on or above the diagonal, column after column.
+__device__ __forceinline__ void ortho_upper_tile(int t, int &tm, int &tn) {
+    tn = (int)((sqrtf(8.f * (float)t + 1.f) - 1.f) * 0.5f);
+    while ((tn + 1) * (tn + 2) / 2 <= t) ++tn;
+    while (tn * (tn + 1) / 2 > t) --tn;
+    tm = t - tn * (tn + 1) / 2;
+}
+
+// Eight neighbours of a row of a matrix of pairs.
+__device__ __forceinline__ void ortho_store_pairs(f16_t *p, const float (&v)[8]) {
+    f16x8 hi, lo;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        f16_t x, y;
+        ortho_split(v[j], x, y);
+        hi[j] = x;
+        lo[j] = y;
+    }
+    *reinterpret_cast<f16x8 *>(p) = hi;
+    *reinterpret_cast<f16x8 *>(p + 32) = lo;
+}
+
+// QUADS: that many times four wavefronts share a tile, each four with every QUADS-th stage of k and stages of their own (for where
+// tiles are fewer than CUs and a tile's time is a chain of stages).
+template <int T, int NS, int QUADS, int WHAT, typename U>
+__global__ __launch_bounds__(256 * QUADS, NS * T * 256 > 80 * 1024 ? 1 : 2) void ortho_product_tile(OrthoProduct p, OrthoIo<U> io)
 {
     constexpr bool ACROSS = WHAT == kOrthoStep || WHAT == kOrthoLast, SYM = !ACROSS;
     typedef PairTile<T> O;
     constexpr int MB = T / 64, LD = T + 1;  // (eight rows further is eight banks further)
-    constexpr int STAGE = 2 * O::LEN, BYTES = NS * STAGE * 2, OUT = T / 2 * LD * 4, LOADS = 2 * O::CALLS;
+    constexpr int STAGE = 2 * O::LEN, BYTES = QUADS * NS * STAGE * 2, OUT = T / 2 * LD * 4, LOADS = 2 * O::CALLS;
     __shared__ __align__(16) char lds[BYTES > OUT ? BYTES : OUT];
-    f16_t *stage = reinterpret_cast<f16_t *>(lds);
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave >> 1, wn = wave & 1;
+    const int lane = threadIdx.x & 63, quad = QUADS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 8);
+    const int tid = threadIdx.x & 255, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave >> 1, wn = wave & 1;
+    f16_t *stage = reinterpret_cast<f16_t *>(lds) + quad * NS * STAGE;
     const int per = SYM ? p.tiles_m * (p.tiles_m + 1) / 2 : p.tiles_m * p.tiles_n;
     const uint32_t id = xcd_neighbours(blockIdx.x, gridDim.x);
-    const int64_t b = id / (uint32_t)per;
+    const uint32_t group = id / (uint32_t)per;  // matrix, or matrix and share
+    const int64_t b = WHAT == kOrthoShare ? group / (uint32_t)p.shares : group;
     int tm, tn;
-    if constexpr (SYM) {  // tiles on or above the diagonal, column after column
-        const int t = (int)(id - b * per);
-        tn = (int)((sqrtf(8.f * (float)t + 1.f) - 1.f) * 0.5f);
-        while ((tn + 1) * (tn + 2) / 2 <= t) ++tn;
-        while (tn * (tn + 1) / 2 > t) --tn;
-        tm = t - tn * (tn + 1) / 2;
+    if constexpr (SYM) {
+        ortho_upper_tile((int)(id - group * per), tm, tn);
     } else {
-        const int t = (int)(id - b * per);
+        const int t = (int)(id - group * per);
         tm = t % p.tiles_m;
         tn = t / p.tiles_m;
     }
-    const f16_t *const left = p.L + b * p.l_matrix + (int64_t)tm * T * 2 * p.l_ld;
-    const f16_t *const right = p.R + b * p.r_matrix + (ACROSS ? (int64_t)tn * T * 2 : (int64_t)tn * T * 2 * p.r_ld);
+    int stages = p.k / O::KC, begin = 0;
+    if constexpr (WHAT == kOrthoShare) {  // (a share has a multiple of QUADS stages, and one at least)
+        const int units = stages / QUADS, share = (int)(group % (uint32_t)p.shares);
+        begin = (int)((int64_t)units * share / p.shares) * QUADS;
+        stages = (int)((int64_t)units * (share + 1) / p.shares) * QUADS - begin;
+    }
+    stages /= QUADS;
+    const f16_t *const left = p.L + b * p.l_matrix + (int64_t)tm * T * 2 * p.l_ld + begin * 64;
+    const f16_t *const right = p.R + b * p.r_matrix + begin * 64 + (ACROSS ? (int64_t)tn * T * 2 : (int64_t)tn * T * 2 * p.r_ld);
     // (the products with the small parts in sums of their own: as parts of one sum each would round it once more, 2468
     // columns 3.3e-6 off instead of 1.9e-6)
     f32x16 acc[MB][MB], low[MB][MB];
@@ -470,6 +501,7 @@ __global__ __launch_bounds__(256, NS * T * 256 > 80 * 1024 ? 1 : 2) void ortho_p
     const PairFetch<T, ACROSS> fetch_r(p.r_ld, wave, lane);
     const auto fetch = [&](int q, int buf) {
         f16_t *s = stage + buf * STAGE;
+        q = q * QUADS + quad;
         fetch_l(left + q * 64, s, wave);
         fetch_r(right + (ACROSS ? q * O::KC * 2 * p.r_ld : q * 64), s + O::LEN, wave);
     };
@@ -510,7 +542,6 @@ __global__ __launch_bounds__(256, NS * T * 256 > 80 * 1024 ? 1 : 2) void ortho_p
     };
     // Half a stage's operands are read while the other half's products run; between the halves the workgroup meets: the next
     // stage is there, and everybody has read this one, whose place the next loads take.
-    const int stages = p.k / O::KC;
     int sent = 0;
     for (; sent < NS && sent < stages; ++sent) fetch(sent, sent);
     if (sent == NS) stage_barrier<(NS - 1) * LOADS>();
@@ -535,38 +566,54 @@ __global__ __launch_bounds__(256, NS * T * 256 > 80 * 1024 ? 1 : 2) void ortho_p
     read(second, (stages - 1) % NS, 1);
     multiply(first);
     multiply(second);
+    if constexpr (QUADS > 1) {  // the second four's sums to the first
+        static_assert(QUADS == 2 && MB == 1 && BYTES >= 256 * 32 * 4, "");
+        float *const sums = reinterpret_cast<float *>(lds) + wave * 32 * 64 + lane;
+        __syncthreads();
+        if (quad == 1)
+#pragma unroll
+            for (int q = 0; q < 16; ++q) {
+                sums[q * 64] = acc[0][0][q];
+                sums[(q + 16) * 64] = low[0][0][q];
+            }
+        __syncthreads();
+        if (quad == 0)
+#pragma unroll
+            for (int q = 0; q < 16; ++q) {
+                acc[0][0][q] += sums[q * 64];
+                low[0][0][q] += sums[(q + 16) * 64];
+            }
+    }
+    if constexpr (WHAT == kOrthoShare) {
+        static_assert(MB == 1, "");
+        float *const to = p.sums + (int64_t)id * T * T;
+        if (quad == 0)
+#pragma unroll
+            for (int q = 0; q < 16; ++q)
+                to[(wm * 32 + 8 * (q >> 2) + 4 * (lane >> 5) + (q & 3)) * T + wn * 32 + (lane & 31)] = acc[0][0][q] + low[0][0][q];
+        return;
+    }
     // The tile goes out through LDS, half its rows at a time, so that every thread stores eight neighbours of a row; a tile
     // above the diagonal also to its mirror image.  What is added is requested before the first half is written.
     constexpr int TASKS = T / 2 * T / 8 / 256;  // of a thread, per half
     const auto place = [&](int64_t row, int64_t col) { return b * p.c_matrix + pair_at(row, col, p.c_ld); };
     f16x8 e_hi[2][TASKS], e_lo[2][TASKS];
     if constexpr (WHAT != kOrthoGram)
+        if (quad == 0)
 #pragma unroll
         for (int half = 0; half < 2; ++half)
 #pragma unroll
             for (int u = 0; u < TASKS; ++u) {
-                const int q = threadIdx.x + u * 256;
+                const int q = tid + u * 256;
                 const int64_t at = place(tm * T + half * (T / 2) + q / (T / 8), tn * T + q % (T / 8) * 8);
                 e_hi[half][u] = *reinterpret_cast<const f16x8 *>(p.E + at);
                 e_lo[half][u] = *reinterpret_cast<const f16x8 *>(p.E + at + 32);
             }
     float *out = reinterpret_cast<float *>(lds);
-    const auto store = [&](const float (&v)[8], int64_t at) {
-        f16x8 hi, lo;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            f16_t x, y;
-            ortho_split(v[j], x, y);
-            hi[j] = x;
-            lo[j] = y;
-        }
-        *reinterpret_cast<f16x8 *>(p.C + at) = hi;
-        *reinterpret_cast<f16x8 *>(p.C + at + 32) = lo;
-    };
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
         __syncthreads();
-        if (wm == half)
+        if (wm == half && quad == 0)
 #pragma unroll
             for (int i = 0; i < MB; ++i)
 #pragma unroll
@@ -582,7 +629,8 @@ __global__ __launch_bounds__(256, NS * T * 256 > 80 * 1024 ? 1 : 2) void ortho_p
         const int m0 = tm * T + half * (T / 2), n0 = tn * T;
 #pragma unroll
         for (int u = 0; u < TASKS; ++u) {
-            const int q = threadIdx.x + u * 256, r = q / (T / 8), c = q % (T / 8) * 8;
+            if (quad != 0) break;
+            const int q = tid + u * 256, r = q / (T / 8), c = q % (T / 8) * 8;
             float v[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
@@ -593,7 +641,7 @@ __global__ __launch_bounds__(256, NS * T * 256 > 80 * 1024 ? 1 : 2) void ortho_p
                 }
             }
             if constexpr (WHAT != kOrthoLast) {
-                store(v, place(m0 + r, n0 + c));
+                ortho_store_pairs(p.C + place(m0 + r, n0 + c), v);
             } else if (!turn && m0 + r < io.short_side) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[j] *= 1.f / kOrthoScaleX;
@@ -604,18 +652,59 @@ __global__ __launch_bounds__(256, NS * T * 256 > 80 * 1024 ? 1 : 2) void ortho_p
         __syncthreads();
 #pragma unroll
         for (int u = 0; u < TASKS; ++u) {
-            const int q = threadIdx.x + u * 256, c = q / (T / 16), r = q % (T / 16) * 8;
+            if (quad != 0) break;
+            const int q = tid + u * 256, c = q / (T / 16), r = q % (T / 16) * 8;
             float v[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] = out[(r + j) * LD + c];
             if constexpr (WHAT != kOrthoLast) {
-                store(v, place(n0 + c, m0 + r));
+                ortho_store_pairs(p.C + place(n0 + c, m0 + r), v);
             } else if (n0 + c < io.long_side) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[j] *= 1.f / kOrthoScaleX;
                 io.put8(b * io.o_matrix + (n0 + c) * io.o_j + (m0 + r), v, io.short_side - m0 - r);
             }
         }
+    }
+}
+
+// A = X X^T from the sums of the shares, in order.  A workgroup takes a tile.
+template <int T>
+__global__ __launch_bounds__(256) void ortho_gram_finish(OrthoProduct p)
+{
+    constexpr int LD = T + 1, TASKS = T * T / 8 / 256;
+    __shared__ float out[T * LD];
+    const int per = p.tiles_m * (p.tiles_m + 1) / 2;
+    const int64_t b = blockIdx.x / (uint32_t)per;
+    const int t = (int)(blockIdx.x - b * per);
+    int tm, tn;
+    ortho_upper_tile(t, tm, tn);
+    const float *from = p.sums + (b * p.shares * per + t) * T * T;
+    f16_t *const C = p.C + b * p.c_matrix;
+#pragma unroll
+    for (int u = 0; u < TASKS; ++u) {
+        const int q = threadIdx.x + u * 256, r = q / (T / 8), c = q % (T / 8) * 8;
+        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+        for (int share = 0; share < p.shares; ++share) {
+            float x[8];
+            load_any<float, 8>(from + (int64_t)share * per * T * T + r * T + c, x);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] += x[j];
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) out[r * LD + c + j] = v[j] = p.beta * v[j];
+        ortho_store_pairs(C + pair_at(tm * T + r, tn * T + c, p.c_ld), v);
+    }
+    if (tm == tn) return;  // uniform
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < TASKS; ++u) {
+        const int q = threadIdx.x + u * 256, c = q / (T / 8), r = q % (T / 8) * 8;
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = out[(r + j) * LD + c];
+        ortho_store_pairs(C + pair_at(tn * T + c, tm * T + r, p.c_ld), v);
     }
 }
 

@@ -345,3 +345,41 @@ def test_two_recordings_and_two_handles(lib):
         torch.cuda.synchronize()
         for o, w in zip((out_a, out_b, out_c), want):
             assert torch.equal(o, w)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("batch,rows,cols", [(2, 200, 12000), (1, 12000, 70), (1, 700, 1600), (1, 66, 1537), (3, 1600, 129), (1, 320, 330),
+                                             (2, 500, 319), (1, 100, 40000)])
+def test_few_tiles_and_long_sides(lib, batch, rows, cols, dtype):
+    """Tiles of eight wavefronts, and Gram matrices in shares of the long side."""
+    m = rand(rows + cols, batch, rows, cols, dtype=dtype)
+    h = lib.Handle()
+    got = lib.cdgrab_orthogonalize(h, m)
+    for b in range(batch):
+        check(got[b], m[b], dtype)
+    assert torch.equal(lib.cdgrab_orthogonalize(h, m), got)
+    m[0, -1, -1] = float("nan")
+    again = lib.cdgrab_orthogonalize(h, m)
+    assert torch.isnan(again[0]).all()
+    assert torch.equal(again[1:], got[1:])
+
+
+def test_shares_recorded(lib):
+    m, small = rand(1, 90, 9000), rand(2, 700, 1600)
+    want = lib.cdgrab_orthogonalize(lib.Handle(), m)
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(stream):
+        h = lib.Handle(stream=stream)
+        out = torch.empty_like(m)
+        lib.cdgrab_orthogonalize(h, m, out=out)
+        stream.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            lib.cdgrab_orthogonalize(h, m, out=out)
+        for _ in range(3):
+            out.fill_(float("nan"))
+            graph.replay()
+            stream.synchronize()
+            assert torch.equal(out, want)
+            lib.cdgrab_orthogonalize(h, small)
