@@ -202,7 +202,8 @@ int run_linear(cdgrab_handle *h, const TokenRows &tok, const T *X, int64_t x_str
 // The largest singular value that the steps can make of values up to 1: they are refused beyond what the kernels' scales
 // have room for (X up to 3.5, the factor b A + c A^2 up to 30).  With l = s^2 a step takes s to s (a + b l + c l^2); both that
 // and the factor are largest at an end of 0 .. most^2 or where their slopes are zero.
-bool ortho_in_range(int64_t steps, const OrthoCoeffs &c) {
+bool ortho_in_range(int64_t steps, const OrthoCoeffs &c, double *largest) {
+    *largest = 1.0001;
     if (!std::isfinite(c.a) || !std::isfinite(c.b) || !std::isfinite(c.c)) return false;
     double most = 1.0001;
     for (int64_t s = 0; s < steps; ++s) {
@@ -226,31 +227,67 @@ bool ortho_in_range(int64_t steps, const OrthoCoeffs &c) {
             next = std::max(next, y);
         }
         most = 1.001 * next;
+        *largest = std::max(*largest, most);
     }
     return most <= 3.51;
 }
 
-template <int NT, typename T>
-int run_ortho_narrow(cdgrab_handle *h, const char *who, int64_t batch, OrthoIo<T> io, int64_t steps, const OrthoCoeffs &c) {
-    constexpr int64_t N = NT * 16;
-    // one workgroup per matrix while a matrix is short or there are enough of them (us of one launch -> three: 12 x 4000 46 -> 27, 30 x
-    // 1000 37 -> 27, 64 x 512 111 -> 73)
-    if (io.long_side <= 1024 / (NT * NT) * 2 || batch >= h->num_cu) {
-        hipLaunchKernelGGL((ortho_narrow<NT, T>), dim3((unsigned)batch), dim3(kOrthoThreads), 0, h->stream, io, (int)steps, c);
-        HIP_TRY(h, hipGetLastError());
-        return CDGRAB_OK;
+// Steps that one Gram matrix serves.  A step takes an eigenvalue l of it to l q(l)^2, q = a + b l + c l^2, and what rounding has added
+// to the matrix grows by the slope of that, q (a + 3 b l + 5 c l^2), at the most: 2^-52 of the trace stays below 2^-30, which is nothing
+// beside 1 and beside the rounding of the results.  (Default coefficients: a^2 = 11.9 at l = 0, six steps.)
+int64_t ortho_gram_steps(const OrthoCoeffs &c, double largest) {
+    double slope = 1.0;
+    for (int q = 0; q <= 64; ++q) {
+        const double l = largest * largest * q / 64;
+        slope = std::max(slope, std::abs((c.a + c.b * l + c.c * l * l) * (c.a + 3.0 * c.b * l + 5.0 * c.c * l * l)));
     }
-    const int64_t fill = std::max<int64_t>(1, h->num_cu / batch);
-    const int64_t per = round_up((io.long_side + std::min<int64_t>(fill, 128) - 1) / std::min<int64_t>(fill, 128), 256);
-    const int chunks = (int)((io.long_side + per - 1) / per);
-    double *parts = nullptr;
-    const int rc = layer_room(h, who, batch * (chunks + 1) * N * N, &parts);
-    if (rc) return rc;
-    double *P = parts + batch * chunks * N * N;
+    return slope > 1.25 ? std::max<int64_t>(1, (int64_t)(22.0 / std::log2(slope))) : 64;
+}
+
+// `chunks` of `per` columns with their sums in `parts`; none: one workgroup per matrix.
+template <int NT, typename T>
+void launch_ortho_narrow(cdgrab_handle *h, int64_t batch, const OrthoIo<T> &io, int64_t steps, int first, const OrthoCoeffs &c, int chunks,
+                         int64_t per, double *parts) {
+    if (!parts) {
+        hipLaunchKernelGGL((ortho_narrow<NT, T>), dim3((unsigned)batch), dim3(kOrthoThreads), 0, h->stream, io, (int)steps, first, c);
+        return;
+    }
+    double *P = parts + batch * chunks * NT * NT * 256;
     hipLaunchKernelGGL((ortho_narrow_gram<NT, T>), dim3((unsigned)(batch * chunks)), dim3(kOrthoThreads), 0, h->stream, io, chunks, per, parts);
     hipLaunchKernelGGL((ortho_narrow_chain<NT>), dim3((unsigned)batch), dim3(kOrthoThreads), 0, h->stream, io.short_side, chunks, parts,
-                       (int)steps, c, P);
+                       (int)steps, first, c, P);
     hipLaunchKernelGGL((ortho_narrow_apply<NT, T>), dim3((unsigned)(batch * chunks)), dim3(kOrthoThreads), 0, h->stream, io, chunks, per, P);
+}
+
+template <int NT, typename T>
+int run_ortho_narrow(cdgrab_handle *h, const char *who, int64_t batch, const OrthoIo<T> &io, int64_t steps, const OrthoCoeffs &c) {
+    // one workgroup per matrix while a matrix is short or there are enough of them (us of one launch -> three: 12 x 4000 46 -> 27, 30 x
+    // 1000 37 -> 27, 64 x 512 111 -> 73)
+    const bool whole = io.long_side <= 1024 / (NT * NT) * 2 || batch >= h->num_cu;
+    const int64_t fill = whole ? 1 : std::min<int64_t>(std::max<int64_t>(1, h->num_cu / batch), 128);
+    const int64_t per = round_up((io.long_side + fill - 1) / fill, 256);
+    const int chunks = whole ? 0 : (int)((io.long_side + per - 1) / per);
+    // steps in stretches, of one Gram matrix each, with X in between
+    const int64_t stretches = std::max<int64_t>(1, (steps + c.per_gram - 1) / c.per_gram), cells = (int64_t)io.short_side * io.long_side;
+    const int64_t x_len = stretches > 1 ? batch * cells : 0, parts_len = whole ? 0 : batch * (chunks + 1) * NT * NT * 256;
+    double *X = nullptr;
+    if (x_len + parts_len > 0) {
+        const int rc = layer_room(h, who, x_len + parts_len, &X);
+        if (rc) return rc;
+    }
+    double *const parts = whole ? nullptr : X + x_len;
+    if (stretches == 1) {
+        launch_ortho_narrow<NT>(h, batch, io, steps, 1, c, chunks, per, parts);
+    } else {
+        const bool turn = io.m_i < io.m_j;
+        const int64_t x_i = turn ? 1 : io.long_side, x_j = turn ? io.short_side : 1;
+        const OrthoIo<double> between{X, X, nullptr, 0.f, x_i, x_j, cells, x_i, x_j, cells, io.short_side, io.long_side};
+        const uint32_t groups = (uint32_t)std::min((cells + 1023) / 1024, std::max<int64_t>(1, kMaxGroups / batch));
+        hipLaunchKernelGGL((ortho_doubles<T, false>), dim3((unsigned)(batch * groups)), dim3(256), 0, h->stream, io, groups, X);
+        for (int64_t s = 0; s < stretches; ++s)
+            launch_ortho_narrow<NT>(h, batch, between, steps * (s + 1) / stretches - steps * s / stretches, s == 0, c, chunks, per, parts);
+        hipLaunchKernelGGL((ortho_doubles<T, true>), dim3((unsigned)(batch * groups)), dim3(256), 0, h->stream, io, groups, X);
+    }
     HIP_TRY(h, hipGetLastError());
     return CDGRAB_OK;
 }
@@ -404,10 +441,12 @@ int run_ortho(cdgrab_handle *h, const char *who, int64_t batch, int64_t rows, in
 }
 
 int ortho_coeffs(cdgrab_handle *h, const char *who, int64_t steps, const double *coeffs, OrthoCoeffs *c) {
-    *c = coeffs ? OrthoCoeffs{coeffs[0], coeffs[1], coeffs[2]} : OrthoCoeffs{3.4445, -4.775, 2.0315};
+    *c = coeffs ? OrthoCoeffs{coeffs[0], coeffs[1], coeffs[2], 1} : OrthoCoeffs{3.4445, -4.775, 2.0315, 1};
     if (steps < 0 || steps > 64) return fail(h, CDGRAB_EINVAL, "%s: steps=%lld (0 .. 64)", who, (long long)steps);
-    if (!ortho_in_range(steps, *c))
+    double largest = 0.0;
+    if (!ortho_in_range(steps, *c, &largest))
         return fail(h, CDGRAB_EINVAL, "%s: with coefficients %g %g %g the steps can take a singular value beyond 3.5", who, c->a, c->b, c->c);
+    c->per_gram = ortho_gram_steps(*c, largest);
     return CDGRAB_OK;
 }
 

@@ -8,6 +8,9 @@
 //   - short side up to kOrthoNarrow: X_K = P_K X_0 with P_K a polynomial in A_0 = X_0 X_0^T.  One pass over the matrix for A_0 in
 //     double, the recurrence on matrices of the short side (all of which commute), one pass for the product: bytes of the matrix
 //     twice.  (In fp32 this form loses too much: the small eigenvalues of A_0 are the squares of the singular values.)
+//     Where the matrix lacks rank A_0 has eigenvalues that are rounding, of either sign, and the recurrence makes them grow by a^2 per
+//     step; for a negative one near -1 the polynomial has no bound.  So one A_0 serves as many steps as keep them small
+//     (ortho_gram_steps: six with the default coefficients); then X is made, in double, and its Gram matrix anew.
 //   - else the products as they stand.  Factors are held as the sum of two fp16 (22 bits), and of the four products of the
 //     parts the three larger are taken: errors as of fp32 products (simulated on matrices of 256 .. 2048: 1.0 to 1.1 times), at a
 //     third of the fp16 MFMA rate, five times the fp32 MFMA's.  fp16 has the digits but not the range: the norm bounds every
@@ -21,6 +24,9 @@ namespace cdgrab {
 
 typedef double f64x4 __attribute__((ext_vector_type(4)));
 
+template <typename T> __device__ __forceinline__ double ortho_double(T v) { return (double)(float)v; }
+__device__ __forceinline__ double ortho_double(double v) { return v; }
+
 // Where a matrix's elements lie and where results go: element (i, j), i along the short side, at i * si + j * sj.
 // `sub`: instead of storing O, subtract rate * O from the fp32 array of the same strides (an optimiser's step).
 template <typename T>
@@ -31,11 +37,12 @@ struct OrthoIo {
     float rate;
     int64_t m_i, m_j, m_matrix, o_i, o_j, o_matrix;
     int short_side, long_side;
-    __device__ __forceinline__ double at(int64_t b, int i, int64_t j) const { return (double)(float)M[b * m_matrix + i * m_i + j * m_j]; }
-    __device__ __forceinline__ void put(int64_t b, int i, int64_t j, float v) const {
+    __device__ __forceinline__ double at(int64_t b, int i, int64_t j) const { return ortho_double(M[b * m_matrix + i * m_i + j * m_j]); }
+    __device__ __forceinline__ void put(int64_t b, int i, int64_t j, double v) const {  // (rounded to fp32, unless O is of doubles)
         const int64_t p = b * o_matrix + i * o_i + j * o_j;
-        if (sub) sub[p] = sub[p] - rate * v;
-        else O[p] = (T)v;
+        if (sub) sub[p] = sub[p] - rate * (float)v;
+        else if constexpr (sizeof(T) == 8) O[p] = v;
+        else O[p] = (T)(float)v;
     }
     // Eight results side by side in memory, from element p on, of which the first n are there.
     __device__ __forceinline__ void put8(int64_t p, const float (&v)[8], int n) const {
@@ -55,7 +62,10 @@ struct OrthoIo {
     }
 };
 
-struct OrthoCoeffs { double a, b, c; };
+struct OrthoCoeffs {
+    double a, b, c;
+    int64_t per_gram;  // steps that one Gram matrix serves
+};
 
 // 1 / sqrt of a sum of squares: zero of zero (such a matrix stays as it is), NaN of infinity.
 __device__ __forceinline__ double ortho_root(double t) { return t == 0.0 ? 0.0 : 1.0 / sqrt(t) + (t - t); }
@@ -125,7 +135,8 @@ struct OrthoTiles {
 };
 
 // P (in LDS) from the Gram matrix of M in A (in LDS), entries beyond the short side zero:
-//   A <- A / trace(A), P <- I / sqrt(trace); steps times: Q = a I + b A + c A^2, P <- Q P, A <- Q A Q.
+//   A <- A / trace(A), P <- I / sqrt(trace) (not for an X that steps have made: `first`); steps times:
+//   Q = a I + b A + c A^2, P <- Q P, A <- Q A Q.
 // Everything commutes and is symmetric, so that the order of factors does not matter.  A single tile stays in one wavefront's
 // registers; more go through LDS, three rounds per step.
 template <int NT>
@@ -134,7 +145,7 @@ struct OrthoChain {
     double A[Tiles::LEN], Q[Tiles::LEN], P[Tiles::LEN];
     double trace;
 
-    __device__ __forceinline__ void run(int n, int steps, OrthoCoeffs c) {
+    __device__ __forceinline__ void run(int n, int steps, int first, OrthoCoeffs c) {
         const Tiles tiles;
         __syncthreads();
         if (threadIdx.x < 64) {
@@ -143,7 +154,7 @@ struct OrthoChain {
             if (threadIdx.x == 0) trace = t;
         }
         __syncthreads();
-        const double t = trace, inv = t == 0.0 ? 0.0 : 1.0 / t;
+        const double t = first ? trace : 1.0, inv = t == 0.0 ? 0.0 : 1.0 / t;
         f64x4 a = tiles.load(A), p = tiles.diagonal(ortho_root(t), n);
         const f64x4 one = tiles.diagonal(c.a, NT * 16);
 #pragma unroll
@@ -217,7 +228,7 @@ __device__ __forceinline__ void ortho_gram(const OrthoIo<T> &io, int64_t b, int6
             double x[NT];
 #pragma unroll
             for (int t = 0; t < NT; ++t)
-                x[t] = t * 16 + r < io.short_side && j + u * 4 * WAVES < j1 ? (double)(float)raw[u][t] : 0.0;
+                x[t] = t * 16 + r < io.short_side && j + u * 4 * WAVES < j1 ? ortho_double(raw[u][t]) : 0.0;
             int at = 0;
 #pragma unroll
             for (int ti = 0; ti < NT; ++ti)
@@ -249,7 +260,8 @@ __device__ __forceinline__ void ortho_gram(const OrthoIo<T> &io, int64_t b, int6
         }
 }
 
-// O = P X for columns j0 .. j1 - 1, in double (P's large entries cancel): a wavefront takes sixteen columns at a time.
+// O = P X for columns j0 .. j1 - 1, in double (P's large entries cancel): a wavefront takes sixteen columns at a time, and has
+// read them before it writes them (O may be M).
 template <int NT, typename T>
 __device__ __forceinline__ void ortho_apply(const OrthoIo<T> &io, int64_t b, int64_t j0, int64_t j1, const double *P) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, k = lane >> 4;
@@ -272,14 +284,14 @@ __device__ __forceinline__ void ortho_apply(const OrthoIo<T> &io, int64_t b, int
                 for (int v = 0; v < 4; v += 2) {
                     const double *p = P + (t * NT + ti) * 256 + v * 64 + lane;
                     const bool here = t * 16 + 4 * v + k < io.short_side, next = t * 16 + 4 * v + 4 + k < io.short_side;
-                    even = __builtin_amdgcn_mfma_f64_16x16x4f64(p[0], here ? (double)(float)raw[t][v] : 0.0, even, 0, 0, 0);
-                    odd = __builtin_amdgcn_mfma_f64_16x16x4f64(p[64], next ? (double)(float)raw[t][v + 1] : 0.0, odd, 0, 0, 0);
+                    even = __builtin_amdgcn_mfma_f64_16x16x4f64(p[0], here ? ortho_double(raw[t][v]) : 0.0, even, 0, 0, 0);
+                    odd = __builtin_amdgcn_mfma_f64_16x16x4f64(p[64], next ? ortho_double(raw[t][v + 1]) : 0.0, odd, 0, 0, 0);
                 }
             const f64x4 sum = even + odd;
 #pragma unroll
             for (int v = 0; v < 4; ++v) {
                 const int i = ti * 16 + 4 * v + k;
-                if (i < io.short_side && j < j1) io.put(b, i, j, (float)sum[v]);
+                if (i < io.short_side && j < j1) io.put(b, i, j, sum[v]);
             }
         }
     }
@@ -287,7 +299,7 @@ __device__ __forceinline__ void ortho_apply(const OrthoIo<T> &io, int64_t b, int
 
 // One workgroup per matrix.
 template <int NT, typename T>
-__global__ __launch_bounds__(kOrthoThreads) void ortho_narrow(OrthoIo<T> io, int steps, OrthoCoeffs c)
+__global__ __launch_bounds__(kOrthoThreads) void ortho_narrow(OrthoIo<T> io, int steps, int first, OrthoCoeffs c)
 {
     __shared__ OrthoChain<NT> s;
     __shared__ double lds[kOrthoThreads * 4];
@@ -296,7 +308,7 @@ __global__ __launch_bounds__(kOrthoThreads) void ortho_narrow(OrthoIo<T> io, int
         s.A[OrthoTiles<NT>::at(i, j)] = v;
         s.A[OrthoTiles<NT>::at(j, i)] = v;
     });
-    s.run(io.short_side, steps, c);
+    s.run(io.short_side, steps, first, c);
     ortho_apply<NT>(io, b, 0, io.long_side, s.P);
 }
 
@@ -312,7 +324,7 @@ __global__ __launch_bounds__(kOrthoThreads) void ortho_narrow_gram(OrthoIo<T> io
 }
 template <int NT>
 __global__ __launch_bounds__(kOrthoThreads) void ortho_narrow_chain(int n, int chunks, const double *__restrict__ parts, int steps,
-                                                                    OrthoCoeffs c, double *__restrict__ out)
+                                                                    int first, OrthoCoeffs c, double *__restrict__ out)
 {
     __shared__ OrthoChain<NT> s;
     typedef OrthoTiles<NT> Tiles;
@@ -327,7 +339,7 @@ __global__ __launch_bounds__(kOrthoThreads) void ortho_narrow_chain(int n, int c
         const int i = ti * 16 + (q % 256 / 64) * 4 + q % 64 / 16, j = tj * 16 + q % 16;
         if (ti < tj) s.A[Tiles::at(j, i)] = sum;
     }
-    s.run(n, steps, c);
+    s.run(n, steps, first, c);
     for (int q = threadIdx.x; q < Tiles::LEN; q += kOrthoThreads) out[(int64_t)blockIdx.x * Tiles::LEN + q] = s.P[q];
 }
 template <int NT, typename T>
@@ -338,6 +350,21 @@ __global__ __launch_bounds__(kOrthoThreads) void ortho_narrow_apply(OrthoIo<T> i
     for (int q = threadIdx.x; q < OrthoTiles<NT>::LEN; q += kOrthoThreads) p[q] = P[b * OrthoTiles<NT>::LEN + q];
     __syncthreads();
     ortho_apply<NT>(io, b, c * per, (c + 1) * per < io.long_side ? (c + 1) * per : io.long_side, p);
+}
+
+// More steps than one Gram matrix serves: X between stretches of steps, [matrix] and as the caller's rows lie, dense.  OUT: from X
+// to where the results go.
+template <typename T, bool OUT>
+__global__ __launch_bounds__(256) void ortho_doubles(OrthoIo<T> io, uint32_t groups, double *__restrict__ X)
+{
+    const int64_t b = blockIdx.x / groups, cells = (int64_t)io.short_side * io.long_side;
+    const bool turn = (OUT ? io.o_i : io.m_i) < (OUT ? io.o_j : io.m_j);
+    for (int64_t q = (blockIdx.x - b * groups) * 256 + threadIdx.x; q < cells; q += (int64_t)groups * 256) {
+        const int i = (int)(turn ? q % io.short_side : q / io.long_side);
+        const int64_t j = turn ? q / io.short_side : q % io.long_side;
+        if constexpr (OUT) io.put(b, i, j, X[b * cells + q]);
+        else X[b * cells + q] = io.at(b, i, j);
+    }
 }
 
 // ---- longer sides: products of pairs of fp16 --------------------------------------------------------------------------------
@@ -909,7 +936,7 @@ __global__ __launch_bounds__(256) void ortho_scaled(OrthoIo<T> io, const double 
     for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < cells; q += (int64_t)gridDim.x * 256) {
         const int i = (int)(turn ? q % io.short_side : q / io.long_side);
         const int64_t j = turn ? q / io.short_side : q % io.long_side;
-        io.put(b, i, j, (float)(io.at(b, i, j) * norm));
+        io.put(b, i, j, io.at(b, i, j) * norm);
     }
 }
 
