@@ -421,7 +421,9 @@ int cdgrab_pergrad_linear(cdgrab_handle *h, const cdgrab_token_rows *t, int64_t 
  *   M, O: `batch` matrices [rows][cols] of `type` dev, m_stride / o_stride elements from row to row, m_matrix / o_matrix from
  *   matrix to matrix (any value if batch is 1); coeffs: {a, b, c} host, or NULL: 3.4445, -4.775, 2.0315
  *   (about 0.7 .. 1.2 after five steps, from 0.01 of the norm on).
- * Products with the error of fp32 ones whatever the type, or better; the result is rounded once.  A matrix of zeros stays
+ * Products with the error of fp32 ones whatever the type, or better, for elements of at least 2^-27 of the matrix's norm;
+ * smaller ones enter with an error of about 2^-49 of the norm (nothing of this on shorter sides up to 32, whose products are in
+ * double).  The result is rounded once.  A matrix of zeros stays
  * zero, one with an element that is not finite becomes NaN.  Coefficients under which a singular value could pass 3.5
  * within the steps are refused.  Like the calls above it may be captured once it has run with the same sizes.
  * Errors: EINVAL (sizes, a shorter side > 16384, a side > 2^20, more than 2^32 elements, a batch > 2^21, type, steps < 0

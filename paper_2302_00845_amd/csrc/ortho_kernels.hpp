@@ -14,8 +14,10 @@
 //   - else the products as they stand.  Factors are held as the sum of two fp16 (22 bits), and of the four products of the
 //     parts the three larger are taken: errors as of fp32 products (simulated on matrices of 256 .. 2048: 1.0 to 1.1 times), at a
 //     third of the fp16 MFMA rate, five times the fp32 MFMA's.  fp16 has the digits but not the range: the norm bounds every
-//     element, and a fixed power of two in front keeps the parts normal.  A and A^2 are symmetric: half of their tiles are
-//     computed.
+//     element, a fixed power of two in front uses the range, and the small part is held kOrthoLift times as large, so that it has its
+//     eleven bits as long as the large part has.  Elements of X from 2^-27 of the norm on have 22 bits, smaller ones are off by
+//     about 2^-49 of the norm (with the small part as it is: from 2^-16 on, and by 2^-38; rows 1e-7 of the others
+//     came out half a percent off).  A and A^2 are symmetric: half of their tiles are computed.
 #pragma once
 #include "narrow_common.hpp"
 #include "mfma_tiles.hpp"
@@ -369,6 +371,7 @@ __global__ __launch_bounds__(256) void ortho_doubles(OrthoIo<T> io, uint32_t gro
 
 // ---- longer sides: products of pairs of fp16 --------------------------------------------------------------------------------
 constexpr float kOrthoScaleX = 8192.f, kOrthoScaleA = 2048.f;  // X up to 7.9, A and b A + c A^2 up to 31 (the host sees to it)
+constexpr float kOrthoLift = 2048.f;  // of the small parts
 constexpr int kOrthoSums = 64;  // sums of squares per matrix
 
 // Sums of squares of matrix b of `rows` x `cols` as it lies in memory; a wavefront takes every 256th row.
@@ -395,11 +398,12 @@ __global__ __launch_bounds__(256) void ortho_squares(const T *__restrict__ M, in
     if (threadIdx.x == 0) sums[blockIdx.x] = (part[0] + part[1]) + (part[2] + part[3]);
 }
 
-// v as a pair of fp16.
+// v as a pair of fp16, and what is made of pairs: a value, a product from its large and its small terms.
 __device__ __forceinline__ void ortho_split(float v, f16_t &hi, f16_t &lo) {
     hi = (f16_t)v;
-    lo = (f16_t)(v - (float)hi);
+    lo = (f16_t)((v - (float)hi) * kOrthoLift);
 }
+__device__ __forceinline__ float ortho_join(float large, float small) { return fmaf(small, 1.f / kOrthoLift, large); }
 
 // X_0 as pairs, [short][long] padded with zeros to sp x lp: 32 x 32 elements a workgroup, turned through LDS where the rows
 // of M are the long side.
@@ -515,8 +519,8 @@ __global__ __launch_bounds__(256 * QUADS, NS * T * 256 > 80 * 1024 ? 1 : 2) void
     stages /= QUADS;
     const f16_t *const left = p.L + b * p.l_matrix + (int64_t)tm * T * 2 * p.l_ld + begin * 64;
     const f16_t *const right = p.R + b * p.r_matrix + begin * 64 + (ACROSS ? (int64_t)tn * T * 2 : (int64_t)tn * T * 2 * p.r_ld);
-    // (the products with the small parts in sums of their own: as parts of one sum each would round it once more, 2468
-    // columns 3.3e-6 off instead of 1.9e-6)
+    // (the products with the small parts in sums of their own, of another scale; and as parts of one sum each would round it once
+    // more, 2468 columns 3.3e-6 off instead of 1.9e-6)
     f32x16 acc[MB][MB], low[MB][MB];
 #pragma unroll
     for (int i = 0; i < MB; ++i)
@@ -617,7 +621,7 @@ __global__ __launch_bounds__(256 * QUADS, NS * T * 256 > 80 * 1024 ? 1 : 2) void
         if (quad == 0)
 #pragma unroll
             for (int q = 0; q < 16; ++q)
-                to[(wm * 32 + 8 * (q >> 2) + 4 * (lane >> 5) + (q & 3)) * T + wn * 32 + (lane & 31)] = acc[0][0][q] + low[0][0][q];
+                to[(wm * 32 + 8 * (q >> 2) + 4 * (lane >> 5) + (q & 3)) * T + wn * 32 + (lane & 31)] = ortho_join(acc[0][0][q], low[0][0][q]);
         return;
     }
     // The tile goes out through LDS, half its rows at a time, so that every thread stores eight neighbours of a row; a tile
@@ -648,7 +652,7 @@ __global__ __launch_bounds__(256 * QUADS, NS * T * 256 > 80 * 1024 ? 1 : 2) void
 #pragma unroll
                     for (int q = 0; q < 16; ++q)
                         out[(i * 32 + 8 * (q >> 2) + 4 * (lane >> 5) + (q & 3)) * LD + wn * (T / 2) + j * 32 + (lane & 31)] =
-                            p.beta * (acc[i][j][q] + low[i][j][q]);
+                            p.beta * ortho_join(acc[i][j][q], low[i][j][q]);
         __syncthreads();
         // the values are read from LDS once more, along the other side
         const bool turn = WHAT == kOrthoLast && io.o_i < io.o_j;  // (the caller's rows are the long side)
@@ -663,7 +667,7 @@ __global__ __launch_bounds__(256 * QUADS, NS * T * 256 > 80 * 1024 ? 1 : 2) void
             for (int j = 0; j < 8; ++j) {
                 v[j] = out[r * LD + c + j];
                 if constexpr (WHAT != kOrthoGram) {
-                    v[j] = fmaf(p.alpha, (float)e_hi[half][u][j] + (float)e_lo[half][u][j], v[j]);
+                    v[j] = fmaf(p.alpha, ortho_join((float)e_hi[half][u][j], (float)e_lo[half][u][j]), v[j]);
                     if (again) out[r * LD + c + j] = v[j];
                 }
             }
@@ -842,7 +846,9 @@ __global__ __launch_bounds__(kOrthoSmallThreads) void ortho_small(OrthoIo<T> io,
             multiply(o);
         }
 #pragma unroll
-        for (int u = 0; u < PER; ++u) out.v[u] += low[u];
+        for (int u = 0; u < PER; ++u)
+#pragma unroll
+            for (int q = 0; q < 16; ++q) out.v[u][q] = ortho_join(out.v[u][q], low[u][q]);
         return out;
     };
     const auto put = [&](f16_t *mh, f16_t *ml, int stride, int i0, int j0, const Blocks &x) {
@@ -871,7 +877,7 @@ __global__ __launch_bounds__(kOrthoSmallThreads) void ortho_small(OrthoIo<T> io,
                 const int at = (i0 + row) * stride + j0 + 32 * u + 2 * q + quad;
                 const f16x4 hi = *reinterpret_cast<const f16x4 *>(mh + at), lo = *reinterpret_cast<const f16x4 *>(ml + at);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) x.v[u][q + e] = fmaf(alpha, (float)hi[e] + (float)lo[e], beta * x.v[u][q + e]);
+                for (int e = 0; e < 4; ++e) x.v[u][q + e] = fmaf(alpha, ortho_join((float)hi[e], (float)lo[e]), beta * x.v[u][q + e]);
             }
     };
     const int nb = sp / 32, units = nb * (lp / 32 / PER);
@@ -916,7 +922,7 @@ __global__ __launch_bounds__(kOrthoSmallThreads) void ortho_small(OrthoIo<T> io,
     for (int o = wave; o < outer; o += WAVES)
         for (int q = lane; q < inner; q += 64) {
             const int at = turn ? q * xs + o : o * xs + q;
-            const float v = ((float)Xh[at] + (float)Xl[at]) * (1.f / kOrthoScaleX);
+            const float v = ortho_join((float)Xh[at], (float)Xl[at]) * (1.f / kOrthoScaleX);
             const int64_t p = b * io.o_matrix + o * o_row + q;
             if (io.sub) io.sub[p] = io.sub[p] - io.rate * v;
             else io.O[p] = (T)v;
