@@ -1023,9 +1023,12 @@ void Epoch::set_block(int64_t p0, int64_t nb, const float *stage_base) {
     for (int j = rm.nb; j < kMaxBlockPairs; ++j) rm.off[2 * j] = rm.off[2 * j + 1] = 0;
 }
 
+int train_generate(void *vctx, int64_t first_pair, int64_t count, float *staging, void *);
+
 int Epoch::generate(int64_t first, int64_t count, float *stage_buf) {
     MARK(h, 1, kGen);
     const int grc = gen(gen_ctx, first, count, stage_buf, h->stream);
+    if (grc != 0 && gen == train_generate) return grc;  // (no caller's: it has said itself what is wrong)
     if (grc != 0)
         return fail(h, CDGRAB_EGEN, "generator callback returned %d at pair %lld", grc, (long long)first);
     return CDGRAB_OK;
@@ -1476,6 +1479,12 @@ int64_t train_chunk_pairs(const cdgrab_handle *h, int64_t m, int64_t n, int64_t 
     return std::min(base * k, pairs);
 }
 
+// The orthogonalised update of a step, or (without `launch`) its workspace.
+int train_orthogonal(TrainCtx *c, bool launch) {
+    return run_ortho<float>(c->h, "cdgrab_train_epoch_softmax_orthogonal", 1, c->in_dim + 1, c->classes, c->velocity, c->classes, 0,
+                            c->orth_steps, c->orth, nullptr, c->W, c->lr, c->classes, 0, launch);
+}
+
 // The steps j .. j_end - 1 of a chunk, a launch pair each.
 int train_step_launches(TrainCtx *c, int64_t j, int64_t j_end, int64_t k_first, float *staging) {
     cdgrab_handle *h = c->h;
@@ -1492,8 +1501,7 @@ int train_step_launches(TrainCtx *c, int64_t j, int64_t j_end, int64_t k_first, 
         if (c->perm_in) update(train_step_update<true>);
         else update(train_step_update<false>);
         if (c->orth_steps >= 0) {
-            const int rc = run_ortho<float>(h, "cdgrab_train_epoch_softmax_orthogonal", 1, c->in_dim + 1, c->classes, c->velocity,
-                                            c->classes, 0, c->orth_steps, c->orth, nullptr, c->W, c->lr, c->classes, 0);
+            const int rc = train_orthogonal(c, true);
             if (rc) return rc;
         }
     }
@@ -1545,7 +1553,7 @@ int train_blocks(TrainCtx *c, int64_t j, int64_t j_end, int64_t k_first, float *
 
 int train_generate(void *vctx, int64_t first_pair, int64_t count, float *staging, void *) {
     TrainCtx *c = static_cast<TrainCtx *>(vctx);
-    if (first_pair % c->m != 0 || count % c->m != 0) return 1;  // chunks are whole step pairs
+    if (first_pair % c->m != 0 || count % c->m != 0) return fail(c->h, CDGRAB_EGEN, "training epoch: a chunk is not whole step pairs");
     const int64_t k_first = first_pair / c->m, j = 2 * k_first, j_end = j + 2 * (count / c->m);
     return c->block_steps > 0 ? train_blocks(c, j, j_end, k_first, staging)
                               : train_step_launches(c, j, j_end, k_first, staging);
@@ -1574,6 +1582,8 @@ static int train_epoch_impl(cdgrab_handle *h, const char *who, int64_t m, int64_
     if (rc) return rc;
     TrainCtx ctx{h, m, n, in_dim, classes, (in_dim + 1) * classes, X, y, perm_in, W, velocity,
                  grads_out, loss_out, lr, momentum, block_steps, 0, 1, orth_steps, orth};
+    // (before anything is enqueued: a step whose update has no workspace would leave its velocity behind)
+    if (orth_steps >= 0 && (rc = train_orthogonal(&ctx, false))) return rc;
     if (block_steps > 0) {
         const int64_t blocks = (std::min(2 * (chunk / m), n) + block_steps - 1) / block_steps;  // of a chunk
         const int64_t blk = (block_steps * m + kTilePairs - 1) / kTilePairs;

@@ -260,7 +260,8 @@ void launch_ortho_narrow(cdgrab_handle *h, int64_t batch, const OrthoIo<T> &io, 
 }
 
 template <int NT, typename T>
-int run_ortho_narrow(cdgrab_handle *h, const char *who, int64_t batch, const OrthoIo<T> &io, int64_t steps, const OrthoCoeffs &c) {
+int run_ortho_narrow(cdgrab_handle *h, const char *who, int64_t batch, const OrthoIo<T> &io, int64_t steps, const OrthoCoeffs &c,
+                     bool launch) {
     // one workgroup per matrix while a matrix is short or there are enough of them (us of one launch -> three: 12 x 4000 46 -> 27, 30 x
     // 1000 37 -> 27, 64 x 512 111 -> 73)
     const bool whole = io.long_side <= 1024 / (NT * NT) * 2 || batch >= h->num_cu;
@@ -275,6 +276,7 @@ int run_ortho_narrow(cdgrab_handle *h, const char *who, int64_t batch, const Ort
         const int rc = layer_room(h, who, x_len + parts_len, &X);
         if (rc) return rc;
     }
+    if (!launch) return CDGRAB_OK;
     double *const parts = whole ? nullptr : X + x_len;
     if (stretches == 1) {
         launch_ortho_narrow<NT>(h, batch, io, steps, 1, c, chunks, per, parts);
@@ -293,7 +295,7 @@ int run_ortho_narrow(cdgrab_handle *h, const char *who, int64_t batch, const Ort
 }
 
 template <int TILE, typename T>
-int run_ortho_products(cdgrab_handle *h, const char *who, int64_t batch, OrthoIo<T> io, int64_t steps, const OrthoCoeffs &c) {
+int run_ortho_products(cdgrab_handle *h, const char *who, int64_t batch, OrthoIo<T> io, int64_t steps, const OrthoCoeffs &c, bool launch) {
     const int64_t sp = round_up(io.short_side, TILE), lp = round_up(io.long_side, TILE);
     const int64_t x_len = 2 * sp * lp, a_len = 2 * sp * sp, per_matrix = 2 * x_len + 2 * a_len + kOrthoSums * 4;  // fp16 elements
     const int64_t tm = sp / TILE, tn = lp / TILE;
@@ -307,7 +309,7 @@ int run_ortho_products(cdgrab_handle *h, const char *who, int64_t batch, OrthoIo
     const int64_t shares_len = shares > 1 ? at_once * half * shares * TILE * TILE * 2 : 0;  // (in fp16 elements)
     f16_t *ws = nullptr;
     const int rc = layer_room(h, who, at_once * per_matrix + shares_len, &ws);
-    if (rc) return rc;
+    if (rc || !launch) return rc;
     float *const parts = reinterpret_cast<float *>(ws + at_once * per_matrix);
     double *sums = reinterpret_cast<double *>(ws);
     f16_t *at = ws + at_once * kOrthoSums * 4;
@@ -394,23 +396,25 @@ struct OrthoSmall {
     }
 };
 
-// M and O (or `sub`) of `batch` matrices of rows x cols, `m_row` / `o_row` elements from row to row.
+// M and O (or `sub`) of `batch` matrices of rows x cols, `m_row` / `o_row` elements from row to row.  Without `launch`: the workspace
+// is made as large as such a call needs it, and nothing is enqueued.
 template <typename T>
 int run_ortho(cdgrab_handle *h, const char *who, int64_t batch, int64_t rows, int64_t cols, const T *M, int64_t m_row, int64_t m_matrix,
-              int64_t steps, const OrthoCoeffs &c, T *O, float *sub, float rate, int64_t o_row, int64_t o_matrix) {
+              int64_t steps, const OrthoCoeffs &c, T *O, float *sub, float rate, int64_t o_row, int64_t o_matrix,
+              bool launch = true) {
     const bool wide = rows <= cols;
     const OrthoIo<T> io{M, O, sub, rate, wide ? m_row : 1, wide ? 1 : m_row, m_matrix, wide ? o_row : 1, wide ? 1 : o_row, o_matrix,
                         (int)std::min(rows, cols), (int)std::max(rows, cols)};
-    if (io.short_side <= 16) return run_ortho_narrow<1>(h, who, batch, io, steps, c);
-    if (io.short_side <= 32) return run_ortho_narrow<2>(h, who, batch, io, steps, c);
+    if (io.short_side <= 16) return run_ortho_narrow<1>(h, who, batch, io, steps, c, launch);
+    if (io.short_side <= 32) return run_ortho_narrow<2>(h, who, batch, io, steps, c, launch);
     if (io.short_side <= kOrthoNarrow && (steps == 0 || !OrthoSmall(io.short_side, io.long_side).fits))
-        return run_ortho_narrow<4>(h, who, batch, io, steps, c);
+        return run_ortho_narrow<4>(h, who, batch, io, steps, c, launch);
     if (steps == 0) {
         for (int64_t b0 = 0; b0 < batch; b0 += 32768) {
             const int64_t n = std::min<int64_t>(32768, batch - b0);
             double *sums = nullptr;
             const int rc = layer_room(h, who, n * kOrthoSums, &sums);
-            if (rc) return rc;
+            if (rc || !launch) return rc;
             OrthoIo<T> part = io;
             part.M += b0 * io.m_matrix;
             if (part.O) part.O += b0 * io.o_matrix;
@@ -425,6 +429,7 @@ int run_ortho(cdgrab_handle *h, const char *who, int64_t batch, int64_t rows, in
     }
     const OrthoSmall small(io.short_side, io.long_side);
     if (small.fits) {
+        if (!launch) return CDGRAB_OK;
         const auto go = [&](auto kernel) {
             hipLaunchKernelGGL(kernel, dim3((unsigned)batch), dim3(kOrthoSmallThreads), 0, h->stream, io, (int)small.sp, (int)small.lp,
                                (int)steps, c);
@@ -436,8 +441,8 @@ int run_ortho(cdgrab_handle *h, const char *who, int64_t batch, int64_t rows, in
         return CDGRAB_OK;
     }
     const int64_t s = io.short_side, tiles = batch * ((s + 127) / 128) * ((s + 127) / 128 + 1) / 2;
-    if (tiles >= h->num_cu / 2) return run_ortho_products<128>(h, who, batch, io, steps, c);
-    return run_ortho_products<64>(h, who, batch, io, steps, c);
+    if (tiles >= h->num_cu / 2) return run_ortho_products<128>(h, who, batch, io, steps, c, launch);
+    return run_ortho_products<64>(h, who, batch, io, steps, c, launch);
 }
 
 int ortho_coeffs(cdgrab_handle *h, const char *who, int64_t steps, const double *coeffs, OrthoCoeffs *c) {
