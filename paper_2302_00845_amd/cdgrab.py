@@ -156,8 +156,32 @@ def _ptr(t: Optional[torch.Tensor], dtype, shape, name, device) -> Optional[int]
     return t.data_ptr()
 
 
+# The current stream's number (torch.cuda.current_stream makes an object of it: 2 us, a third of a small call).
+_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _empty(h, shape, dtype) -> torch.Tensor:
+    """An output of a call.  It is allocated on the handle's stream, where the call writes it: memory that the current
+    stream has let go of may still be in use there.  The current stream is taken to be where it will be read."""
+    if h.stream is None or h.stream_number == _current_stream(h.device_index):
+        return torch.empty(shape, dtype=dtype, device=h.device)
+    with torch.cuda.stream(h.stream):
+        out = torch.empty(shape, dtype=dtype, device=h.device)
+    out.record_stream(torch.cuda.current_stream(h.device))
+    return out
+
+
+def _empty_like(h, t: torch.Tensor) -> torch.Tensor:
+    if h.stream is None or h.stream_number == _current_stream(h.device_index):
+        return torch.empty_like(t, memory_format=torch.contiguous_format)
+    return _empty(h, t.shape, t.dtype)
+
+
 class Handle:
-    """Owns a cdgrab_handle (workspace + stream binding) on one GPU."""
+    """Owns a cdgrab_handle (workspace + stream binding) on one GPU.
+
+    Calls run on the handle's stream.  Where that is not the current stream, the caller orders the inputs before the call and
+    what reads the outputs after it, as between any two streams."""
 
     def __init__(self, device: int = 0, block_pairs: int = 0, timing: int = 0,
                  pass1_groups: int = 0, stream: Optional[torch.cuda.Stream] = None,
@@ -167,6 +191,7 @@ class Handle:
         if stream is None:
             stream = torch.cuda.current_stream(self.device)
         self.stream = stream
+        self.stream_number, self.device_index = stream.cuda_stream, device
         opt = _Options(device=device, block_pairs=block_pairs, stream=stream.cuda_stream,
                        timing=timing, pass1_groups=pass1_groups,
                        apply_mode=apply_mode, gram_mode=gram_mode, apply_groups=apply_groups)
@@ -203,7 +228,7 @@ def cdgrab_pergrad(h: Handle, X: torch.Tensor, y: torch.Tensor, W: torch.Tensor,
     N, in_dim = X.shape
     classes = W.shape[1]
     if G_out is None:
-        G_out = torch.empty((N, (in_dim + 1) * classes), dtype=torch.float32, device=h.device)
+        G_out = _empty(h, (N, (in_dim + 1) * classes), torch.float32)
     h._check(h._lib.cdgrab_pergrad(
         h._h, N, in_dim, classes,
         _ptr(X, torch.float32, (N, in_dim), "X", h.device),
@@ -227,11 +252,11 @@ def cdgrab_balance_epoch(h: Handle, m: int, n: int, d: int,
     """
     dev = h.device
     half = n // 2 if n >= 0 else 0
-    signs = torch.empty((max(m, 0), max(half, 0)), dtype=torch.int8, device=dev)
-    perm = torch.empty((max(m, 0), max(n, 0)), dtype=torch.int32, device=dev)
-    r32 = torch.empty((max(d, 0),), dtype=torch.float32, device=dev) if want_r32 else None
-    r64 = torch.empty((max(d, 0),), dtype=torch.float64, device=dev) if want_r64 else None
-    dots = torch.empty((max(m, 0), max(half, 0)), dtype=torch.float64, device=dev) if want_dots else None
+    signs = _empty(h, (max(m, 0), max(half, 0)), torch.int8)
+    perm = _empty(h, (max(m, 0), max(n, 0)), torch.int32)
+    r32 = _empty(h, (max(d, 0),), torch.float32) if want_r32 else None
+    r64 = _empty(h, (max(d, 0),), torch.float64) if want_r64 else None
+    dots = _empty(h, (max(m, 0), max(half, 0)), torch.float64) if want_dots else None
     gptr = _ptr(grads, torch.float32, (m, n, d), "grads", dev) if grads is not None else None
     gen_ptr = ctypes.cast(gen, ctypes.c_void_p) if gen is not None else None
     h._check(h._lib.cdgrab_balance_epoch(
@@ -266,7 +291,7 @@ def cdgrab_balance_epoch_static(h: Handle, grads: torch.Tensor, out: dict,
 def cdgrab_reorder(h: Handle, signs: torch.Tensor, perm_in: Optional[torch.Tensor] = None) -> torch.Tensor:
     """General reorder from per-example +-1 signs [m][n] (int8)."""
     m, n = signs.shape
-    out = torch.empty((m, n), dtype=torch.int32, device=h.device)
+    out = _empty(h, (m, n), torch.int32)
     h._check(h._lib.cdgrab_reorder(
         h._h, m, n, _ptr(signs, torch.int8, (m, n), "signs", h.device),
         _ptr(perm_in, torch.int32, (m, n), "perm_in", h.device), out.data_ptr()))
@@ -277,7 +302,7 @@ def cdgrab_herding_bound(h: Handle, z: torch.Tensor, perm: Optional[torch.Tensor
     """Parallel herding objective of z[m][n][d] (indexed by example id) visited in
     the orders perm[m][n]; returns a one-element float64 GPU tensor."""
     m, n, d = z.shape
-    out = torch.empty((1,), dtype=torch.float64, device=h.device)
+    out = _empty(h, (1,), torch.float64)
     h._check(h._lib.cdgrab_herding_bound(
         h._h, m, n, d, _ptr(z, torch.float32, (m, n, d), "z", h.device),
         _ptr(perm, torch.int32, (m, n), "perm", h.device), out.data_ptr()))
@@ -295,10 +320,10 @@ def cdgrab_train_epoch_softmax(h: Handle, X: torch.Tensor, y: torch.Tensor, W: t
     classes = W.shape[1]
     d = (in_dim + 1) * classes
     dev = h.device
-    signs = torch.empty((m, n // 2), dtype=torch.int8, device=dev)
-    perm = torch.empty((m, n), dtype=torch.int32, device=dev)
-    grads = torch.empty((m, n, d), dtype=torch.float32, device=dev) if want_grads else None
-    loss = torch.empty((m, n), dtype=torch.float32, device=dev) if want_loss else None
+    signs = _empty(h, (m, n // 2), torch.int8)
+    perm = _empty(h, (m, n), torch.int32)
+    grads = _empty(h, (m, n, d), torch.float32) if want_grads else None
+    loss = _empty(h, (m, n), torch.float32) if want_loss else None
     h._check(h._lib.cdgrab_train_epoch_softmax(
         h._h, m, n, in_dim, classes,
         _ptr(X, torch.float32, (m, n, in_dim), "X", dev), _ptr(y, torch.int32, (m, n), "y", dev),
@@ -321,8 +346,8 @@ def cdgrab_train_softmax(h: Handle, X: torch.Tensor, y: torch.Tensor, W: torch.T
     classes = W.shape[1]
     d = (in_dim + 1) * classes
     dev = h.device
-    signs = torch.empty((m, n // 2), dtype=torch.int8, device=dev)
-    loss = torch.empty((epochs, m, n), dtype=torch.float32, device=dev) if want_loss else None
+    signs = _empty(h, (m, n // 2), torch.int8)
+    loss = _empty(h, (epochs, m, n), torch.float32) if want_loss else None
     h._check(h._lib.cdgrab_train_softmax(
         h._h, m, n, in_dim, classes,
         _ptr(X, torch.float32, (m, n, in_dim), "X", dev), _ptr(y, torch.int32, (m, n), "y", dev),
@@ -337,8 +362,8 @@ def cdgrab_balance_epoch_independent(h: Handle, grads: torch.Tensor,
                                      perm_in: Optional[torch.Tensor] = None) -> dict:
     """ID-GraB (PairBal): m independent one-worker walks over grads[m][n][d]."""
     m, n, d = grads.shape
-    signs = torch.empty((m, n // 2), dtype=torch.int8, device=h.device)
-    perm = torch.empty((m, n), dtype=torch.int32, device=h.device)
+    signs = _empty(h, (m, n // 2), torch.int8)
+    perm = _empty(h, (m, n), torch.int32)
     h._check(h._lib.cdgrab_balance_epoch_independent(
         h._h, m, n, d, _ptr(grads, torch.float32, (m, n, d), "grads", h.device),
         _ptr(perm_in, torch.int32, (m, n), "perm_in", h.device), signs.data_ptr(), perm.data_ptr()))
@@ -351,10 +376,10 @@ def cdgrab_balance_epoch_stale_mean(h: Handle, grads: torch.Tensor,
     """Centralized GraB balancing of grads[n][d] centred by a stale mean."""
     n, d = grads.shape
     dev = h.device
-    signs = torch.empty((n,), dtype=torch.int8, device=dev)
-    perm = torch.empty((n,), dtype=torch.int32, device=dev)
-    mean = torch.empty((d,), dtype=torch.float32, device=dev)
-    r64 = torch.empty((d,), dtype=torch.float64, device=dev)
+    signs = _empty(h, (n,), torch.int8)
+    perm = _empty(h, (n,), torch.int32)
+    mean = _empty(h, (d,), torch.float32)
+    r64 = _empty(h, (d,), torch.float64)
     h._check(h._lib.cdgrab_balance_epoch_stale_mean(
         h._h, n, d, _ptr(grads, torch.float32, (n, d), "grads", dev),
         _ptr(stale_mean, torch.float32, (d,), "stale_mean", dev),
@@ -368,10 +393,10 @@ def cdgrab_balance_epoch_randomized(h: Handle, grads: torch.Tensor, uniforms: to
     """cdgrab_balance_epoch with the randomized sign rule; uniforms[m][n/2] in [0,1)."""
     m, n, d = grads.shape
     dev = h.device
-    signs = torch.empty((m, n // 2), dtype=torch.int8, device=dev)
-    perm = torch.empty((m, n), dtype=torch.int32, device=dev)
-    r64 = torch.empty((d,), dtype=torch.float64, device=dev)
-    dots = torch.empty((m, n // 2), dtype=torch.float64, device=dev)
+    signs = _empty(h, (m, n // 2), torch.int8)
+    perm = _empty(h, (m, n), torch.int32)
+    r64 = _empty(h, (d,), torch.float64)
+    dots = _empty(h, (m, n // 2), torch.float64)
     h._check(h._lib.cdgrab_balance_epoch_randomized(
         h._h, m, n, d, _ptr(grads, torch.float32, (m, n, d), "grads", dev),
         _ptr(uniforms, torch.float32, (m, n // 2), "uniforms", dev),
@@ -442,15 +467,15 @@ def _token_rows(X: torch.Tensor, rows: int, first, count, tokens: Optional[int],
                       _ptr(count, torch.int32, (examples,), "count", device))
 
 
-def _grad_rows(G_out: Optional[torch.Tensor], examples: int, d: int, device):
+def _grad_rows(h, G_out: Optional[torch.Tensor], examples: int, d: int):
     """(G, stride): [examples][d] fp32, a stretch of longer rows if given so."""
     if G_out is None:
-        return torch.empty((examples, d), dtype=torch.float32, device=device), d or 1
+        return _empty(h, (examples, d), torch.float32), d or 1
     if G_out.dtype != torch.float32:
         raise TypeError("G_out must be float32, got %s" % G_out.dtype)
     if tuple(G_out.shape) != (examples, d):
         raise ValueError("G_out must have shape %s, got %s" % ((examples, d), tuple(G_out.shape)))
-    _, _, _, stride = _rows(G_out, "G_out", device)
+    _, _, _, stride = _rows(G_out, "G_out", h.device)
     return G_out, stride
 
 
@@ -461,12 +486,14 @@ def cdgrab_layernorm(h: Handle, X: torch.Tensor, gain: Optional[torch.Tensor] = 
     dev = h.device
     px, rows, width, sx = _rows(X, "X", dev)
     if Y is None:
-        Y = torch.empty_like(X, memory_format=torch.contiguous_format)
+        Y = _empty_like(h, X)
         py, sy = Y.data_ptr(), width or 1
     else:
         py, _, _, sy = _rows(Y, "Y", dev, X)
-    h._check(h._lib.cdgrab_layernorm(h._h, rows, width, _ELEM[X.dtype], px, sx, _vector(gain, width, "gain", dev),
-                                     _vector(bias, width, "bias", dev), eps, py, sy))
+    rc = h._lib.cdgrab_layernorm(h._h, rows, width, _ELEM[X.dtype], px, sx, _vector(gain, width, "gain", dev),
+                                 _vector(bias, width, "bias", dev), eps, py, sy)
+    if rc:
+        h._check(rc)
     return Y
 
 
@@ -488,17 +515,19 @@ def cdgrab_pergrad_layernorm(h: Handle, X: torch.Tensor, dY: torch.Tensor, gain:
     if dX is not None:
         pd, _, _, sd = _rows(dX, "dX", dev, X)
     elif want_dx:
-        dX = torch.empty_like(X, memory_format=torch.contiguous_format)
+        dX = _empty_like(h, X)
         if first is not None or count is not None:
             with torch.cuda.stream(h.stream):  # before the call's kernels, wherever they run
                 dX.zero_()
         pd, sd = dX.data_ptr(), width or 1
     G, pg, sg = None, None, 0
     if G_out is not None or want_grads:
-        G, sg = _grad_rows(G_out, t.examples, (2 if with_bias else 1) * width, dev)
+        G, sg = _grad_rows(h, G_out, t.examples, (2 if with_bias else 1) * width)
         pg = G.data_ptr()
-    h._check(h._lib.cdgrab_pergrad_layernorm(h._h, ctypes.byref(t), width, _ELEM[X.dtype], px, sx, py, sy,
-                                             _vector(gain, width, "gain", dev), eps, pd, sd, 1 if with_bias else 0, pg, sg))
+    rc = h._lib.cdgrab_pergrad_layernorm(h._h, ctypes.byref(t), width, _ELEM[X.dtype], px, sx, py, sy,
+                                         _vector(gain, width, "gain", dev), eps, pd, sd, 1 if with_bias else 0, pg, sg)
+    if rc:
+        h._check(rc)
     return dX, G
 
 
@@ -513,9 +542,11 @@ def cdgrab_pergrad_linear(h: Handle, X: torch.Tensor, D: torch.Tensor, with_bias
     if D.dtype != X.dtype or D.shape[:-1] != X.shape[:-1]:
         raise ValueError("D must be %s of rows %s, got %s %s" % (X.dtype, tuple(X.shape[:-1]), D.dtype, tuple(D.shape)))
     t = _token_rows(X, rows, first, count, tokens, dev)
-    G, sg = _grad_rows(G_out, t.examples, (n_in + (1 if with_bias else 0)) * n_out, dev)
-    h._check(h._lib.cdgrab_pergrad_linear(h._h, ctypes.byref(t), n_in, n_out, _ELEM[X.dtype], px, sx, pd, sd,
-                                          1 if with_bias else 0, G.data_ptr(), sg))
+    G, sg = _grad_rows(h, G_out, t.examples, (n_in + (1 if with_bias else 0)) * n_out)
+    rc = h._lib.cdgrab_pergrad_linear(h._h, ctypes.byref(t), n_in, n_out, _ELEM[X.dtype], px, sx, pd, sd,
+                                      1 if with_bias else 0, G.data_ptr(), sg)
+    if rc:
+        h._check(rc)
     return G
 
 
@@ -533,7 +564,7 @@ def cdgrab_orthogonalize(h: Handle, M: torch.Tensor, steps: int = 5, coeffs=None
     if M.dim() not in (2, 3):
         raise ValueError("M must be [rows][cols] or [batch][rows][cols], got %s" % (tuple(M.shape),))
     if out is None:
-        out = torch.empty_like(M, memory_format=torch.contiguous_format)
+        out = _empty_like(h, M)
     elif out.dtype != M.dtype or out.shape != M.shape:
         raise ValueError("out must be %s %s, got %s %s" % (M.dtype, tuple(M.shape), out.dtype, tuple(out.shape)))
     if M.dtype not in _ELEM:
@@ -547,8 +578,10 @@ def cdgrab_orthogonalize(h: Handle, M: torch.Tensor, steps: int = 5, coeffs=None
         if cols > 1 and strides[-1] != 1:
             raise ValueError("%s: the elements of a row must lie side by side" % name)
         at.append((t.data_ptr(), strides[-2] if rows > 1 else cols, strides[0]))
-    h._check(h._lib.cdgrab_orthogonalize(h._h, M.shape[0] if M.dim() == 3 else 1, rows, cols, _ELEM[M.dtype], *at[0], steps,
-                                         _coeffs(coeffs), *at[1]))
+    rc = h._lib.cdgrab_orthogonalize(h._h, M.shape[0] if M.dim() == 3 else 1, rows, cols, _ELEM[M.dtype], *at[0], steps,
+                                     _coeffs(coeffs), *at[1])
+    if rc:
+        h._check(rc)
     return out
 
 
@@ -562,10 +595,10 @@ def cdgrab_train_epoch_softmax_orthogonal(h: Handle, X: torch.Tensor, y: torch.T
     classes = W.shape[1]
     d = (in_dim + 1) * classes
     dev = h.device
-    signs = torch.empty((m, n // 2), dtype=torch.int8, device=dev)
-    perm = torch.empty((m, n), dtype=torch.int32, device=dev)
-    grads = torch.empty((m, n, d), dtype=torch.float32, device=dev) if want_grads else None
-    loss = torch.empty((m, n), dtype=torch.float32, device=dev) if want_loss else None
+    signs = _empty(h, (m, n // 2), torch.int8)
+    perm = _empty(h, (m, n), torch.int32)
+    grads = _empty(h, (m, n, d), torch.float32) if want_grads else None
+    loss = _empty(h, (m, n), torch.float32) if want_loss else None
     h._check(h._lib.cdgrab_train_epoch_softmax_orthogonal(
         h._h, m, n, in_dim, classes,
         _ptr(X, torch.float32, (m, n, in_dim), "X", dev), _ptr(y, torch.int32, (m, n), "y", dev),
