@@ -380,7 +380,8 @@ typedef struct cdgrab_token_rows {
 /* Layer norm of every row:  Y = gain * (X - mean) / sqrt(var + eps) + bias, mean and variance
  * (over `width`, biased) of the row.
  *   X, Y [rows][width] of `type` dev; gain, bias [width] fp32 dev, or NULL: one, zero.
- * Statistics in fp32; a row with an element that is not finite becomes NaN.
+ * Statistics in fp32; a row with an element that is not finite becomes NaN, and so does one whose squared differences from
+ * the mean add up to more than 3.4e38 (elements beyond about 1e19).
  * Errors: EINVAL (sizes, width > 16384, type, eps < 0, null, strides, overlap), EHIP. */
 int cdgrab_layernorm(cdgrab_handle *h, int64_t rows, int64_t width, int32_t type, const void *X,
                      int64_t x_stride, const float *gain, const float *bias, float eps, void *Y,
@@ -391,7 +392,8 @@ int cdgrab_layernorm(cdgrab_handle *h, int64_t rows, int64_t width, int32_t type
  *     DX = (g - mean(g) - h mean(g h)) / sqrt(var + eps),
  *     G[e][c] = sum over the example's rows of DY[c] h[c]          (gain),
  *     G[e][width + c] = sum over the example's rows of DY[c]       (bias; only if with_bias).
- * One example that holds all rows gives the ordinary gradient of the batch.
+ * One example that holds all rows gives the ordinary gradient of the batch.  DX of a row that the forward pass makes
+ * NaN is NaN, and so is the gain's gradient of its examples.
  *   X (the forward pass's input), DY, DX [rows][width] of `type` dev, gain as there,
  *   G: row e at G + e * g_stride, fp32 dev.  DX or G may be NULL: not wanted.
  * Overlapping examples are allowed.

@@ -7,7 +7,8 @@
 // share it between the read and the write, sixteen bytes a thread and access, so that nothing is read twice; the backward
 // pass takes mean and deviation from the row it has to read anyway instead of from a forward pass's arrays.
 // Statistics and sums in fp32: the mean is taken first and corrected by the mean of what is left, so that a row far from
-// zero keeps its digits; results are rounded once, to the rows' type.
+// zero keeps its digits; results are rounded once, to the rows' type.  A row whose sum of squares is beyond fp32 becomes NaN: with
+// a deviation of infinity it would become the bias.
 #pragma once
 #include "layer_common.hpp"
 
@@ -120,7 +121,7 @@ __global__ __launch_bounds__(LANES > kNormThreads ? LANES : kNormThreads) void n
             }
         RowSums<LANES, 2>::take(s, lds);
         const float left = s[0] * inv_width, var = fmaxf(fmaf(-left, left, s[1] * inv_width), 0.f);
-        const float r = 1.f / sqrtf((s[1] != s[1] ? s[1] : var) + eps);  // (fmaxf drops a NaN)
+        const float r = 1.f / sqrtf(var + eps) + (s[1] - s[1]);  // (NaN of a sum that is not finite)
         if (row < rows)
 #pragma unroll
             for (int k = 0; k < K; ++k)
@@ -190,7 +191,7 @@ __global__ __launch_bounds__(LANES > kNormThreads ? LANES : kNormThreads) void n
                 }
             RowSums<LANES, 4>::take(s, lds);
             const float left = s[0] * inv_width, var = fmaxf(fmaf(-left, left, s[1] * inv_width), 0.f);
-            const float r = 1.f / sqrtf((s[1] != s[1] ? s[1] : var) + eps);
+            const float r = 1.f / sqrtf(var + eps) + (s[1] - s[1]);
             const float mean_g = s[2] * inv_width, mean_gh = r * fmaf(-left, s[2], s[3]) * inv_width;
 #pragma unroll
             for (int k = 0; k < K; ++k) {
