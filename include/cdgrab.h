@@ -409,8 +409,9 @@ int cdgrab_pergrad_layernorm(cdgrab_handle *h, const cdgrab_token_rows *t, int64
  * the layout of cdgrab_pergrad, which is this with one row per example and D = softmax - onehot.
  *   X [rows][in_dim], D [rows][out_dim] (gradient of the layer's output) of `type` dev,
  *   G: row e at G + e * g_stride, fp32 dev.
- * Products of bf16 and fp16 elements are exact, those of fp32 elements good to 2^-23; sums in fp32.  An infinite fp32
- * element (or one above 3.38e38) makes the sums it enters NaN.
+ * Products of bf16 and fp16 elements are exact, those of fp32 elements good to 2^-23 (below 2^-110 in size elements may lose
+ * digits); sums in fp32.  An infinite element makes the sums it enters infinite or NaN, and an fp32 element beyond 3.38e38
+ * may count as infinite.
  * Errors: EINVAL (sizes, in_dim or out_dim > 2^20, more than 2^32 elements per row, type, with_bias not 0 or 1,
  * null, strides, overlap), ENOMEM, EHIP. */
 int cdgrab_pergrad_linear(cdgrab_handle *h, const cdgrab_token_rows *t, int64_t in_dim, int64_t out_dim,
