@@ -52,13 +52,27 @@ struct OnDevice {
 
 int64_t elem_size(int32_t type) { return type == CDGRAB_F32 ? 4 : 2; }
 
-// Do na rows of wa bytes from a, sa bytes apart, and nb rows from b share a byte?  (Of unequal strides: could they?)
+// Do na rows of wa bytes from a, sa bytes apart, and nb rows from b share a byte?  (Of unequal strides: could they?  A single row
+// has the other array's.)
 bool rows_overlap(const void *a, int64_t na, int64_t wa, int64_t sa, const void *b, int64_t nb, int64_t wb, int64_t sb) {
     if (!a || !b || na < 1 || nb < 1) return false;
     if (!ranges_overlap(a, (na - 1) * sa + wa, b, (nb - 1) * sb + wb)) return false;
-    if (sa != sb || na == 1 || nb == 1) return true;
+    if (na == 1) sa = sb;
+    if (nb == 1) sb = sa;
+    if (sa != sb || (na == 1 && nb == 1)) return true;
     const int64_t off = (int64_t)(reinterpret_cast<intptr_t>(b) - reinterpret_cast<intptr_t>(a)), at = ((off % sa) + sa) % sa;
     return at < wa || at + wb > sa;
+}
+
+// The same of `batch` matrices of rows x width bytes each, s bytes from row to row and t from matrix to matrix: they share nothing if
+// their stretches do not, taken as rows, or if all their rows lie at whole multiples of s and these do not.
+bool matrices_overlap(int64_t batch, int64_t rows, int64_t width, const void *a, int64_t sa, int64_t ta, const void *b, int64_t sb,
+                      int64_t tb) {
+    const int64_t la = (rows - 1) * sa + width, lb = (rows - 1) * sb + width;  // of a matrix
+    if (!rows_overlap(a, batch, la, ta, b, batch, lb, tb)) return false;
+    if (batch == 1) return rows_overlap(a, rows, width, sa, b, rows, width, sb);
+    if (rows == 1 || ta % sa != 0 || tb % sb != 0) return true;
+    return rows_overlap(a, (batch - 1) * (ta / sa) + rows, width, sa, b, (batch - 1) * (tb / sb) + rows, width, sb);
 }
 
 bool bad_type(int32_t type) { return type != CDGRAB_F32 && type != CDGRAB_BF16 && type != CDGRAB_F16; }
@@ -650,8 +664,8 @@ extern "C" int cdgrab_orthogonalize(cdgrab_handle *h, int64_t batch, int64_t row
                        m_matrix > (INT64_MAX >> 4) / batch || o_matrix > (INT64_MAX >> 4) / batch)))
         return fail(h, CDGRAB_EINVAL, "%s: a stride below the size, or a misaligned or too long array", who);
     if (batch == 1) m_matrix = o_matrix = 0;
-    const int64_t m_len = (batch - 1) * m_matrix + (rows - 1) * m_stride + cols, o_len = (batch - 1) * o_matrix + (rows - 1) * o_stride + cols;
-    if (ranges_overlap(M, m_len * size, O, o_len * size)) return fail(h, CDGRAB_EINVAL, "%s: M and O must not overlap", who);
+    if (matrices_overlap(batch, rows, cols * size, M, m_stride * size, m_matrix * size, O, o_stride * size, o_matrix * size))
+        return fail(h, CDGRAB_EINVAL, "%s: M and O must not overlap", who);
     const OnDevice on(h->device);
     HIP_TRY(h, on.err);
     const auto by_type = [&](auto elem) {
