@@ -570,13 +570,9 @@ extern "C" int cdgrab_pergrad_layernorm(cdgrab_handle *h, const cdgrab_token_row
                 }
                 launch(norm_backward<T, VEC, LANES, K, false>);
             }
-            if (partial) {
-                const int64_t groups = (cols + 31) / 32;
-                const int64_t most_e = std::max<int64_t>(1, kMaxGroups / groups);
-                for (int64_t e0 = 0; e0 < tok.examples; e0 += most_e)
-                    hipLaunchKernelGGL(norm_grad_finish, dim3((unsigned)(std::min(most_e, tok.examples - e0) * groups)), dim3(256), 0,
-                                       h->stream, partial + e0 * chunks * cols, (int)chunks, (int)cols, G + e0 * g_stride, g_stride);
-            }
+            if (partial)  // (fewer than `fill` examples, 2^11, of at most 2^10 groups of columns: one launch)
+                hipLaunchKernelGGL(norm_grad_finish, dim3((unsigned)(tok.examples * ((cols + 31) / 32))), dim3(256), 0, h->stream, partial,
+                                   (int)chunks, (int)cols, G, g_stride);
         });
     });
     if (rc) return rc;
