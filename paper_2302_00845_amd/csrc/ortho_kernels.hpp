@@ -839,8 +839,7 @@ __global__ __launch_bounds__(kOrthoSmallThreads) void ortho_small(OrthoIo<T> io,
 #pragma unroll
             for (int u = 0; u < PER; ++u) low[u] = mfma32(o.rh[u], o.ll, low[u]);
         };
-#pragma unroll 2
-        for (int k = 0; k < length; k += 16) {
+        for (int k = 0; k < length; k += 16) {  // (not unrolled: the transposing reads are convergent, the length is known at run time only)
             Operands o;
             read(o, k);
             multiply(o);
