@@ -237,8 +237,8 @@ __device__ __forceinline__ void ortho_gram(const OrthoIo<T> &io, int64_t b, int6
 #pragma unroll
                 for (int tj = ti; tj < NT; ++tj, ++at) acc[at] = __builtin_amdgcn_mfma_f64_16x16x4f64(x[ti], x[tj], acc[at], 0, 0, 0);
         }
-        // The results are copied at the loop's head, and there the compiler puts 4 wait states instead of 18 between the last
-        // product and the copy of its last two registers: without the next line rows 28 .. 31 of a tile miss products.
+        // Where the compiler copies the results at the loop's head it has put 4 wait states instead of 18 between the last product and
+        // the copy of its last two registers: rows 28 .. 31 of a tile missed products.  (As this stands it does not copy them.)
         __builtin_amdgcn_sched_barrier(0);
         asm volatile("s_nop 15\n\ts_nop 15");
         __builtin_amdgcn_sched_barrier(0);
