@@ -160,21 +160,25 @@ def _ptr(t: Optional[torch.Tensor], dtype, shape, name, device) -> Optional[int]
 _current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
-def _empty(h, shape, dtype) -> torch.Tensor:
-    """An output of a call.  It is allocated on the handle's stream, where the call writes it: memory that the current
-    stream has let go of may still be in use there.  The current stream is taken to be where it will be read."""
+def _allocator(h):
+    """torch.empty for the outputs of a call.  They are allocated on the handle's stream, where the call writes them: memory
+    that the current stream has let go of may still be in use there.  The current stream is taken to be where they will be
+    read."""
     if h.stream is None or h.stream_number == _current_stream(h.device_index):
-        return torch.empty(shape, dtype=dtype, device=h.device)
-    with torch.cuda.stream(h.stream):
-        out = torch.empty(shape, dtype=dtype, device=h.device)
-    out.record_stream(torch.cuda.current_stream(h.device))
-    return out
+        return torch.empty
+
+    def empty(shape, **kinds):
+        with torch.cuda.stream(h.stream):
+            out = torch.empty(shape, **kinds)
+        out.record_stream(torch.cuda.current_stream(h.device))
+        return out
+    return empty
 
 
 def _empty_like(h, t: torch.Tensor) -> torch.Tensor:
     if h.stream is None or h.stream_number == _current_stream(h.device_index):
         return torch.empty_like(t, memory_format=torch.contiguous_format)
-    return _empty(h, t.shape, t.dtype)
+    return _allocator(h)(t.shape, dtype=t.dtype, device=t.device)
 
 
 class Handle:
@@ -228,7 +232,7 @@ def cdgrab_pergrad(h: Handle, X: torch.Tensor, y: torch.Tensor, W: torch.Tensor,
     N, in_dim = X.shape
     classes = W.shape[1]
     if G_out is None:
-        G_out = _empty(h, (N, (in_dim + 1) * classes), torch.float32)
+        G_out = _allocator(h)((N, (in_dim + 1) * classes), dtype=torch.float32, device=h.device)
     h._check(h._lib.cdgrab_pergrad(
         h._h, N, in_dim, classes,
         _ptr(X, torch.float32, (N, in_dim), "X", h.device),
@@ -252,11 +256,12 @@ def cdgrab_balance_epoch(h: Handle, m: int, n: int, d: int,
     """
     dev = h.device
     half = n // 2 if n >= 0 else 0
-    signs = _empty(h, (max(m, 0), max(half, 0)), torch.int8)
-    perm = _empty(h, (max(m, 0), max(n, 0)), torch.int32)
-    r32 = _empty(h, (max(d, 0),), torch.float32) if want_r32 else None
-    r64 = _empty(h, (max(d, 0),), torch.float64) if want_r64 else None
-    dots = _empty(h, (max(m, 0), max(half, 0)), torch.float64) if want_dots else None
+    empty = _allocator(h)
+    signs = empty((max(m, 0), max(half, 0)), dtype=torch.int8, device=dev)
+    perm = empty((max(m, 0), max(n, 0)), dtype=torch.int32, device=dev)
+    r32 = empty((max(d, 0),), dtype=torch.float32, device=dev) if want_r32 else None
+    r64 = empty((max(d, 0),), dtype=torch.float64, device=dev) if want_r64 else None
+    dots = empty((max(m, 0), max(half, 0)), dtype=torch.float64, device=dev) if want_dots else None
     gptr = _ptr(grads, torch.float32, (m, n, d), "grads", dev) if grads is not None else None
     gen_ptr = ctypes.cast(gen, ctypes.c_void_p) if gen is not None else None
     h._check(h._lib.cdgrab_balance_epoch(
@@ -291,7 +296,7 @@ def cdgrab_balance_epoch_static(h: Handle, grads: torch.Tensor, out: dict,
 def cdgrab_reorder(h: Handle, signs: torch.Tensor, perm_in: Optional[torch.Tensor] = None) -> torch.Tensor:
     """General reorder from per-example +-1 signs [m][n] (int8)."""
     m, n = signs.shape
-    out = _empty(h, (m, n), torch.int32)
+    out = _allocator(h)((m, n), dtype=torch.int32, device=h.device)
     h._check(h._lib.cdgrab_reorder(
         h._h, m, n, _ptr(signs, torch.int8, (m, n), "signs", h.device),
         _ptr(perm_in, torch.int32, (m, n), "perm_in", h.device), out.data_ptr()))
@@ -302,7 +307,7 @@ def cdgrab_herding_bound(h: Handle, z: torch.Tensor, perm: Optional[torch.Tensor
     """Parallel herding objective of z[m][n][d] (indexed by example id) visited in
     the orders perm[m][n]; returns a one-element float64 GPU tensor."""
     m, n, d = z.shape
-    out = _empty(h, (1,), torch.float64)
+    out = _allocator(h)((1,), dtype=torch.float64, device=h.device)
     h._check(h._lib.cdgrab_herding_bound(
         h._h, m, n, d, _ptr(z, torch.float32, (m, n, d), "z", h.device),
         _ptr(perm, torch.int32, (m, n), "perm", h.device), out.data_ptr()))
@@ -320,10 +325,11 @@ def cdgrab_train_epoch_softmax(h: Handle, X: torch.Tensor, y: torch.Tensor, W: t
     classes = W.shape[1]
     d = (in_dim + 1) * classes
     dev = h.device
-    signs = _empty(h, (m, n // 2), torch.int8)
-    perm = _empty(h, (m, n), torch.int32)
-    grads = _empty(h, (m, n, d), torch.float32) if want_grads else None
-    loss = _empty(h, (m, n), torch.float32) if want_loss else None
+    empty = _allocator(h)
+    signs = empty((m, n // 2), dtype=torch.int8, device=dev)
+    perm = empty((m, n), dtype=torch.int32, device=dev)
+    grads = empty((m, n, d), dtype=torch.float32, device=dev) if want_grads else None
+    loss = empty((m, n), dtype=torch.float32, device=dev) if want_loss else None
     h._check(h._lib.cdgrab_train_epoch_softmax(
         h._h, m, n, in_dim, classes,
         _ptr(X, torch.float32, (m, n, in_dim), "X", dev), _ptr(y, torch.int32, (m, n), "y", dev),
@@ -346,8 +352,9 @@ def cdgrab_train_softmax(h: Handle, X: torch.Tensor, y: torch.Tensor, W: torch.T
     classes = W.shape[1]
     d = (in_dim + 1) * classes
     dev = h.device
-    signs = _empty(h, (m, n // 2), torch.int8)
-    loss = _empty(h, (epochs, m, n), torch.float32) if want_loss else None
+    empty = _allocator(h)
+    signs = empty((m, n // 2), dtype=torch.int8, device=dev)
+    loss = empty((epochs, m, n), dtype=torch.float32, device=dev) if want_loss else None
     h._check(h._lib.cdgrab_train_softmax(
         h._h, m, n, in_dim, classes,
         _ptr(X, torch.float32, (m, n, in_dim), "X", dev), _ptr(y, torch.int32, (m, n), "y", dev),
@@ -362,8 +369,9 @@ def cdgrab_balance_epoch_independent(h: Handle, grads: torch.Tensor,
                                      perm_in: Optional[torch.Tensor] = None) -> dict:
     """ID-GraB (PairBal): m independent one-worker walks over grads[m][n][d]."""
     m, n, d = grads.shape
-    signs = _empty(h, (m, n // 2), torch.int8)
-    perm = _empty(h, (m, n), torch.int32)
+    empty = _allocator(h)
+    signs = empty((m, n // 2), dtype=torch.int8, device=h.device)
+    perm = empty((m, n), dtype=torch.int32, device=h.device)
     h._check(h._lib.cdgrab_balance_epoch_independent(
         h._h, m, n, d, _ptr(grads, torch.float32, (m, n, d), "grads", h.device),
         _ptr(perm_in, torch.int32, (m, n), "perm_in", h.device), signs.data_ptr(), perm.data_ptr()))
@@ -376,10 +384,11 @@ def cdgrab_balance_epoch_stale_mean(h: Handle, grads: torch.Tensor,
     """Centralized GraB balancing of grads[n][d] centred by a stale mean."""
     n, d = grads.shape
     dev = h.device
-    signs = _empty(h, (n,), torch.int8)
-    perm = _empty(h, (n,), torch.int32)
-    mean = _empty(h, (d,), torch.float32)
-    r64 = _empty(h, (d,), torch.float64)
+    empty = _allocator(h)
+    signs = empty((n,), dtype=torch.int8, device=dev)
+    perm = empty((n,), dtype=torch.int32, device=dev)
+    mean = empty((d,), dtype=torch.float32, device=dev)
+    r64 = empty((d,), dtype=torch.float64, device=dev)
     h._check(h._lib.cdgrab_balance_epoch_stale_mean(
         h._h, n, d, _ptr(grads, torch.float32, (n, d), "grads", dev),
         _ptr(stale_mean, torch.float32, (d,), "stale_mean", dev),
@@ -393,10 +402,11 @@ def cdgrab_balance_epoch_randomized(h: Handle, grads: torch.Tensor, uniforms: to
     """cdgrab_balance_epoch with the randomized sign rule; uniforms[m][n/2] in [0,1)."""
     m, n, d = grads.shape
     dev = h.device
-    signs = _empty(h, (m, n // 2), torch.int8)
-    perm = _empty(h, (m, n), torch.int32)
-    r64 = _empty(h, (d,), torch.float64)
-    dots = _empty(h, (m, n // 2), torch.float64)
+    empty = _allocator(h)
+    signs = empty((m, n // 2), dtype=torch.int8, device=dev)
+    perm = empty((m, n), dtype=torch.int32, device=dev)
+    r64 = empty((d,), dtype=torch.float64, device=dev)
+    dots = empty((m, n // 2), dtype=torch.float64, device=dev)
     h._check(h._lib.cdgrab_balance_epoch_randomized(
         h._h, m, n, d, _ptr(grads, torch.float32, (m, n, d), "grads", dev),
         _ptr(uniforms, torch.float32, (m, n // 2), "uniforms", dev),
@@ -470,7 +480,7 @@ def _token_rows(X: torch.Tensor, rows: int, first, count, tokens: Optional[int],
 def _grad_rows(h, G_out: Optional[torch.Tensor], examples: int, d: int):
     """(G, stride): [examples][d] fp32, a stretch of longer rows if given so."""
     if G_out is None:
-        return _empty(h, (examples, d), torch.float32), d or 1
+        return _allocator(h)((examples, d), dtype=torch.float32, device=h.device), d or 1
     if G_out.dtype != torch.float32:
         raise TypeError("G_out must be float32, got %s" % G_out.dtype)
     if tuple(G_out.shape) != (examples, d):
@@ -595,10 +605,11 @@ def cdgrab_train_epoch_softmax_orthogonal(h: Handle, X: torch.Tensor, y: torch.T
     classes = W.shape[1]
     d = (in_dim + 1) * classes
     dev = h.device
-    signs = _empty(h, (m, n // 2), torch.int8)
-    perm = _empty(h, (m, n), torch.int32)
-    grads = _empty(h, (m, n, d), torch.float32) if want_grads else None
-    loss = _empty(h, (m, n), torch.float32) if want_loss else None
+    empty = _allocator(h)
+    signs = empty((m, n // 2), dtype=torch.int8, device=dev)
+    perm = empty((m, n), dtype=torch.int32, device=dev)
+    grads = empty((m, n, d), dtype=torch.float32, device=dev) if want_grads else None
+    loss = empty((m, n), dtype=torch.float32, device=dev) if want_loss else None
     h._check(h._lib.cdgrab_train_epoch_softmax_orthogonal(
         h._h, m, n, in_dim, classes,
         _ptr(X, torch.float32, (m, n, in_dim), "X", dev), _ptr(y, torch.int32, (m, n), "y", dev),
