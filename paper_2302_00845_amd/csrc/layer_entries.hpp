@@ -247,15 +247,18 @@ bool ortho_in_range(int64_t steps, const OrthoCoeffs &c, double *largest) {
 }
 
 // Steps that one Gram matrix serves.  A step takes an eigenvalue l of it to l q(l)^2, q = a + b l + c l^2, and what rounding has added
-// to the matrix grows by the slope of that, q (a + 3 b l + 5 c l^2), at the most: 2^-52 of the trace stays below 2^-30, which is nothing
-// beside 1 and beside the rounding of the results.  (Default coefficients: a^2 = 11.9 at l = 0, six steps.)
+// to the matrix grows by the slope of that, q (a + 3 b l + 5 c l^2), at the most: 2^-52 of the trace stays below 2^-12, which is little
+// beside 1, where the polynomial's range ends.  (Default coefficients: a^2 = 11.9 at l = 0, eleven steps; matrices that lack rank,
+// and with singular values down to 1e-4 .. 1e-9, are then off by 5e-6 at the most, where products in fp32 are by 5e-3 .. 3e-2.  Of
+// 15/8, -10/8, 3/8 it is 22 steps, and 8e-6.  Simulated further: twelve steps 1e-5, fourteen 1e-3, sixteen diverge.)  A further
+// stretch costs what the first one did: 785 x 10, 5 / 7 / 12 / 20 steps 13 / 14 / 33 / 37 us.
 int64_t ortho_gram_steps(const OrthoCoeffs &c, double largest) {
     double slope = 1.0;
     for (int q = 0; q <= 64; ++q) {
         const double l = largest * largest * q / 64;
         slope = std::max(slope, std::abs((c.a + c.b * l + c.c * l * l) * (c.a + 3.0 * c.b * l + 5.0 * c.c * l * l)));
     }
-    return slope > 1.25 ? std::max<int64_t>(1, (int64_t)(22.0 / std::log2(slope))) : 64;
+    return slope > 1.25 ? std::max<int64_t>(1, (int64_t)(40.0 / std::log2(slope))) : 64;
 }
 
 // `chunks` of `per` columns with their sums in `parts`; none: one workgroup per matrix.

@@ -10,7 +10,7 @@
 //     twice.  (In fp32 this form loses too much: the small eigenvalues of A_0 are the squares of the singular values.)
 //     Where the matrix lacks rank A_0 has eigenvalues that are rounding, of either sign, and the recurrence makes them grow by a^2 per
 //     step; for a negative one near -1 the polynomial has no bound.  So one A_0 serves as many steps as keep them small
-//     (ortho_gram_steps: six with the default coefficients); then X is made, in double, and its Gram matrix anew.
+//     (ortho_gram_steps: eleven with the default coefficients); then X is made, in double, and its Gram matrix anew.
 //   - else the products as they stand.  Factors are held as the sum of two fp16 (22 bits), and of the four products of the
 //     parts the three larger are taken: errors as of fp32 products (simulated on matrices of 256 .. 2048: 1.0 to 1.1 times), at a
 //     third of the fp16 MFMA rate, five times the fp32 MFMA's.  fp16 has the digits but not the range: the norm bounds every
@@ -88,7 +88,7 @@ struct OrthoTiles {
     const bool mine = wave < NT * NT;
     const int ti = wave / NT, tj = wave % NT;
 
-    // this wavefront's tile of X Y, X and Y in LDS
+    // this wavefront's tile of X^T Y (X Y where X is symmetric), X and Y in LDS
     __device__ __forceinline__ f64x4 product(const double *X, const double *Y) const {
         f64x4 even = {0.0, 0.0, 0.0, 0.0}, odd = {0.0, 0.0, 0.0, 0.0};
         if (mine) {
@@ -139,8 +139,10 @@ struct OrthoTiles {
 // P (in LDS) from the Gram matrix of M in A (in LDS), entries beyond the short side zero:
 //   A <- A / trace(A), P <- I / sqrt(trace) (not for an X that steps have made: `first`); steps times:
 //   Q = a I + b A + c A^2, P <- Q P, A <- Q A Q.
-// Everything commutes and is symmetric, so that the order of factors does not matter.  A single tile stays in one wavefront's
-// registers; more go through LDS, three rounds per step.
+// Everything commutes and is symmetric, but for rounding, which Q A Q takes between eigenvalues l and k to (f(l) - f(k)) / (l - k) of it,
+// f(l) = l q(l)^2, while A Q Q would take it to q(k)^2, a^2 for any l beside a small k.  (785 x 10 of rank nine, twenty steps of
+// 15/8, -10/8, 3/8: norm 1.0015 by A Q Q.)  A single tile stays in one wavefront's registers; more go through LDS, three
+// rounds per step.
 template <int NT>
 struct OrthoChain {
     typedef OrthoTiles<NT> Tiles;
@@ -168,7 +170,7 @@ struct OrthoChain {
 #pragma unroll
                     for (int v = 0; v < 4; ++v) q[v] = one[v] + c.b * a[v] + c.c * q[v];
                     p = Tiles::product(q, p);
-                    a = Tiles::product(Tiles::product(q, a), q);
+                    a = Tiles::product(q, Tiles::product(a, q));
                 }
             tiles.store(P, p);
         } else {
@@ -188,13 +190,13 @@ struct OrthoChain {
                     p = tiles.product(Q, P);
                 }
                 const bool more = s + 1 < steps;  // (the last step's A is for nobody)
-                if (more) a = tiles.product(Q, A);
+                if (more) a = tiles.product(A, Q);
                 __syncthreads();
                 tiles.store(P, p);
                 if (more) {
                     tiles.store(A, a);
                     __syncthreads();
-                    a = tiles.product(A, Q);
+                    a = tiles.product(Q, A);
                     __syncthreads();
                     tiles.store(A, a);
                 }

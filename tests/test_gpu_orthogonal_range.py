@@ -112,3 +112,20 @@ def test_training_epoch_of_many_steps(lib, steps):  # noqa: F811
                                                     torch.from_numpy(y).cuda().view(m, n), W, v, lr=lr, momentum=0.9, steps=steps)
     assert torch.isfinite(W).all() and torch.isfinite(v).all() and torch.isfinite(out["loss"]).all()
     assert np.linalg.norm(W.cpu().numpy() - W0) <= n * lr * 1.203 * classes ** 0.5 * 1.01
+
+
+def spread(seed, rows, cols, least):
+    """Singular values from 1 down to `least`, evenly over their logarithm."""
+    u, _ = torch.linalg.qr(rand(seed, rows, rows, dtype=torch.float64).cpu())
+    v, _ = torch.linalg.qr(rand(seed + 1, cols, rows, dtype=torch.float64).cpu())
+    return (u * torch.logspace(0, np.log10(least), rows, dtype=torch.float64) @ v.t()).float().cuda()
+
+
+# The Gram matrix's rounding, 2^-52 of its trace, grows by 3.4445^2 per step, as a part of a singular value's square: at most
+# 2^-12 of that, half of it of the value, after the eleven steps that one matrix serves; and of the matrix's norm only
+# what the few values have that have grown to about one by then, a fifth of them or less: 5e-5.  (15/8: 22 steps.)
+@pytest.mark.parametrize("steps,coeffs", [(11, COEFFS), (12, COEFFS), (22, POLAR), (23, POLAR)])
+@pytest.mark.parametrize("rows,cols,least", [(30, 100, 1e-4), (12, 6000, 1e-6), (60, 900, 1e-7), (32, 50, 1e-9)])
+def test_singular_values_of_all_sizes(lib, rows, cols, least, steps, coeffs):  # noqa: F811
+    m = spread(rows, rows, cols, least)
+    check(lib.cdgrab_orthogonalize(lib.Handle(), m, steps=steps, coeffs=coeffs), m, torch.float32, steps, coeffs, tol=5e-5)
