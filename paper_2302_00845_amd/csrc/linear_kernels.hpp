@@ -222,8 +222,8 @@ __global__ __launch_bounds__(kLinearThreads) void linear_grad(TokenRows tok, int
 
 // Few rows per example (TOK at most): G is the sum of as many outer products, and writing it is all that costs.  A workgroup
 // writes a stretch of kFlatElems consecutive elements of an example's G, whatever rows they belong to, with aligned 16-byte
-// stores; the features and deltas that they need lie in LDS.  60 000 rows of 784 -> 10: 0.45 ms, 4.6 TB/s, nine tenths of
-// what a large copy reaches.  (By tiles of MFMAs 60 000 rows of 784 -> 10 took 2.68 ms: 10 of
+// stores; the features and deltas that they need lie in LDS.  60 000 rows of 784 -> 10: 0.45 ms, 4.6 TB/s, two thirds of
+// what a large fill reaches, nine tenths of what these stores reach by themselves.  (By tiles of MFMAs 60 000 rows of 784 -> 10 took 2.68 ms: 10 of
 // 32 columns used, stores of 40 bytes, and a chain of loads, barriers and products for a few KB.)
 constexpr int kFlatElems = 8192;
 constexpr int kFlatLds = 16000;  // floats of features and deltas at most

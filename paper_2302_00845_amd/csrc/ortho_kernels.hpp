@@ -4,20 +4,23 @@
 //
 // Small singular values grow by a factor of a per step (3.4 by default), and so does what rounding does to their vectors:
 // products in fp32, or as good, are needed between steps even for results of fewer bits (with one product of bf16 factors the
-// result is off by some percent).  Two forms:
-//   - short side up to kOrthoNarrow: X_K = P_K X_0 with P_K a polynomial in A_0 = X_0 X_0^T.  One pass over the matrix for A_0 in
-//     double, the recurrence on matrices of the short side (all of which commute), one pass for the product: bytes of the matrix
-//     twice.  (In fp32 this form loses too much: the small eigenvalues of A_0 are the squares of the singular values.)
-//     Where the matrix lacks rank A_0 has eigenvalues that are rounding, of either sign, and the recurrence makes them grow by a^2 per
-//     step; for a negative one near -1 the polynomial has no bound.  So one A_0 serves as many steps as keep them small
+// result is off by some percent).  Three forms:
+//   - short side up to 32, and up to kOrthoNarrow where the matrix does not fit in LDS: X_K = P_K X_0 with P_K a polynomial in
+//     A_0 = X_0 X_0^T.  One pass over the matrix for A_0 in double, the recurrence on matrices of the short side (all of which
+//     commute), one pass for the product: bytes of the matrix twice.  (In fp32 this form loses too much: the small
+//     eigenvalues of A_0 are the squares of the singular values.)
+//     Where the matrix lacks rank A_0 has eigenvalues that are rounding, of either sign, and the recurrence makes them grow by a^2
+//     per step; for a negative one near -1 the polynomial has no bound.  So one A_0 serves as many steps as keep them small
 //     (ortho_gram_steps: eleven with the default coefficients); then X is made, in double, and its Gram matrix anew.
-//   - else the products as they stand.  Factors are held as the sum of two fp16 (22 bits), and of the four products of the
-//     parts the three larger are taken: errors as of fp32 products (simulated on matrices of 256 .. 2048: 1.0 to 1.1 times), at a
-//     third of the fp16 MFMA rate, five times the fp32 MFMA's.  fp16 has the digits but not the range: the norm bounds every
-//     element, a fixed power of two in front uses the range, and the small part is held kOrthoLift times as large, so that it has its
-//     eleven bits as long as the large part has.  Elements of X from 2^-27 of the norm on have 22 bits, smaller ones are off by
-//     about 2^-49 of the norm (with the small part as it is: from 2^-16 on, and by 2^-38; rows 1e-7 of the others
-//     came out half a percent off).  A and A^2 are symmetric: half of their tiles are computed.
+//   - short side up to 128 of a matrix that fits in LDS as pairs with its Gram matrix (OrthoSmall): the products as they stand,
+//     all steps in one workgroup.
+//   - else the products as they stand, three launches a step.  A and A^2 are symmetric: half of their tiles are computed.
+// Pairs: in the last two forms factors are held as the sum of two fp16 (22 bits), and of the four products of the parts the three
+// larger are taken: errors as of fp32 products (simulated on matrices of 256 .. 2048: 1.0 to 1.1 times), at a third of the fp16
+// MFMA rate, five times the fp32 MFMA's.  fp16 has the digits but not the range: the norm bounds every element, a fixed power of two
+// in front uses the range, and the small part is held kOrthoLift times as large, so that it has its eleven bits as long as the
+// large part has.  Elements of X from 2^-27 of the norm on have 22 bits, smaller ones are off by about 2^-49 of the norm (with
+// the small part as it is: from 2^-16 on, and by 2^-38; rows 1e-7 of the others came out half a percent off).
 #pragma once
 #include "narrow_common.hpp"
 #include "mfma_tiles.hpp"
