@@ -297,7 +297,8 @@ int cdgrab_train_epoch_softmax(cdgrab_handle *h, int64_t m, int64_t n, int64_t i
  *     v <- momentum v + gbar,   W <- W - lr O(v),
  * O(v) as cdgrab_orthogonalize (below) makes it of v as a matrix [in_dim+1][classes].  velocity is required (zeros
  * before the first epoch), also for momentum 0, and must not overlap W; steps and coeffs as there; other arguments, outputs
- * and the balancing as in cdgrab_train_epoch_softmax.  Errors: as there and there. */
+ * and the balancing as in cdgrab_train_epoch_softmax.  Errors: as there and there; where the update's workspace cannot be had
+ * (ENOMEM) nothing has been enqueued. */
 int cdgrab_train_epoch_softmax_orthogonal(cdgrab_handle *h, int64_t m, int64_t n, int64_t in_dim,
                                           int64_t classes, const float *X, const int32_t *y,
                                           const int32_t *perm_in, float *W, float *velocity, float lr,
