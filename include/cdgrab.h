@@ -382,7 +382,7 @@ typedef struct cdgrab_token_rows {
  * (over `width`, biased) of the row.
  *   X, Y [rows][width] of `type` dev; gain, bias [width] fp32 dev, or NULL: one, zero.
  * Statistics in fp32; a row with an element that is not finite becomes NaN, and so does one whose squared differences from
- * the mean add up to more than 3.4e38 (elements beyond about 1e19).
+ * the mean add up to more than 3.4e38 (elements beyond about 1e19), and with eps 0 a row of equal elements.
  * Errors: EINVAL (sizes, width > 16384, type, eps < 0, null, strides, overlap), EHIP. */
 int cdgrab_layernorm(cdgrab_handle *h, int64_t rows, int64_t width, int32_t type, const void *X,
                      int64_t x_stride, const float *gain, const float *bias, float eps, void *Y,

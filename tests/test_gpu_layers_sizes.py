@@ -135,3 +135,17 @@ def test_no_steps_on_many_matrices(lib):  # noqa: F811
     norm = m.flatten(1).double().norm(dim=1).view(-1, 1, 1)
     want = m.double() / norm
     close(out, want, 2 * U * want.abs() + 1e-38, "X0")  # (rounded once, from double)
+
+
+@pytest.mark.parametrize("tokens,n_in,n_out", [(3, 70, 40), (60, 130, 90)])
+def test_first_without_count(lib, tokens, n_in, n_out):  # noqa: F811
+    """Examples of `tokens` rows each, wherever they start; the last one is cut by the array's end."""
+    rows = 3 * tokens + 2
+    x, d, dy = rand(1, rows, n_in), rand(2, rows, n_out), rand(3, rows, n_in)
+    first = torch.tensor([2 * tokens, 1, rows - 2], dtype=torch.int64, device="cuda")
+    spans = [(2 * tokens, tokens), (1, tokens), (rows - 2, 2)]
+    h = lib.Handle()
+    want, tol = linear64(x, d, spans, torch.float32)
+    close(lib.cdgrab_pergrad_linear(h, x, d, first=first, tokens=tokens), want, tol, "linear")
+    _, _, want_g, tol_g = grad64(x, dy, torch.ones(n_in, device="cuda"), 1e-5, spans, torch.float32)
+    close(lib.cdgrab_pergrad_layernorm(h, x, dy, first=first, tokens=tokens)[1], want_g, tol_g, "norm")
