@@ -19,7 +19,9 @@
  *     call with a given shape allocates workspace (and may synchronise the stream
  *     to free a smaller one); later calls of cdgrab_pergrad and the balancing
  *     entry points with dense input enqueue kernels and device-to-device copies
- *     only, so they may be captured in a HIP graph.  A captured call takes its sums in the
+ *     only, so they may be captured in a HIP graph.  The workspace that a captured call
+ *     uses is kept until the handle is destroyed, also when a later call needs a larger
+ *     one; replays and calls share it, so they must not overlap.  A captured call takes its sums in the
  *     order of the eager one.  (Rows of at most 64 elements, 512 pairs and more: if such an
  *     epoch has run on the handle before.  Else, and where up to 64 MB of workspace find no
  *     room, the order is another: the same result on exactly representable input, otherwise

@@ -84,8 +84,8 @@ struct cdgrab_handle {
     double *bands_kept = nullptr;                         // ... or that of this one, which it has replaced
     float *staging = nullptr;  int64_t staging_cap = 0;   // floats: two staging chunks (the fused pass reads the previous block too)
     char *layer_ws = nullptr;  int64_t layer_ws_cap = 0;  // bytes: sums in shares, matrices of the orthogonalised update
-    bool layer_ws_in_graphs = false;                      // recorded launches hold its address ...
-    std::vector<char *> layer_kept;                       // ... or that of one of these, which it has replaced
+    bool recorded = false;                                // recorded launches hold the buffers' addresses ...
+    std::vector<void *> kept;                             // ... or those of these, which larger ones have replaced
     bool fixed_workspace = false;                         // the workspace pointers are borrowed: never grow or free them
 
     hipStream_t side = nullptr;                           // chunks are balanced here while the next one is generated
@@ -358,13 +358,26 @@ int mark(cdgrab_handle *h, int kind_after) {
         }                                                      \
     } while (0)
 
+// Room for `want` elements.  Once a call on the handle has been recorded, a buffer that a larger one replaces is kept until the
+// handle goes: the recording holds its address.
 template <typename T>
 int ensure(cdgrab_handle *h, T *&ptr, int64_t &cap, int64_t want) {
     if (cap >= want) return CDGRAB_OK;
     if (h->fixed_workspace)
         return fail(h, CDGRAB_ENOMEM, "the fixed workspace is too small (%lld elements needed, %lld there)",
                     (long long)want, (long long)cap);
-    if (ptr) { HIP_TRY(h, hipStreamSynchronize(h->stream)); HIP_TRY(h, hipFree(ptr)); ptr = nullptr; cap = 0; }
+    if (ptr && h->recorded) {
+        try {
+            h->kept.push_back(ptr);
+        } catch (...) {
+            return fail(h, CDGRAB_ENOMEM, "out of host memory");
+        }
+    } else if (ptr) {
+        HIP_TRY(h, hipStreamSynchronize(h->stream));
+        HIP_TRY(h, hipFree(ptr));
+    }
+    ptr = nullptr;
+    cap = 0;
     hipError_t e = hipMalloc(reinterpret_cast<void **>(&ptr), (size_t)want * sizeof(T));
     if (e != hipSuccess) {
         ptr = nullptr;
@@ -391,6 +404,11 @@ bool capturing(cdgrab_handle *h) {
     if (hipStreamIsCapturing(h->stream, &status) == hipSuccess) return status != hipStreamCaptureStatusNone;
     (void)hipGetLastError();
     return true;
+}
+
+// To be called where a call that may be recorded begins, before its workspace is looked at.
+void note_recording(cdgrab_handle *h) {
+    if (!h->recorded) h->recorded = capturing(h);
 }
 
 // `want` doubles for the Gram results of long narrow walks, or false: then they go without.  A recorded call allocates nothing
@@ -796,7 +814,7 @@ int cdgrab_destroy(cdgrab_handle *h) {
     if (h->bands) (void)hipFree(h->bands);
     if (h->bands_kept) (void)hipFree(h->bands_kept);
     if (h->layer_ws) (void)hipFree(h->layer_ws);
-    for (char *p : h->layer_kept) (void)hipFree(p);
+    for (void *p : h->kept) (void)hipFree(p);
     delete h;
     return CDGRAB_OK;
 }
@@ -927,6 +945,7 @@ int Epoch::prepare() {
         return fail(h, CDGRAB_EINVAL, "cdgrab_balance_epoch: give exactly one of grads and gen");
     if (n > INT32_MAX) return fail(h, CDGRAB_EINVAL, "cdgrab_balance_epoch: n exceeds int32 range");
     HIP_TRY(h, hipSetDevice(h->device));
+    note_recording(h);
 
     streamed = grads == nullptr;
     int64_t align = 16;
@@ -1683,6 +1702,7 @@ int cdgrab_herding_bound(cdgrab_handle *h, int64_t m, int64_t n, int64_t d, cons
         return fail(h, CDGRAB_EINVAL, "cdgrab_herding_bound: need m>=1, n>=1, d>=1");
     if (!z || !bound_out) return fail(h, CDGRAB_EINVAL, "cdgrab_herding_bound: null pointer");
     HIP_TRY(h, hipSetDevice(h->device));
+    note_recording(h);
     HerdingShape sh;
     sh.m = m; sh.n = n; sh.d = d;
     // enough (segment, four elements) threads to fill the chip, at least one step per segment
@@ -1708,7 +1728,7 @@ int cdgrab_herding_bound(cdgrab_handle *h, int64_t m, int64_t n, int64_t d, cons
     const size_t lds = lds_ids ? ids_bytes : 0;
     const int form = row_form((d % 4 == 0 && reinterpret_cast<uintptr_t>(z) % 16 == 0) ? 4 : 1, d);
     // where the steps' sums are kept for the second pass (and fit), the rows are read once; not in a launch that is
-    // recorded, because their buffer is replaced when a later call has more steps
+    // recorded, for which their buffer would have to be kept when a later call has more steps
     const bool keep = m >= kHerdKeepMinWorkers && n <= kHerdKeepBytes / 32 / quads && !capturing(h) &&
                       room(h, h->herd_steps, h->herd_steps_cap, n * quads * 4);
     hipLaunchKernelGGL(herding_clear, dim3(1), dim3(1), 0, h->stream, bits);

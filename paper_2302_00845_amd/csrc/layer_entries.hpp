@@ -10,30 +10,17 @@ constexpr int64_t kOrthoMaxSide = (int64_t)1 << 20;
 constexpr int64_t kMaxGroups = (int64_t)1 << 21;  // workgroups per launch, of up to 1024 threads (a grid dimension holds fewer than 2^32)
 constexpr int64_t kMaxCells = (int64_t)1 << 32;   // elements of a matrix, of a gradient row: 2^22 workgroups of 256 threads at the most
 
-// Workspace of the layer operators.  What a recorded call has used is kept until the handle goes, also when a larger
-// buffer takes its place: the recording holds its address.  A recorded call allocates nothing.
+// Workspace of the layer operators.  A recorded call allocates nothing.
 template <typename T>
 int layer_room(cdgrab_handle *h, const char *who, int64_t want, T **out) {
     const int64_t bytes = want * (int64_t)sizeof(T);
     const bool recorded = capturing(h);
-    if (h->layer_ws_cap < bytes) {
-        if (recorded)
-            return fail(h, CDGRAB_ENOMEM, "%s: needs %lld bytes of workspace, and none can be allocated while the stream is "
-                        "captured: make the call once before", who, (long long)bytes);
-        if (h->layer_ws && h->layer_ws_in_graphs) {
-            try {
-                h->layer_kept.push_back(h->layer_ws);
-            } catch (...) {
-                return fail(h, CDGRAB_ENOMEM, "%s: out of host memory", who);
-            }
-            h->layer_ws = nullptr;
-            h->layer_ws_cap = 0;
-            h->layer_ws_in_graphs = false;
-        }
-        const int rc = ensure(h, h->layer_ws, h->layer_ws_cap, bytes);
-        if (rc) return rc;
-    }
-    if (recorded) h->layer_ws_in_graphs = true;
+    if (recorded && h->layer_ws_cap < bytes)
+        return fail(h, CDGRAB_ENOMEM, "%s: needs %lld bytes of workspace, and none can be allocated while the stream is "
+                    "captured: make the call once before", who, (long long)bytes);
+    if (recorded) h->recorded = true;
+    const int rc = ensure(h, h->layer_ws, h->layer_ws_cap, bytes);
+    if (rc) return rc;
     *out = reinterpret_cast<T *>(h->layer_ws);
     return CDGRAB_OK;
 }
