@@ -4,8 +4,8 @@
 //   g = gain dy, dx = r (g - mean(g) - h mean(g h)); per example dgain = sum_t dy h, dbias = sum_t dy
 //
 // Both are bound by bytes, in fp32: x in and y out; x and dy in, dx out.  In 16 bits the arithmetic is near (VALU busy 79 and 74 % of the
-// cycles at a width of 768, 4.6 and 4.4 TB/s), at odd widths, whose last group of columns is computed twice, as well (61 and
-// 68 % at 515).  A row stays in the registers of the LANES threads that
+// cycles at a width of 768, 4.6 and 4.4 TB/s), and at odd widths, where threads beyond the row compute what they discard, it is
+// what they wait for as much as bytes (61 and 69 % at 515, 2.1 and 1.9 TB/s).  A row stays in the registers of the LANES threads that
 // share it between the read and the write, sixteen bytes a thread and access, so that nothing is read twice; the backward
 // pass takes mean and deviation from the row it has to read anyway instead of from a forward pass's arrays.
 // Statistics and sums in fp32: the mean is taken first and corrected by the mean of what is left, so that a row far from
