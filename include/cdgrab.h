@@ -438,6 +438,81 @@ int cdgrab_orthogonalize(cdgrab_handle *h, int64_t batch, int64_t rows, int64_t 
                          const void *M, int64_t m_stride, int64_t m_matrix, int32_t steps,
                          const double *coeffs /*host*/, void *O, int64_t o_stride, int64_t o_matrix);
 
+/* ---- Operators over the rows of a sequence --------------------------------------------
+ *
+ * What a transformer has beside layer norm and linear layers: the embedding of token ids, the norms of queries and keys
+ * with the position rotation, and causal attention within each example.  Rows, types, strides, capture and errors as above;
+ * cdgrab_token_rows says which rows an example has, and a row's position is its place in its example.  Rows of no example are
+ * neither read nor written.  Of examples that share rows, outputs of those rows (Y, DX, O, lse, DQ, DK, DV) are those of any one of
+ * them, or of several in part; gradients of parameters (G) are right for every one. */
+
+/* Embedding:  Y[t] = scale * table[ids[t]], rounded once; a row of zeros for an id outside 0 .. vocab - 1.
+ *   ids [rows] int32 dev, table [vocab][width] of `table_type` (fp32 or `type`) dev, Y [rows][width] of `type` dev.
+ * Errors: EINVAL (sizes, width > 2^20, types, scale not finite, null, strides, overlap), EHIP. */
+int cdgrab_embed(cdgrab_handle *h, int64_t rows, int64_t vocab, int64_t width, const int32_t *ids, int32_t table_type,
+                 const void *table, int64_t t_stride, float scale, int32_t type, void *Y, int64_t y_stride);
+
+/* Gradient of cdgrab_embed's table for every example:
+ *     G[e][v * width + c] = scale * sum over the example's rows t with ids[t] = v of DY[t][c];
+ * ids outside 0 .. vocab - 1 have no part in it.  One example that holds all rows gives the ordinary gradient.
+ *   ids [rows] int32 dev, DY [rows][width] of `type` dev, G: row e at G + e * g_stride, fp32 dev, written whole.
+ * Examples of more than 2048 rows use workspace (16 bytes a row, and 8 * width bytes per 64 rows; at most 1 GiB, or one
+ * example's).  Sums in fp32.  Errors: EINVAL (as above; tokens > 2^28, more than 2^32 elements per row of G), ENOMEM, EHIP. */
+int cdgrab_pergrad_embed(cdgrab_handle *h, const cdgrab_token_rows *t, int64_t vocab, int64_t width, int32_t type,
+                         const int32_t *ids, const void *DY, int64_t dy_stride, float scale, float *G, int64_t g_stride);
+
+/* Heads of a row: q_heads queries and behind them k_heads keys of `dim` features each. */
+typedef struct cdgrab_heads {
+    int64_t q_heads, k_heads; /* either may be 0                                              */
+    int64_t dim;              /* even, at most 512                                            */
+    double base;              /* of the rotation: at least 1 (10000 is usual), or 0: none     */
+    float eps;
+} cdgrab_heads;
+
+/* Norm and rotation of every head:  h = X / sqrt(mean(X^2) + eps) over the head's features, u = gain * h, and with
+ * a_i = position * base^(-2 i / dim), i < dim / 2,
+ *     Y[i] = u[i] cos a_i - u[i + dim/2] sin a_i,    Y[i + dim/2] = u[i + dim/2] cos a_i + u[i] sin a_i.
+ *   X, Y [rows][(q_heads + k_heads) * dim] of `type` dev; gain_q (queries), gain_k (keys) [dim] fp32 dev, or NULL: one.
+ * Angles are good to 2^-27 of a turn at any position.  A head with an element that is not finite, or whose squares add up beyond fp32
+ * (elements beyond about 1e19), becomes NaN, and with eps 0 a head of zeros.
+ * Errors: EINVAL (sizes, dim odd or > 512, more than 4096 heads, type, eps < 0, base, null, strides, overlap), EHIP. */
+int cdgrab_headnorm(cdgrab_handle *h, const cdgrab_token_rows *t, const cdgrab_heads *s, int32_t type, const void *X,
+                    int64_t x_stride, const float *gain_q, const float *gain_k, void *Y, int64_t y_stride);
+
+/* Backward pass of cdgrab_headnorm, with the gains' gradients of every example: with u = DY turned back and g = gain * u,
+ *     DX = (g - h mean(g h)) / sqrt(mean(X^2) + eps),
+ *     G[e][c] = sum over the example's rows and queries of u[c] h[c],  G[e][dim + c] = the same of its keys.
+ *   X (the forward pass's input), DY, DX as there; G: row e at G + e * g_stride, fp32 dev.  DX or G may be NULL: not wanted.
+ * Errors: EINVAL (as above; neither DX nor G), ENOMEM, EHIP. */
+int cdgrab_pergrad_headnorm(cdgrab_handle *h, const cdgrab_token_rows *t, const cdgrab_heads *s, int32_t type, const void *X,
+                            int64_t x_stride, const void *DY, int64_t dy_stride, const float *gain_q, const float *gain_k,
+                            void *DX, int64_t dx_stride, float *G, int64_t g_stride);
+
+/* Causal attention within each example: for query i of a head, over the example's rows j <= i,
+ *     s_ij = scale * Q_i . K_j,   lse_i = ln sum_j exp(s_ij),   O_i = sum_j exp(s_ij - lse_i) V_j;
+ * q_heads / kv_heads consecutive heads of queries share a head of keys and values.
+ *   Q, O [rows][q_heads * dim], K, V [rows][kv_heads * dim] of `type` dev; lse [rows][q_heads] fp32 dev, or NULL: not wanted.
+ * Products of bf16 and fp16 elements are exact, those of fp32 elements good to 2^-23; exponentials are rounded to `type`
+ * (fp32: to 2^-24) where they are multiplied with V, sums are fp32.  An element that is not finite makes the results it enters infinite
+ * or NaN, and may do so to those of up to 127 rows before it in its example.
+ * Errors: EINVAL (sizes, dim > 128, more than 4096 heads, q_heads no multiple of kv_heads, more than 2^22 tokens, type,
+ * scale not positive and finite, null, strides, overlap), EHIP. */
+int cdgrab_attention(cdgrab_handle *h, const cdgrab_token_rows *t, int64_t q_heads, int64_t kv_heads, int64_t dim, int32_t type,
+                     float scale, const void *Q, int64_t q_stride, const void *K, int64_t k_stride, const void *V,
+                     int64_t v_stride, void *O, int64_t o_stride, float *lse);
+
+/* Backward pass of cdgrab_attention: with p_ij = exp(s_ij - lse_i) and ds_ij = p_ij (DO_i . V_j - DO_i . O_i),
+ *     DQ_i = scale sum_j ds_ij K_j,   DK_j = scale sum_i ds_ij Q_i,   DV_j = sum_i p_ij DO_i,
+ * the last two over the heads that share K_j and V_j.
+ *   Q, K, V, scale: the forward pass's; O, lse: its outputs; DO as O; DQ as Q, DK and DV as K.
+ * p and ds are rounded to `type` (fp32: to 2^-24) where they are multiplied.  Workspace: 4 * rows * q_heads bytes.
+ * Errors: EINVAL (as above), ENOMEM, EHIP. */
+int cdgrab_attention_backward(cdgrab_handle *h, const cdgrab_token_rows *t, int64_t q_heads, int64_t kv_heads, int64_t dim,
+                              int32_t type, float scale, const void *Q, int64_t q_stride, const void *K, int64_t k_stride,
+                              const void *V, int64_t v_stride, const void *O, int64_t o_stride, const float *lse,
+                              const void *DO, int64_t do_stride, void *DQ, int64_t dq_stride, void *DK, int64_t dk_stride,
+                              void *DV, int64_t dv_stride);
+
 /* Timings of the last cdgrab_balance_epoch on this handle (options.timing >= 1).
  * Synchronises the stream.  Errors: EINVAL (timing was off), EHIP. */
 int cdgrab_get_timing(cdgrab_handle *h, cdgrab_timing *out /*host*/);

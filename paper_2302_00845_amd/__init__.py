@@ -7,15 +7,21 @@ same entry-point names; PyTorch is used only for device memory and streams.
 from .cdgrab import (  # noqa: F401
     CdgrabError,
     Handle,
+    cdgrab_attention,
+    cdgrab_attention_backward,
     cdgrab_balance_epoch,
     cdgrab_balance_epoch_independent,
     cdgrab_balance_epoch_randomized,
     cdgrab_balance_epoch_stale_mean,
     cdgrab_balance_epoch_static,
+    cdgrab_embed,
+    cdgrab_headnorm,
     cdgrab_herding_bound,
     cdgrab_layernorm,
     cdgrab_orthogonalize,
     cdgrab_pergrad,
+    cdgrab_pergrad_embed,
+    cdgrab_pergrad_headnorm,
     cdgrab_pergrad_layernorm,
     cdgrab_pergrad_linear,
     cdgrab_plan_epoch,

@@ -64,6 +64,11 @@ class _TokenRows(ctypes.Structure):
                 ("first", ctypes.c_void_p), ("count", ctypes.c_void_p)]
 
 
+class _Heads(ctypes.Structure):
+    _fields_ = [("q_heads", ctypes.c_int64), ("k_heads", ctypes.c_int64), ("dim", ctypes.c_int64),
+                ("base", ctypes.c_double), ("eps", ctypes.c_float)]
+
+
 _ELEM = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}  # CDGRAB_F32, _BF16, _F16
 
 
@@ -124,6 +129,19 @@ def load_library():
     lib.cdgrab_pergrad_linear.restype = ctypes.c_int
     lib.cdgrab_orthogonalize.argtypes = [P, i64, i64, i64, i32, P, i64, i64, i32, P, P, i64, i64]
     lib.cdgrab_orthogonalize.restype = ctypes.c_int
+    f32, rows_of, heads_of = ctypes.c_float, ctypes.POINTER(_TokenRows), ctypes.POINTER(_Heads)
+    lib.cdgrab_embed.argtypes = [P, i64, i64, i64, P, i32, P, i64, f32, i32, P, i64]
+    lib.cdgrab_embed.restype = ctypes.c_int
+    lib.cdgrab_pergrad_embed.argtypes = [P, rows_of, i64, i64, i32, P, P, i64, f32, P, i64]
+    lib.cdgrab_pergrad_embed.restype = ctypes.c_int
+    lib.cdgrab_headnorm.argtypes = [P, rows_of, heads_of, i32, P, i64, P, P, P, i64]
+    lib.cdgrab_headnorm.restype = ctypes.c_int
+    lib.cdgrab_pergrad_headnorm.argtypes = [P, rows_of, heads_of, i32, P, i64, P, i64, P, P, P, i64, P, i64]
+    lib.cdgrab_pergrad_headnorm.restype = ctypes.c_int
+    lib.cdgrab_attention.argtypes = [P, rows_of, i64, i64, i64, i32, f32] + [P, i64] * 4 + [P]
+    lib.cdgrab_attention.restype = ctypes.c_int
+    lib.cdgrab_attention_backward.argtypes = [P, rows_of, i64, i64, i64, i32, f32] + [P, i64] * 4 + [P] + [P, i64] * 4
+    lib.cdgrab_attention_backward.restype = ctypes.c_int
     lib.cdgrab_get_timing.argtypes = [P, ctypes.POINTER(Timing)]
     lib.cdgrab_get_timing.restype = ctypes.c_int
     _lib = lib
@@ -593,6 +611,187 @@ def cdgrab_orthogonalize(h: Handle, M: torch.Tensor, steps: int = 5, coeffs=None
     if rc:
         h._check(rc)
     return out
+
+
+# ---- operators over the rows of a sequence ---------------------------------------------------
+
+def _ids(ids: torch.Tensor, shape, device) -> int:
+    return _ptr(ids, torch.int32, shape, "ids", device)
+
+
+def _made_like(h, t: torch.Tensor, shape, dtype, partly: bool) -> torch.Tensor:
+    """An output that the call makes; zeros where it may not write all of it (`partly`)."""
+    out = _allocator(h)(shape, dtype=dtype, device=t.device)
+    if partly:
+        with torch.cuda.stream(h.stream):  # before the call's kernels, wherever they run
+            out.zero_()
+    return out
+
+
+def cdgrab_embed(h: Handle, ids: torch.Tensor, table: torch.Tensor, scale: float = 1.0,
+                 dtype: Optional[torch.dtype] = None, Y: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Y[..., width] = scale * table[ids], ids [...] int32, table [vocab][width] float32 or of Y's type (``dtype``, by
+    default the table's); zeros for an id outside the table."""
+    dev = h.device
+    pt, vocab, width, st = _rows(table, "table", dev)
+    if table.dim() != 2:
+        raise ValueError("table must be [vocab][width], got %s" % (tuple(table.shape),))
+    if Y is None:
+        Y = _allocator(h)((*ids.shape, width), dtype=dtype or table.dtype, device=dev)
+    elif tuple(Y.shape) != (*ids.shape, width) or (dtype is not None and Y.dtype != dtype):
+        raise ValueError("Y must be %s %s, got %s %s" % (dtype or table.dtype, (*ids.shape, width), Y.dtype, tuple(Y.shape)))
+    if Y.dtype not in _ELEM:
+        raise TypeError("Y must be float32, bfloat16 or float16, got %s" % Y.dtype)
+    if table.dtype not in (torch.float32, Y.dtype):
+        raise TypeError("table must be float32 or %s, got %s" % (Y.dtype, table.dtype))
+    py, rows, _, sy = _rows(Y if Y.dim() > 1 else Y.unsqueeze(0), "Y", dev)
+    rc = h._lib.cdgrab_embed(h._h, rows, vocab, width, _ids(ids, ids.shape, dev), _ELEM[table.dtype], pt, st, scale,
+                             _ELEM[Y.dtype], py, sy)
+    if rc:
+        h._check(rc)
+    return Y
+
+
+def cdgrab_pergrad_embed(h: Handle, ids: torch.Tensor, dY: torch.Tensor, vocab: int, scale: float = 1.0,
+                         first: Optional[torch.Tensor] = None, count: Optional[torch.Tensor] = None,
+                         tokens: Optional[int] = None, G_out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Per-example gradients G[examples][vocab * width] of cdgrab_embed's table from its output's gradients dY; rows of
+    examples as in cdgrab_pergrad_layernorm, an id per row."""
+    dev = h.device
+    py, rows, width, sy = _rows(dY, "dY", dev)
+    t = _token_rows(dY, rows, first, count, tokens, dev)
+    G, sg = _grad_rows(h, G_out, t.examples, vocab * width)
+    rc = h._lib.cdgrab_pergrad_embed(h._h, ctypes.byref(t), vocab, width, _ELEM[dY.dtype], _ids(ids, dY.shape[:-1], dev), py, sy,
+                                     scale, G.data_ptr(), sg)
+    if rc:
+        h._check(rc)
+    return G
+
+
+def _heads(width: int, q_heads: int, k_heads: int, base: float, eps: float) -> _Heads:
+    heads = q_heads + k_heads
+    if q_heads < 0 or k_heads < 0 or heads < 1 or width % heads:
+        raise ValueError("rows of %d features are not those of %d + %d heads" % (width, q_heads, k_heads))
+    return _Heads(q_heads, k_heads, width // heads, base, eps)
+
+
+def cdgrab_headnorm(h: Handle, X: torch.Tensor, gain_q: Optional[torch.Tensor] = None,
+                    gain_k: Optional[torch.Tensor] = None, *, q_heads: int, k_heads: int, eps: float = 1e-6,
+                    base: float = 10000.0, first: Optional[torch.Tensor] = None, count: Optional[torch.Tensor] = None,
+                    tokens: Optional[int] = None, Y: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Norm of every head's features (root mean square, gains [dim] float32 for queries and keys) and rotation by the row's
+    position in its example (``base`` 0: none).  X[..., (q_heads + k_heads) * dim] holds the queries' heads and behind them the
+    keys'; rows of examples as in cdgrab_pergrad_layernorm.  Rows of no example keep what Y holds (zero where the call makes Y)."""
+    dev = h.device
+    px, rows, width, sx = _rows(X, "X", dev)
+    t = _token_rows(X, rows, first, count, tokens, dev)
+    s = _heads(width, q_heads, k_heads, base, eps)
+    if Y is None:
+        Y = _made_like(h, X, X.shape, X.dtype, first is not None or count is not None)
+        py, sy = Y.data_ptr(), width or 1
+    else:
+        py, _, _, sy = _rows(Y, "Y", dev, X)
+    rc = h._lib.cdgrab_headnorm(h._h, ctypes.byref(t), ctypes.byref(s), _ELEM[X.dtype], px, sx,
+                                _vector(gain_q, s.dim, "gain_q", dev), _vector(gain_k, s.dim, "gain_k", dev), py, sy)
+    if rc:
+        h._check(rc)
+    return Y
+
+
+def cdgrab_pergrad_headnorm(h: Handle, X: torch.Tensor, dY: torch.Tensor, gain_q: Optional[torch.Tensor] = None,
+                            gain_k: Optional[torch.Tensor] = None, *, q_heads: int, k_heads: int, eps: float = 1e-6,
+                            base: float = 10000.0, first: Optional[torch.Tensor] = None,
+                            count: Optional[torch.Tensor] = None, tokens: Optional[int] = None,
+                            dX: Optional[torch.Tensor] = None, G_out: Optional[torch.Tensor] = None,
+                            want_dx: bool = True, want_grads: bool = True):
+    """Backward pass of cdgrab_headnorm: (dX, G), G[examples][gain_q's gradient | gain_k's gradient], 2 * dim wide."""
+    dev = h.device
+    px, rows, width, sx = _rows(X, "X", dev)
+    py, _, _, sy = _rows(dY, "dY", dev, X)
+    t = _token_rows(X, rows, first, count, tokens, dev)
+    s = _heads(width, q_heads, k_heads, base, eps)
+    pd, sd = None, width
+    if dX is not None:
+        pd, _, _, sd = _rows(dX, "dX", dev, X)
+    elif want_dx:
+        dX = _made_like(h, X, X.shape, X.dtype, first is not None or count is not None)
+        pd, sd = dX.data_ptr(), width or 1
+    G, pg, sg = None, None, 0
+    if G_out is not None or want_grads:
+        G, sg = _grad_rows(h, G_out, t.examples, 2 * s.dim)
+        pg = G.data_ptr()
+    rc = h._lib.cdgrab_pergrad_headnorm(h._h, ctypes.byref(t), ctypes.byref(s), _ELEM[X.dtype], px, sx, py, sy,
+                                        _vector(gain_q, s.dim, "gain_q", dev), _vector(gain_k, s.dim, "gain_k", dev), pd, sd,
+                                        pg, sg)
+    if rc:
+        h._check(rc)
+    return dX, G
+
+
+def _attention_rows(h, Q, K, V, q_heads, kv_heads, scale, first, count, tokens):
+    """(spans, head dim, scale, [pointer, stride] of Q, K and V)"""
+    dev = h.device
+    pq, rows, qw, sq = _rows(Q, "Q", dev)
+    if q_heads < 1 or kv_heads < 1 or q_heads % kv_heads or qw % q_heads:
+        raise ValueError("rows of %d features and %d heads of queries on %d of keys do not go together" % (qw, q_heads, kv_heads))
+    dim = qw // q_heads
+    at = [pq, sq]
+    for x, name in ((K, "K"), (V, "V")):
+        if x.dtype != Q.dtype or tuple(x.shape) != (*Q.shape[:-1], kv_heads * dim):
+            raise ValueError("%s must be %s %s, got %s %s" % (name, Q.dtype, (*Q.shape[:-1], kv_heads * dim), x.dtype, tuple(x.shape)))
+        p, _, _, sx = _rows(x, name, dev)
+        at += [p, sx]
+    return _token_rows(Q, rows, first, count, tokens, dev), dim, dim ** -0.5 if scale is None and dim else scale or 0.0, at
+
+
+def _rows_or_made(h, t, name, like, partly):
+    """(tensor, pointer, stride) of an output of the type and shape of `like`."""
+    if t is None:
+        t = _made_like(h, like, like.shape, like.dtype, partly)
+        return t, t.data_ptr(), like.shape[-1] or 1
+    p, _, _, s = _rows(t, name, h.device, like)
+    return t, p, s
+
+
+def cdgrab_attention(h: Handle, Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, *, q_heads: int, kv_heads: int,
+                     scale: Optional[float] = None, first: Optional[torch.Tensor] = None,
+                     count: Optional[torch.Tensor] = None, tokens: Optional[int] = None, O: Optional[torch.Tensor] = None,
+                     want_lse: bool = True):
+    """Causal attention within each example: (O, lse).  Q[..., q_heads * dim], K and V[..., kv_heads * dim], lse[..., q_heads]
+    float32 (logarithms of the sums, for the backward pass); ``scale`` is 1 / sqrt(dim) by default; rows of examples as in
+    cdgrab_pergrad_layernorm.  Rows of no example keep what O holds (zero where the call makes it, and in lse)."""
+    t, dim, scale, at = _attention_rows(h, Q, K, V, q_heads, kv_heads, scale, first, count, tokens)
+    partly = first is not None or count is not None
+    O, po, so = _rows_or_made(h, O, "O", Q, partly)
+    lse = _made_like(h, Q, (*Q.shape[:-1], q_heads), torch.float32, partly) if want_lse else None
+    rc = h._lib.cdgrab_attention(h._h, ctypes.byref(t), q_heads, kv_heads, dim, _ELEM[Q.dtype], scale, *at, po, so,
+                                 lse.data_ptr() if want_lse else None)
+    if rc:
+        h._check(rc)
+    return O, lse
+
+
+def cdgrab_attention_backward(h: Handle, Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, O: torch.Tensor,
+                              lse: torch.Tensor, dO: torch.Tensor, *, q_heads: int, kv_heads: int,
+                              scale: Optional[float] = None, first: Optional[torch.Tensor] = None,
+                              count: Optional[torch.Tensor] = None, tokens: Optional[int] = None,
+                              dQ: Optional[torch.Tensor] = None, dK: Optional[torch.Tensor] = None,
+                              dV: Optional[torch.Tensor] = None):
+    """Backward pass of cdgrab_attention from its outputs O and lse and the gradient dO: (dQ, dK, dV), which may be given, as
+    stretches of one array's rows too.  Rows of no example keep what they hold (zero where the call makes them)."""
+    t, dim, scale, at = _attention_rows(h, Q, K, V, q_heads, kv_heads, scale, first, count, tokens)
+    po, _, _, so = _rows(O, "O", h.device, Q)
+    pg, _, _, sg = _rows(dO, "dO", h.device, Q)
+    pl = _ptr(lse, torch.float32, (*Q.shape[:-1], q_heads), "lse", h.device)
+    partly = first is not None or count is not None
+    dQ, pq, sq = _rows_or_made(h, dQ, "dQ", Q, partly)
+    dK, pk, sk = _rows_or_made(h, dK, "dK", K, partly)
+    dV, pv, sv = _rows_or_made(h, dV, "dV", V, partly)
+    rc = h._lib.cdgrab_attention_backward(h._h, ctypes.byref(t), q_heads, kv_heads, dim, _ELEM[Q.dtype], scale, *at, po, so, pl,
+                                          pg, sg, pq, sq, pk, sk, pv, sv)
+    if rc:
+        h._check(rc)
+    return dQ, dK, dV
 
 
 def cdgrab_train_epoch_softmax_orthogonal(h: Handle, X: torch.Tensor, y: torch.Tensor, W: torch.Tensor,

@@ -26,6 +26,9 @@
 #include "norm_kernels.hpp"
 #include "linear_kernels.hpp"
 #include "ortho_kernels.hpp"
+#include "embed_kernels.hpp"
+#include "headnorm_kernels.hpp"
+#include "attention_kernels.hpp"
 
 using namespace cdgrab;
 
@@ -743,6 +746,7 @@ int launch_column_mean(cdgrab_handle *h, int64_t n, int64_t d, const float *rows
 }  // namespace
 
 #include "layer_entries.hpp"
+#include "sequence_entries.hpp"
 
 extern "C" {
 

@@ -1,0 +1,181 @@
+// Norms of queries and keys with the position rotation, for each head of a row: forward, and backward with the gains' gradient of
+// every example.
+//
+//   r = 1 / sqrt(mean(x^2) + eps), h = x r, u = gain h, and pairs (u_i, u_{i + dim/2}) turned by the angle pos base^(-2 i / dim):
+//   y_i = u_i cos - u_{i + dim/2} sin,  y_{i + dim/2} = u_{i + dim/2} cos + u_i sin
+//   back: u = dy turned by the negative angle, g = gain u, dx = r (g - h mean(g h)), dgain = sum over rows and heads of u h
+//
+// Bound by bytes: x in and y out; x and dy in, dx out.  A head's features lie in the registers of LANES threads, each with the same
+// places of both halves, so that a pair is in one thread.  The angles' cosines and sines are the same for all heads: a workgroup
+// computes those of its rows once, into LDS.  Sums in fp32, results are rounded once.
+#pragma once
+#include "norm_kernels.hpp"
+
+namespace cdgrab {
+
+constexpr int kHeadMaxDim = 512, kHeadThreads = 256;
+constexpr int kHeadTable = 2048;  // angles of a workgroup's rows at a time
+
+// Turns per position, as fractions of 2^64: position * turn modulo 2^64 is the angle exactly up to the rounding of `turn`, also
+// where an fp32 angle of a far position would have no digits left.
+struct HeadTurns { uint64_t turn[kHeadMaxDim / 2]; };
+
+// cos and sin of a fraction of a turn: the nearest quarter turn is taken off in whole numbers, the rest (up to an eighth) goes into
+// the series of both functions, the first terms left out below 3e-9.
+__device__ __forceinline__ float2 cos_sin_turns(uint64_t turns) {
+    const uint32_t quarter = (uint32_t)((turns + ((uint64_t)1 << 61)) >> 62);
+    const int32_t rest = (int32_t)((turns - ((uint64_t)quarter << 62)) >> 32);
+    const float x = (float)rest * 1.46291807926715968e-9f, x2 = x * x;  // 2 pi / 2^32
+    float s = fmaf(x2, 1.f / 362880.f, -1.f / 5040.f);
+    s = fmaf(x2, s, 1.f / 120.f);
+    s = fmaf(x2, s, -1.f / 6.f);
+    s = fmaf(x * x2, s, x);
+    float c = fmaf(x2, -1.f / 3628800.f, 1.f / 40320.f);
+    c = fmaf(x2, c, -1.f / 720.f);
+    c = fmaf(x2, c, 1.f / 24.f);
+    c = fmaf(x2, c, -0.5f);
+    c = fmaf(x2, c, 1.f);
+    const float a = quarter & 1 ? s : c, b = quarter & 1 ? c : s;
+    return make_float2((quarter + 1) & 2 ? -a : a, quarter & 2 ? -b : b);
+}
+
+struct HeadShape {
+    int q_heads, heads, half;  // queries' heads, queries' and keys', half of a head's features
+    int rows;                  // rows at a time
+    float eps;
+};
+
+// Cosines and sines of `rows` positions from `at` on.
+__device__ __forceinline__ void head_angles(float2 *table, const HeadTurns &turns, int64_t at, int rows, int half) {
+    for (int q = threadIdx.x; q < rows * half; q += kHeadThreads) {
+        const int r = q / half, i = q - r * half;
+        table[q] = cos_sin_turns((uint64_t)(at + r) * turns.turn[i]);
+    }
+}
+
+// Workgroup b takes chunk b % chunks of the rows of example b / chunks, `rows` rows at a time; LANES threads a head.
+// BACKWARD: DY and DX in the place of Y; the gains' gradients [2][dim] to G or to `partial` [examples][chunks][2 dim].
+template <typename T, int VEC, int LANES, bool BACKWARD>
+__global__ __launch_bounds__(kHeadThreads) void head_norm(
+    TokenRows tok, int chunks, HeadShape sh, HeadTurns turns, const T *__restrict__ X, int64_t x_stride, const T *__restrict__ DY,
+    int64_t dy_stride, const float *__restrict__ gain_q, const float *__restrict__ gain_k, T *__restrict__ Y, int64_t y_stride,
+    float *__restrict__ G, int64_t g_stride, float *__restrict__ partial)
+{
+    constexpr int GROUPS = kHeadThreads / LANES;
+    __shared__ float2 table[kHeadTable];
+    __shared__ float part[BACKWARD ? GROUPS * LANES * VEC : 1];
+    const int t = threadIdx.x % LANES, mine = threadIdx.x / LANES, half = sh.half;
+    const NormSlice<VEC, LANES, 1> sl(t, half);
+    const int pos = sl.pos[0];
+    const int64_t e = tok.base + blockIdx.x / chunks;
+    const int c = (int)(blockIdx.x % chunks);
+    const RowSpan span = rows_of(tok, e);
+    const int64_t per = ((span.count + chunks - 1) / chunks + sh.rows - 1) / sh.rows * sh.rows;
+    const int64_t t0 = c * per < span.count ? c * per : span.count, t1 = t0 + per < span.count ? t0 + per : span.count;
+    float wq[2][VEC], wk[2][VEC], dq[2][VEC], dk[2][VEC];
+#pragma unroll
+    for (int p = 0; p < 2; ++p)
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+            wq[p][j] = gain_q ? gain_q[p * half + pos + j] : 1.f;
+            wk[p][j] = gain_k ? gain_k[p * half + pos + j] : 1.f;
+            dq[p][j] = dk[p][j] = 0.f;
+        }
+    const float inv = 0.5f / (float)half;
+    for (int64_t at = t0; at < t1; at += sh.rows) {
+        const int rows = (int)(t1 - at < sh.rows ? t1 - at : sh.rows);
+        __syncthreads();  // (the last rows' angles have been read)
+        head_angles(table, turns, at, rows, half);
+        __syncthreads();
+        const int items = rows * sh.heads;
+        for (int base = 0; base < items; base += GROUPS) {
+            const int item = base + mine < items ? base + mine : items - 1;
+            const bool live = base + mine < items;
+            const int r = item / sh.heads, head = item - r * sh.heads;
+            const bool query = head < sh.q_heads;
+            const int64_t row = span.first + at + r;
+            const int64_t off = (int64_t)head * 2 * half + pos;
+            T x[2][VEC], dy[2][VEC];
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+                load_any<T, VEC>(X + row * x_stride + off + p * half, x[p]);
+                if constexpr (BACKWARD) load_any<T, VEC>(DY + row * dy_stride + off + p * half, dy[p]);
+            }
+            const float2 *turn = table + r * half + pos;
+            if constexpr (!BACKWARD) {
+                float ss = 0.f;
+#pragma unroll
+                for (int p = 0; p < 2; ++p)
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) ss = sl.own(0, j) ? fmaf((float)x[p][j], (float)x[p][j], ss) : ss;
+                ss = lanes_sum<LANES>(ss);
+                const float rs = 1.f / sqrtf(fmaf(ss, inv, sh.eps)) + (ss - ss);  // (NaN of a sum that is not finite)
+                T y[2][VEC];
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    const float2 cs = turn[j];
+                    const float a = (float)x[0][j] * rs * (query ? wq[0][j] : wk[0][j]), b = (float)x[1][j] * rs * (query ? wq[1][j] : wk[1][j]);
+                    y[0][j] = (T)fmaf(a, cs.x, -(b * cs.y));
+                    y[1][j] = (T)fmaf(b, cs.x, a * cs.y);
+                }
+                if (live && sl.any(0))
+#pragma unroll
+                    for (int p = 0; p < 2; ++p) store_any<T, VEC>(Y + row * y_stride + off + p * half, y[p]);
+            } else {
+                float u[2][VEC], s[2] = {0.f, 0.f};  // sums of x^2, g x
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    const float2 cs = turn[j];
+                    const float a = (float)dy[0][j], b = (float)dy[1][j];
+                    u[0][j] = fmaf(a, cs.x, b * cs.y);
+                    u[1][j] = fmaf(b, cs.x, -(a * cs.y));
+#pragma unroll
+                    for (int p = 0; p < 2; ++p) {
+                        const float v = sl.own(0, j) ? (float)x[p][j] : 0.f;
+                        s[0] = fmaf(v, v, s[0]);
+                        s[1] = fmaf(u[p][j] * (query ? wq[p][j] : wk[p][j]), v, s[1]);
+                    }
+                }
+                s[0] = lanes_sum<LANES>(s[0]);
+                s[1] = lanes_sum<LANES>(s[1]);
+                const float rs = 1.f / sqrtf(fmaf(s[0], inv, sh.eps)) + (s[0] - s[0]);
+                const float mean = s[1] * rs * inv;
+#pragma unroll
+                for (int p = 0; p < 2; ++p) {
+                    T out[VEC];
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) {
+                        const float hat = (float)x[p][j] * rs;
+                        out[j] = (T)(rs * fmaf(u[p][j], query ? wq[p][j] : wk[p][j], -(hat * mean)));
+                        const float add = u[p][j] * hat;
+                        if (live) {
+                            if (query) dq[p][j] += add;
+                            else dk[p][j] += add;
+                        }
+                    }
+                    if (Y && live && sl.any(0)) store_any<T, VEC>(Y + row * y_stride + off + p * half, out);
+                }
+            }
+        }
+    }
+    if constexpr (BACKWARD) {
+        if (!G && !partial) return;
+        float *to = chunks > 1 ? partial + (e * chunks + c) * 4 * half : G + e * g_stride;
+#pragma unroll
+        for (int which = 0; which < 4; ++which) {
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < VEC; ++j)
+                if (sl.own(0, j)) part[mine * LANES * VEC + pos + j] = which < 2 ? dq[which & 1][j] : dk[which & 1][j];
+            __syncthreads();
+            for (int col = threadIdx.x; col < half; col += kHeadThreads) {
+                float sum = 0.f;
+#pragma unroll 8
+                for (int g = 0; g < GROUPS; ++g) sum += part[g * LANES * VEC + col];
+                to[which * half + col] = sum;
+            }
+        }
+    }
+}
+
+}  // namespace cdgrab

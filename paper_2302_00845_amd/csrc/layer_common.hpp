@@ -67,10 +67,10 @@ __device__ __forceinline__ float dpp_add_f32(float x) {
 }
 template <int LANES>
 __device__ __forceinline__ float lanes_sum(float x) {
-    static_assert(LANES == 8 || LANES == 16 || LANES == 32 || LANES == 64, "");
-    x = dpp_add_f32<0xB1>(x);   // quad_perm 1 0 3 2
-    x = dpp_add_f32<0x4E>(x);   // quad_perm 2 3 0 1
-    x = dpp_add_f32<0x141>(x);  // row_half_mirror
+    static_assert(LANES >= 1 && LANES <= 64 && (LANES & (LANES - 1)) == 0, "");
+    if constexpr (LANES >= 2) x = dpp_add_f32<0xB1>(x);   // quad_perm 1 0 3 2
+    if constexpr (LANES >= 4) x = dpp_add_f32<0x4E>(x);   // quad_perm 2 3 0 1
+    if constexpr (LANES >= 8) x = dpp_add_f32<0x141>(x);  // row_half_mirror
     if constexpr (LANES >= 16) x = dpp_add_f32<0x140>(x);  // row_mirror
     if constexpr (LANES >= 32) {
         const auto p = __builtin_amdgcn_permlane16_swap(__float_as_int(x), __float_as_int(x), false, false);
