@@ -491,7 +491,7 @@ int cdgrab_pergrad_headnorm(cdgrab_handle *h, const cdgrab_token_rows *t, const 
 /* Causal attention within each example: for query i of a head, over the example's rows j <= i,
  *     s_ij = scale * Q_i . K_j,   lse_i = ln sum_j exp(s_ij),   O_i = sum_j exp(s_ij - lse_i) V_j;
  * q_heads / kv_heads consecutive heads of queries share a head of keys and values.
- *   Q, O [rows][q_heads * dim], K, V [rows][kv_heads * dim] of `type` dev; lse [rows][q_heads] fp32 dev, or NULL: not wanted.
+ *   Q, O [rows][q_heads * dim], K, V [rows][kv_heads * dim] of `type` dev; lse [q_heads][rows] fp32 dev, or NULL: not wanted.
  * Products of bf16 and fp16 elements are exact, those of fp32 elements good to 2^-23; exponentials are rounded to `type`
  * (fp32: to 2^-24) where they are multiplied with V, sums are fp32.  An element that is not finite makes the results it enters infinite
  * or NaN, and may do so to those of up to 127 rows before it in its example.

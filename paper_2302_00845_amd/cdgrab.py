@@ -757,13 +757,13 @@ def cdgrab_attention(h: Handle, Q: torch.Tensor, K: torch.Tensor, V: torch.Tenso
                      scale: Optional[float] = None, first: Optional[torch.Tensor] = None,
                      count: Optional[torch.Tensor] = None, tokens: Optional[int] = None, O: Optional[torch.Tensor] = None,
                      want_lse: bool = True):
-    """Causal attention within each example: (O, lse).  Q[..., q_heads * dim], K and V[..., kv_heads * dim], lse[..., q_heads]
+    """Causal attention within each example: (O, lse).  Q[..., q_heads * dim], K and V[..., kv_heads * dim], lse[q_heads, ...]
     float32 (logarithms of the sums, for the backward pass); ``scale`` is 1 / sqrt(dim) by default; rows of examples as in
     cdgrab_pergrad_layernorm.  Rows of no example keep what O holds (zero where the call makes it, and in lse)."""
     t, dim, scale, at = _attention_rows(h, Q, K, V, q_heads, kv_heads, scale, first, count, tokens)
     partly = first is not None or count is not None
     O, po, so = _rows_or_made(h, O, "O", Q, partly)
-    lse = _made_like(h, Q, (*Q.shape[:-1], q_heads), torch.float32, partly) if want_lse else None
+    lse = _made_like(h, Q, (q_heads, *Q.shape[:-1]), torch.float32, partly) if want_lse else None
     rc = h._lib.cdgrab_attention(h._h, ctypes.byref(t), q_heads, kv_heads, dim, _ELEM[Q.dtype], scale, *at, po, so,
                                  lse.data_ptr() if want_lse else None)
     if rc:
@@ -782,7 +782,7 @@ def cdgrab_attention_backward(h: Handle, Q: torch.Tensor, K: torch.Tensor, V: to
     t, dim, scale, at = _attention_rows(h, Q, K, V, q_heads, kv_heads, scale, first, count, tokens)
     po, _, _, so = _rows(O, "O", h.device, Q)
     pg, _, _, sg = _rows(dO, "dO", h.device, Q)
-    pl = _ptr(lse, torch.float32, (*Q.shape[:-1], q_heads), "lse", h.device)
+    pl = _ptr(lse, torch.float32, (q_heads, *Q.shape[:-1]), "lse", h.device)
     partly = first is not None or count is not None
     dQ, pq, sq = _rows_or_made(h, dQ, "dQ", Q, partly)
     dK, pk, sk = _rows_or_made(h, dK, "dK", K, partly)

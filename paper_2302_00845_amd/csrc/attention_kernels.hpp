@@ -25,8 +25,9 @@ constexpr int kAttRows = 128;  // queries (keys) of a workgroup, 32 a wavefront
 constexpr int kAttMaxDim = 128;
 
 struct AttHeads {
-    int64_t pairs;      // examples of the launch * kv_heads
-    int kv_heads, group;  // queries' heads that share keys and values
+    int64_t pairs, unit0;  // examples * kv_heads; the launch's first workgroup
+    int tiles;             // of kAttRows rows that an example has at most
+    int kv_heads, group;   // queries' heads that share keys and values
     int dim;
     float scale;
 };
@@ -116,11 +117,11 @@ struct AttStage {
     static constexpr int LEN = P::N * PLANE;
     T v[PER][8];
     // rows `at` .. of `base`, those from `end` on are zero and not read
-    __device__ __forceinline__ void load(const T *base, int64_t stride, int64_t at, int64_t end, int dim) {
+    __device__ __forceinline__ void load(const T *base, int64_t stride, int at, int end, int dim) {
 #pragma unroll
         for (int q = 0; q < PER; ++q) {
             const int i = threadIdx.x + q * kAttThreads, r = i / USED, piece = i % USED;
-            att_piece<T>(base + (at + r) * stride, piece * 8, dim, (TOTAL % kAttThreads == 0 || i < TOTAL) && at + r < end, v[q]);
+            att_piece<T>(base + (int64_t)(at + r) * stride, piece * 8, dim, (TOTAL % kAttThreads == 0 || i < TOTAL) && at + r < end, v[q]);
         }
     }
     __device__ __forceinline__ void store(E *lds) const {
@@ -134,6 +135,84 @@ struct AttStage {
             for (int p = 0; p < P::N; ++p)
                 *reinterpret_cast<typename AttFrag<T>::vec *>(lds + p * PLANE + r * L::LD + (piece ^ L::swap(r)) * 8) = f.v[p];
         }
+    }
+};
+
+// Two operands' tiles of ROWS rows on their way to LDS.  DIRECT (16-bit elements in whole, aligned pieces): from memory to LDS without
+// registers, a tile ahead, into the other of two buffers; otherwise through registers, where fp32 elements are split.  Rows from `end` on
+// are zero, or with DIRECT the last one again: they meet weights of zero.
+template <typename T, int D, int ROWS, bool DIRECT>
+struct AttPipe {
+    typedef AttStage<T, D, ROWS> Stage;
+    typedef typename Stage::E E;
+    static constexpr int LEN = 2 * Stage::LEN, LDS = LEN;
+    Stage a, b;
+    E *lds;
+    int dim;
+    __device__ __forceinline__ AttPipe(E *lds, int dim, int64_t, int64_t) : lds(lds), dim(dim) {}
+    __device__ __forceinline__ void fetch(const T *A, int64_t a_stride, const T *B, int64_t b_stride, int at, int end) {
+        a.load(A, a_stride, at, end, dim);
+        b.load(B, b_stride, at, end, dim);
+    }
+    // The tile fetched last, for the whole workgroup; then the next one may be fetched.
+    __device__ __forceinline__ const E *turn() {
+        __syncthreads();  // (the last tile has been read)
+        a.store(lds);
+        b.store(lds + Stage::LEN);
+        __syncthreads();
+        return lds;
+    }
+};
+template <typename T, int D, int ROWS>
+struct AttPipe<T, D, ROWS, true> {
+    typedef AttLayout<D> L;
+    typedef typename LinearPlanes<T>::elem E;
+    static constexpr int ONE = ROWS * L::LD, LEN = 2 * ONE, LDS = 2 * LEN, CALLS = ROWS * L::PIECES / kAttThreads;
+    static_assert(LinearPlanes<T>::N == 1 && CALLS * kAttThreads == ROWS * L::PIECES, "");
+    E *lds;
+    int buf = 0, row[CALLS];
+    uint32_t piece[CALLS], at_a[CALLS], at_b[CALLS];  // bytes
+    bool there[CALLS];
+    __device__ __forceinline__ AttPipe(E *lds, int dim, int64_t a_stride, int64_t b_stride) : lds(lds) {
+        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+#pragma unroll
+        for (int q = 0; q < CALLS; ++q) {
+            const int slot = (q * (kAttThreads / 64) + wave) * 64 + lane;
+            row[q] = slot / L::PIECES;
+            const int p = slot % L::PIECES ^ L::swap(row[q]);
+            there[q] = p * 8 < dim;
+            piece[q] = p * 16;
+            at_a[q] = (uint32_t)(row[q] * (int)a_stride * 2) + piece[q];
+            at_b[q] = (uint32_t)(row[q] * (int)b_stride * 2) + piece[q];
+        }
+        if (dim < D) {  // uniform: what is never loaded is zero
+            typedef uint32_t words __attribute__((ext_vector_type(4)));
+            for (int i = threadIdx.x; i < LDS / 8; i += kAttThreads) reinterpret_cast<words *>(lds)[i] = words{0, 0, 0, 0};
+            __syncthreads();
+        }
+    }
+    __device__ __forceinline__ void one(const T *from, int64_t stride, const uint32_t (&offset)[CALLS], E *to, int at, int end) const {
+        typedef __attribute__((address_space(3))) void *Lds;
+        typedef const __attribute__((address_space(1))) void *Mem;
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const char *base = reinterpret_cast<const char *>(from + at * stride);
+        const bool whole = at + ROWS <= end;  // uniform
+#pragma unroll
+        for (int q = 0; q < CALLS; ++q) {
+            uint32_t o = offset[q];
+            if (!whole) o = (uint32_t)((row[q] < end - at ? row[q] : end - at - 1) * (int)stride * 2) + piece[q];
+            if (there[q]) __builtin_amdgcn_global_load_lds((Mem)(base + o), (Lds)(to + (q * (kAttThreads / 64) + wave) * 512), 16, 0, 0);
+        }
+    }
+    __device__ __forceinline__ void fetch(const T *A, int64_t a_stride, const T *B, int64_t b_stride, int at, int end) const {
+        one(A, a_stride, at_a, lds + buf * LEN, at, end);
+        one(B, b_stride, at_b, lds + buf * LEN + ONE, at, end);
+    }
+    __device__ __forceinline__ const E *turn() {
+        stage_barrier<0>();
+        const E *now = lds + buf * LEN;
+        buf ^= 1;
+        return now;
     }
 };
 
@@ -177,6 +256,115 @@ struct AttRead {
     }
 };
 
+// The `across` operands of 32 rows, all features.  DIRECT: read at once and waited for, in one piece of assembly each 32 or 64 features:
+// in front of a transposing read by its builtin the compiler waits for all loads to LDS that are on their way, the next tile's
+// (it cannot see that they go elsewhere), which took away what fetching ahead brings.
+template <typename T, int D, int ROWS, bool DIRECT>
+struct AttAcross {
+    const AttRead<T, D, ROWS> &read;
+    const typename AttRead<T, D, ROWS>::E *tile;
+    int first;
+    __device__ __forceinline__ AttAcross(const AttRead<T, D, ROWS> &read, const typename AttRead<T, D, ROWS>::E *tile, int first)
+        : read(read), tile(tile), first(first) {}
+    __device__ __forceinline__ AttFrag<T> get(int step, int d) const { return read.across(tile, first + step * 16, d); }
+};
+template <typename T, int D, int ROWS>
+struct AttAcross<T, D, ROWS, true> {
+    typedef AttLayout<D> L;
+    typedef typename LinearPlanes<T>::elem E;
+    s16x4 v[2][D / 32][2];
+    __device__ __forceinline__ AttAcross(const AttRead<T, D, ROWS> &read, const E *tile, int first) {
+        typedef const __attribute__((address_space(3))) E *Ptr;
+        constexpr int ROW = L::LD * 2;  // bytes
+        const uint32_t base = (uint32_t)(uintptr_t)(Ptr)(tile + first * L::LD + read.token);
+#pragma unroll
+        for (int d = 0; d < D / 32; d += 2) {
+            const uint32_t lo = base + 2 * (read.lo ^ (d * 32)), hi = base + 2 * (read.hi ^ (d * 32));
+            if constexpr (D == 32) {
+                asm volatile("ds_read_b64_tr_b16 %0, %4\n\tds_read_b64_tr_b16 %1, %5 offset:%6\n\t"
+                             "ds_read_b64_tr_b16 %2, %4 offset:%7\n\tds_read_b64_tr_b16 %3, %5 offset:%8\n\ts_waitcnt lgkmcnt(0)"
+                             : "=&v"(v[0][0][0]), "=&v"(v[0][0][1]), "=&v"(v[1][0][0]), "=&v"(v[1][0][1])
+                             : "v"(lo), "v"(hi), "n"(8 * ROW), "n"(16 * ROW), "n"(24 * ROW)
+                             : "memory");
+            } else if (d + 1 < D / 32) {
+                const uint32_t lo1 = base + 2 * (read.lo ^ (d * 32 + 32)), hi1 = base + 2 * (read.hi ^ (d * 32 + 32));
+                asm volatile("ds_read_b64_tr_b16 %0, %8\n\tds_read_b64_tr_b16 %1, %9 offset:%12\n\t"
+                             "ds_read_b64_tr_b16 %2, %10\n\tds_read_b64_tr_b16 %3, %11 offset:%12\n\t"
+                             "ds_read_b64_tr_b16 %4, %8 offset:%13\n\tds_read_b64_tr_b16 %5, %9 offset:%14\n\t"
+                             "ds_read_b64_tr_b16 %6, %10 offset:%13\n\tds_read_b64_tr_b16 %7, %11 offset:%14\n\ts_waitcnt lgkmcnt(0)"
+                             : "=&v"(v[0][d][0]), "=&v"(v[0][d][1]), "=&v"(v[0][d + 1][0]), "=&v"(v[0][d + 1][1]), "=&v"(v[1][d][0]),
+                               "=&v"(v[1][d][1]), "=&v"(v[1][d + 1][0]), "=&v"(v[1][d + 1][1])
+                             : "v"(lo), "v"(hi), "v"(lo1), "v"(hi1), "n"(8 * ROW), "n"(16 * ROW), "n"(24 * ROW)
+                             : "memory");
+            } else {
+                asm volatile("ds_read_b64_tr_b16 %0, %4\n\tds_read_b64_tr_b16 %1, %5 offset:%6\n\t"
+                             "ds_read_b64_tr_b16 %2, %4 offset:%7\n\tds_read_b64_tr_b16 %3, %5 offset:%8\n\ts_waitcnt lgkmcnt(0)"
+                             : "=&v"(v[0][d][0]), "=&v"(v[0][d][1]), "=&v"(v[1][d][0]), "=&v"(v[1][d][1])
+                             : "v"(lo), "v"(hi), "n"(8 * ROW), "n"(16 * ROW), "n"(24 * ROW)
+                             : "memory");
+            }
+        }
+    }
+    __device__ __forceinline__ AttFrag<T> get(int step, int d) const {
+        AttFrag<T> f;
+        f.v[0] = __builtin_bit_cast(typename AttFrag<T>::vec, __builtin_shufflevector(v[step][d][0], v[step][d][1], 0, 1, 2, 3, 4, 5, 6, 7));
+        return f;
+    }
+};
+
+// The `across` operands of 16 rows of two tiles, `apart` elements from each other; DIRECT as above.
+template <typename T, int D, int ROWS, bool DIRECT>
+struct AttAcrossBoth {
+    const AttRead<T, D, ROWS> &read;
+    const typename AttRead<T, D, ROWS>::E *a, *b;
+    int first;
+    __device__ __forceinline__ AttAcrossBoth(const AttRead<T, D, ROWS> &read, const typename AttRead<T, D, ROWS>::E *a,
+                                             const typename AttRead<T, D, ROWS>::E *b, int first) : read(read), a(a), b(b), first(first) {}
+    __device__ __forceinline__ AttFrag<T> get_a(int d) const { return read.across(a, first, d); }
+    __device__ __forceinline__ AttFrag<T> get_b(int d) const { return read.across(b, first, d); }
+};
+template <typename T, int D, int ROWS>
+struct AttAcrossBoth<T, D, ROWS, true> {
+    typedef AttLayout<D> L;
+    typedef typename LinearPlanes<T>::elem E;
+    s16x4 v[2][D / 32][2];
+    // (b lies behind a in AttPipe's buffers)
+    __device__ __forceinline__ AttAcrossBoth(const AttRead<T, D, ROWS> &read, const E *a, const E *, int first) {
+        typedef const __attribute__((address_space(3))) E *Ptr;
+        constexpr int ROW = L::LD * 2, APART = ROWS * ROW;  // bytes
+        const uint32_t base = (uint32_t)(uintptr_t)(Ptr)(a + first * L::LD + read.token);
+#pragma unroll
+        for (int d = 0; d < D / 32; d += 2) {
+            const uint32_t lo = base + 2 * (read.lo ^ (d * 32)), hi = base + 2 * (read.hi ^ (d * 32));
+            if (d + 1 < D / 32) {
+                const int e = d + 1 < D / 32 ? d + 1 : d;  // (the compiler looks at it for D = 32 as well)
+                const uint32_t lo1 = base + 2 * (read.lo ^ (e * 32)), hi1 = base + 2 * (read.hi ^ (e * 32));
+                asm volatile("ds_read_b64_tr_b16 %0, %8\n\tds_read_b64_tr_b16 %1, %9 offset:%12\n\t"
+                             "ds_read_b64_tr_b16 %2, %10\n\tds_read_b64_tr_b16 %3, %11 offset:%12\n\t"
+                             "ds_read_b64_tr_b16 %4, %8 offset:%13\n\tds_read_b64_tr_b16 %5, %9 offset:%14\n\t"
+                             "ds_read_b64_tr_b16 %6, %10 offset:%13\n\tds_read_b64_tr_b16 %7, %11 offset:%14\n\ts_waitcnt lgkmcnt(0)"
+                             : "=&v"(v[0][d][0]), "=&v"(v[0][d][1]), "=&v"(v[0][e][0]), "=&v"(v[0][e][1]), "=&v"(v[1][d][0]),
+                               "=&v"(v[1][d][1]), "=&v"(v[1][e][0]), "=&v"(v[1][e][1])
+                             : "v"(lo), "v"(hi), "v"(lo1), "v"(hi1), "n"(8 * ROW), "n"(APART), "n"(APART + 8 * ROW)
+                             : "memory");
+            } else {
+                asm volatile("ds_read_b64_tr_b16 %0, %4\n\tds_read_b64_tr_b16 %1, %5 offset:%6\n\t"
+                             "ds_read_b64_tr_b16 %2, %4 offset:%7\n\tds_read_b64_tr_b16 %3, %5 offset:%8\n\ts_waitcnt lgkmcnt(0)"
+                             : "=&v"(v[0][d][0]), "=&v"(v[0][d][1]), "=&v"(v[1][d][0]), "=&v"(v[1][d][1])
+                             : "v"(lo), "v"(hi), "n"(8 * ROW), "n"(APART), "n"(APART + 8 * ROW)
+                             : "memory");
+            }
+        }
+    }
+    __device__ __forceinline__ AttFrag<T> get(int which, int d) const {
+        AttFrag<T> f;
+        f.v[0] = __builtin_bit_cast(typename AttFrag<T>::vec, __builtin_shufflevector(v[which][d][0], v[which][d][1], 0, 1, 2, 3, 4, 5, 6, 7));
+        return f;
+    }
+    __device__ __forceinline__ AttFrag<T> get_a(int d) const { return get(0, d); }
+    __device__ __forceinline__ AttFrag<T> get_b(int d) const { return get(1, d); }
+};
+
 // Sum and maximum over the two lanes of a column.
 __device__ __forceinline__ float both_sum(float x) {
     const auto p = __builtin_amdgcn_permlane32_swap(__float_as_int(x), __float_as_int(x), false, false);
@@ -216,23 +404,31 @@ __device__ __forceinline__ void att_write(T *to, const f32x16 (&acc)[D / 32], fl
         }
 }
 
-// What a workgroup works on: workgroups of one pair (example, key head) are a multiple of eight apart, that is on one XCD, whose L2
-// then holds its keys and values; the longest tiles come first.
+// What a workgroup works on.  All of a pair (example, head of keys) run on one XCD one after the other, so that its L2 holds what they
+// share: workgroups go round the XCDs, so every eighth belongs to the same pair.  The longest of a pair come first.
 struct AttPlace {
     RowSpan span;
-    int64_t row0;   // the tile's first row in the example
-    int kv, head;   // heads of keys, of queries
+    int row0, count;  // the tile's first row in the example, the example's rows
+    int kv, head;     // heads of keys, of queries
     bool there;
-    __device__ __forceinline__ AttPlace(const TokenRows &tok, const AttHeads &a, bool backwards, bool members) {
-        const int64_t padded = (a.pairs + 7) & ~(int64_t)7;
-        const int64_t pair = blockIdx.x % padded, member = members ? blockIdx.x / padded : 0;
+    // QUERIES: a workgroup per tile and head of queries, later tiles are the longer ones.  Otherwise one per tile of keys, and the first tiles of
+    // all pairs come first: there are fewer workgroups, and a long one that starts late keeps the others waiting (16 x 1024 tokens, 16
+    // heads on 4 of 128: 250 us, pair by pair 383).
+    template <bool QUERIES>
+    __device__ __forceinline__ AttPlace(const TokenRows &tok, const AttHeads &a, std::integral_constant<bool, QUERIES>) {
+        const int members = QUERIES ? a.group : 1;
+        const int64_t unit = a.unit0 + blockIdx.x, turn = unit >> 3, groups = (a.pairs + 7) >> 3, per = QUERIES ? (int64_t)a.tiles * members : groups;
+        const int64_t whole = turn / per, part = turn - whole * per, pair = (QUERIES ? whole : part) * 8 + (unit & 7);
+        const int rest = (int)(QUERIES ? part : whole), tile = rest / members;
         there = pair < a.pairs;
         if (!there) return;
-        span = rows_of(tok, tok.base + pair / a.kv_heads);
-        kv = (int)(pair % a.kv_heads);
-        head = kv * a.group + (int)member;
-        row0 = (int64_t)(backwards ? gridDim.y - 1 - blockIdx.y : blockIdx.y) * kAttRows;
-        there = row0 < span.count;
+        const int64_t e = pair / a.kv_heads;
+        span = rows_of(tok, tok.base + e);
+        kv = (int)(pair - e * a.kv_heads);
+        head = kv * a.group + (rest - tile * members);
+        row0 = (QUERIES ? a.tiles - 1 - tile : tile) * kAttRows;
+        count = (int)span.count;  // (at most kAttMaxTokens)
+        there = row0 < count;
     }
 };
 
@@ -248,19 +444,19 @@ template <> constexpr float kAttShiftBack<f16_t> = 14.f;
 // A staged tile's rows; LDS for two of them, all planes.
 template <typename T> constexpr int att_step() { return LinearPlanes<T>::N == 1 ? 64 : 32; }
 
-template <typename T, int D>
+template <typename T, int D, bool DIRECT>
 __global__ __launch_bounds__(kAttThreads, LinearPlanes<T>::N == 1 ? 2 : 1) void attention_forward(
     TokenRows tok, AttHeads a, const T *__restrict__ Q, int64_t q_stride, const T *__restrict__ K, int64_t k_stride,
-    const T *__restrict__ V, int64_t v_stride, T *__restrict__ O, int64_t o_stride, float *__restrict__ lse, int64_t q_heads)
+    const T *__restrict__ V, int64_t v_stride, T *__restrict__ O, int64_t o_stride, float *__restrict__ lse)
 {
     typedef typename LinearPlanes<T>::elem E;
     constexpr int STEP = att_step<T>(), KB = STEP / 32, DB = D / 32;
-    typedef AttStage<T, D, STEP> Stage;
-    __shared__ __align__(16) E lds[2 * Stage::LEN];
-    const AttPlace at(tok, a, true, true);
+    typedef AttPipe<T, D, STEP, DIRECT> Pipe;
+    __shared__ __align__(16) E lds[Pipe::LDS];
+    const AttPlace at(tok, a, std::true_type{});
     if (!at.there) return;  // uniform
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t first = at.row0 + wave * 32, mine = first + (lane & 31), count = at.span.count;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int first = at.row0 + wave * 32, mine = first + (lane & 31), count = at.count;
     const T *q = Q + (at.span.first + (mine < count ? mine : 0)) * q_stride + (int64_t)at.head * a.dim;
     const T *k = K + at.span.first * k_stride + (int64_t)at.kv * a.dim, *v = V + at.span.first * v_stride + (int64_t)at.kv * a.dim;
     AttColumns<T, D> cols;
@@ -271,29 +467,22 @@ __global__ __launch_bounds__(kAttThreads, LinearPlanes<T>::N == 1 ? 2 : 1) void 
     for (int d = 0; d < DB; ++d) acc[d] = zero16();
     float most = -INFINITY, sum = 0.f;  // (of the lane's own rows)
     const float c = a.scale * kLog2E;
-    const int64_t end = at.row0 + kAttRows < count ? at.row0 + kAttRows : count;  // keys
-    Stage sk, sv;
-    sk.load(k, k_stride, 0, end, a.dim);
-    sv.load(v, v_stride, 0, end, a.dim);
-    for (int64_t t = 0; t < end; t += STEP) {
-        __syncthreads();  // (the last tile has been read)
-        sk.store(lds);
-        sv.store(lds + Stage::LEN);
-        __syncthreads();
-        if (t + STEP < end) {
-            sk.load(k, k_stride, t + STEP, end, a.dim);
-            sv.load(v, v_stride, t + STEP, end, a.dim);
-        }
+    const int end = at.row0 + kAttRows < count ? at.row0 + kAttRows : count;  // keys
+    Pipe pipe(lds, a.dim, k_stride, v_stride);
+    pipe.fetch(k, k_stride, v, v_stride, 0, end);
+    for (int t = 0; t < end; t += STEP) {
+        const E *tk = pipe.turn(), *tv = tk + Pipe::LEN / 2;
+        if (t + STEP < end) pipe.fetch(k, k_stride, v, v_stride, t + STEP, end);
         if (t > first + 31) continue;  // all later than this wavefront's queries
         f32x16 s[KB];
 #pragma unroll
         for (int b = 0; b < KB; ++b) {
             s[b] = zero16();
 #pragma unroll
-            for (int d = 0; d < D / 16; ++d) s[b] = att_mfma<T>(read.along(lds, b * 32, d), cols.k[d], s[b]);
+            for (int d = 0; d < D / 16; ++d) s[b] = att_mfma<T>(read.along(tk, b * 32, d), cols.k[d], s[b]);
         }
         if (t + STEP - 1 > first) {
-            const int left = (int)(mine - t);  // rows of the tile up to this query
+            const int left = mine - t;  // rows of the tile up to this query
 #pragma unroll
             for (int b = 0; b < KB; ++b)
 #pragma unroll
@@ -316,7 +505,8 @@ __global__ __launch_bounds__(kAttThreads, LinearPlanes<T>::N == 1 ? 2 : 1) void 
                 for (int r = 0; r < 16; ++r) acc[d][r] *= down;
         }
 #pragma unroll
-        for (int b = 0; b < KB; ++b)
+        for (int b = 0; b < KB; ++b) {
+            const AttAcross<T, D, STEP, DIRECT> values(read, tv, b * 32);
 #pragma unroll
             for (int r = 0; r < 16; r += 8) {
                 float p[8];
@@ -328,13 +518,14 @@ __global__ __launch_bounds__(kAttThreads, LinearPlanes<T>::N == 1 ? 2 : 1) void 
                 AttFrag<T> w;
                 w.set(p);
 #pragma unroll
-                for (int d = 0; d < DB; ++d) acc[d] = att_mfma<T>(read.across(lds + Stage::LEN, b * 32 + r * 2, d), w, acc[d]);
+                for (int d = 0; d < DB; ++d) acc[d] = att_mfma<T>(values.get(r / 8, d), w, acc[d]);
             }
+        }
     }
     sum = both_sum(sum);
     if (mine < count) {
         att_write<T, D>(O + (at.span.first + mine) * o_stride + (int64_t)at.head * a.dim, acc, 1.f / sum, a.dim, lane);
-        if (lse && lane < 32) lse[(at.span.first + mine) * q_heads + at.head] = (most + __builtin_amdgcn_logf(sum)) * kLn2;
+        if (lse && lane < 32) lse[at.head * tok.rows + at.span.first + mine] = (most + __builtin_amdgcn_logf(sum)) * kLn2;
     }
 }
 
@@ -370,20 +561,20 @@ struct AttScaled<f16_t, DB> {
 };
 
 // dq by queries; leaves D_i for the other kernel.
-template <typename T, int D>
-__global__ __launch_bounds__(kAttThreads, LinearPlanes<T>::N == 1 ? 2 : 1) void attention_backward_q(
+template <typename T, int D, bool DIRECT>
+__global__ __launch_bounds__(kAttThreads, LinearPlanes<T>::N > 1 ? 1 : D <= 64 ? 4 : 2) void attention_backward_q(
     TokenRows tok, AttHeads a, const T *__restrict__ Q, int64_t q_stride, const T *__restrict__ K, int64_t k_stride,
     const T *__restrict__ V, int64_t v_stride, const T *__restrict__ O, int64_t o_stride, const float *__restrict__ lse,
-    const T *__restrict__ DO, int64_t do_stride, T *__restrict__ DQ, int64_t dq_stride, float *__restrict__ delta, int64_t q_heads)
+    const T *__restrict__ DO, int64_t do_stride, T *__restrict__ DQ, int64_t dq_stride, float *__restrict__ delta)
 {
     typedef typename LinearPlanes<T>::elem E;
     constexpr int STEP = att_step<T>(), KB = STEP / 32, DB = D / 32;
-    typedef AttStage<T, D, STEP> Stage;
-    __shared__ __align__(16) E lds[2 * Stage::LEN];
-    const AttPlace at(tok, a, true, true);
+    typedef AttPipe<T, D, STEP, DIRECT> Pipe;
+    __shared__ __align__(16) E lds[Pipe::LDS];
+    const AttPlace at(tok, a, std::true_type{});
     if (!at.there) return;  // uniform
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t first = at.row0 + wave * 32, mine = first + (lane & 31), count = at.span.count;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int first = at.row0 + wave * 32, mine = first + (lane & 31), count = at.count;
     const bool live = mine < count;
     const int64_t row = at.span.first + (live ? mine : 0);
     const T *k = K + at.span.first * k_stride + (int64_t)at.kv * a.dim, *v = V + at.span.first * v_stride + (int64_t)at.kv * a.dim;
@@ -402,44 +593,37 @@ __global__ __launch_bounds__(kAttThreads, LinearPlanes<T>::N == 1 ? 2 : 1) void 
             for (int j = 0; j < 8; ++j) dot = fmaf((float)x[j], (float)y[j], dot);
         }
         dot = both_sum(dot);
-        if (live && lane < 32) delta[row * q_heads + at.head] = dot;
+        if (live && lane < 32) delta[at.head * tok.rows + row] = dot;
     }
     const AttRead<T, D, STEP> read(lane);
     f32x16 acc[DB];
 #pragma unroll
     for (int d = 0; d < DB; ++d) acc[d] = zero16();
     AttScaled<T, DB> scaled;
-    const float c = a.scale * kLog2E, most = live ? lse[row * q_heads + at.head] * kLog2E : INFINITY;
-    const int64_t end = at.row0 + kAttRows < count ? at.row0 + kAttRows : count;
-    Stage sk, sv;
-    sk.load(k, k_stride, 0, end, a.dim);
-    sv.load(v, v_stride, 0, end, a.dim);
-    for (int64_t t = 0; t < end; t += STEP) {
-        __syncthreads();
-        sk.store(lds);
-        sv.store(lds + Stage::LEN);
-        __syncthreads();
-        if (t + STEP < end) {
-            sk.load(k, k_stride, t + STEP, end, a.dim);
-            sv.load(v, v_stride, t + STEP, end, a.dim);
-        }
+    const float c = a.scale * kLog2E, most = live ? lse[at.head * tok.rows + row] * kLog2E : INFINITY;
+    const int end = at.row0 + kAttRows < count ? at.row0 + kAttRows : count;
+    Pipe pipe(lds, a.dim, k_stride, v_stride);
+    pipe.fetch(k, k_stride, v, v_stride, 0, end);
+    for (int t = 0; t < end; t += STEP) {
+        const E *tk = pipe.turn(), *tv = tk + Pipe::LEN / 2;
+        if (t + STEP < end) pipe.fetch(k, k_stride, v, v_stride, t + STEP, end);
         if (t > first + 31) continue;
-        const bool edge = t + STEP - 1 > first;
-        const int left = (int)(mine - t);
-#pragma unroll
+        const int left = mine - t;
+#pragma unroll 1
         for (int b = 0; b < KB; ++b) {
             f32x16 s = zero16(), ds = zero16();
 #pragma unroll
             for (int d = 0; d < D / 16; ++d) {
-                s = att_mfma<T>(read.along(lds, b * 32, d), q.k[d], s);
-                ds = att_mfma<T>(read.along(lds + Stage::LEN, b * 32, d), g.k[d], ds);
+                s = att_mfma<T>(read.along(tk, b * 32, d), q.k[d], s);
+                ds = att_mfma<T>(read.along(tv, b * 32, d), g.k[d], ds);
             }
+            if (t + b * 32 + 31 > first)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const float p = __builtin_amdgcn_exp2f(fmaf(s[r], c, -most));
-                ds[r] = !edge || b * 32 + att_row(r, lane) <= left ? p * (ds[r] - dot) : 0.f;
-            }
+                for (int r = 0; r < 16; ++r) s[r] = b * 32 + att_row(r, lane) <= left ? s[r] : -INFINITY;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) ds[r] = __builtin_amdgcn_exp2f(fmaf(s[r], c, -most)) * (ds[r] - dot);
             scaled.fit(ds, acc);
+            const AttAcross<T, D, STEP, DIRECT> keys(read, tk, b * 32);
 #pragma unroll
             for (int r = 0; r < 16; r += 8) {
                 float x[8];
@@ -448,7 +632,7 @@ __global__ __launch_bounds__(kAttThreads, LinearPlanes<T>::N == 1 ? 2 : 1) void 
                 AttFrag<T> w;
                 w.set(x);
 #pragma unroll
-                for (int d = 0; d < DB; ++d) acc[d] = att_mfma<T>(read.across(lds, b * 32 + r * 2, d), w, acc[d]);
+                for (int d = 0; d < DB; ++d) acc[d] = att_mfma<T>(keys.get(r / 8, d), w, acc[d]);
             }
         }
     }
@@ -456,21 +640,22 @@ __global__ __launch_bounds__(kAttThreads, LinearPlanes<T>::N == 1 ? 2 : 1) void 
 }
 
 // dk and dv by keys, over all heads that share them.
-template <typename T, int D>
-__global__ __launch_bounds__(kAttThreads, 1) void attention_backward_kv(
+template <typename T, int D, bool DIRECT>
+__global__ __launch_bounds__(kAttThreads, LinearPlanes<T>::N == 1 && D <= 64 ? 3 : 1) void attention_backward_kv(
     TokenRows tok, AttHeads a, const T *__restrict__ Q, int64_t q_stride, const T *__restrict__ K, int64_t k_stride,
     const T *__restrict__ V, int64_t v_stride, const float *__restrict__ lse, const T *__restrict__ DO, int64_t do_stride,
-    const float *__restrict__ delta, T *__restrict__ DK, int64_t dk_stride, T *__restrict__ DV, int64_t dv_stride, int64_t q_heads)
+    const float *__restrict__ delta, T *__restrict__ DK, int64_t dk_stride, T *__restrict__ DV, int64_t dv_stride)
 {
     typedef typename LinearPlanes<T>::elem E;
     constexpr int STEP = att_step<T>(), QB = STEP / 32, DB = D / 32;
-    typedef AttStage<T, D, STEP> Stage;
-    __shared__ __align__(16) E lds[2 * Stage::LEN];
-    __shared__ __align__(16) float most[STEP], dots[STEP];
-    const AttPlace at(tok, a, false, false);
+    typedef AttPipe<T, D, STEP, DIRECT> Pipe;
+    // (One array: with several the compiler waits for all loads to LDS in front of each read.)
+    __shared__ __align__(16) E lds[Pipe::LDS + 8 * STEP];
+    float *const row_values = reinterpret_cast<float *>(lds + Pipe::LDS);  // [2][2][STEP]
+    const AttPlace at(tok, a, std::false_type{});
     if (!at.there) return;  // uniform
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t first = at.row0 + wave * 32, mine = first + (lane & 31), count = at.span.count;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int first = at.row0 + wave * 32, mine = first + (lane & 31), count = at.count;
     const bool live = mine < count;
     const int64_t row = at.span.first + (live ? mine : 0);
     AttColumns<T, D> k, v;
@@ -482,19 +667,18 @@ __global__ __launch_bounds__(kAttThreads, 1) void attention_backward_kv(
     for (int d = 0; d < DB; ++d) dk[d] = dv[d] = zero16();
     AttScaled<T, DB> scaled;
     const float c = a.scale * kLog2E;
-    Stage sq, sg;
+    Pipe pipe(lds, a.dim, q_stride, do_stride);
+    int which = 0;
     float next_most = 0.f, next_dot = 0.f;
-    const auto fetch = [&](int64_t t, int64_t head) {
-        sq.load(Q + at.span.first * q_stride + head * a.dim, q_stride, t, count, a.dim);
-        sg.load(DO + at.span.first * do_stride + head * a.dim, do_stride, t, count, a.dim);
-        if (threadIdx.x < STEP) {
-            const bool there = t + threadIdx.x < count;
-            const int64_t r = (at.span.first + t + threadIdx.x) * q_heads + head;
-            next_most = there ? fmaf(lse[r], kLog2E, -kAttShiftBack<T>) : INFINITY;  // (a row that is not there: p = 0)
-            next_dot = there ? delta[r] : 0.f;
+    const auto fetch = [&](int t, int64_t head) {
+        pipe.fetch(Q + at.span.first * q_stride + head * a.dim, q_stride, DO + at.span.first * do_stride + head * a.dim, do_stride, t, count);
+        if (threadIdx.x < STEP) {  // (nothing is done with them here: that would wait for them)
+            const int64_t r = head * tok.rows + at.span.first + (t + (int)threadIdx.x < count ? t + threadIdx.x : count - 1);
+            next_most = lse[r];
+            next_dot = delta[r];
         }
     };
-    int64_t t = at.row0, next_t = t;
+    int t = at.row0, next_t = t;
     int head = at.head, next_head = head;
     const auto advance = [&]() {
         next_t += STEP;
@@ -505,51 +689,61 @@ __global__ __launch_bounds__(kAttThreads, 1) void attention_backward_kv(
     };
     fetch(t, head);
     for (; head < at.head + a.group; t = next_t, head = next_head) {
-        __syncthreads();
-        sq.store(lds);
-        sg.store(lds + Stage::LEN);
-        if (threadIdx.x < STEP) {
-            most[threadIdx.x] = next_most;
-            dots[threadIdx.x] = next_dot;
+        if (threadIdx.x < STEP) {  // (the other one may still be read)
+            // (a row that is not there: p = 0)
+            row_values[which * 2 * STEP + threadIdx.x] = t + (int)threadIdx.x < count ? (kAttShiftBack<T> * kLn2 - next_most) / a.scale : -INFINITY;
+            row_values[which * 2 * STEP + STEP + threadIdx.x] = -next_dot;
         }
-        __syncthreads();
+        const E *tq = pipe.turn(), *tg = tq + Pipe::LEN / 2;
+        const float *most = row_values + which * 2 * STEP, *dots = most + STEP;
+        which ^= 1;
         advance();
         if (next_head < at.head + a.group) fetch(next_t, next_head);
-#pragma unroll
+        if (t + STEP - 1 < first) continue;  // all earlier than this wavefront's keys
+#pragma unroll 1
         for (int b = 0; b < QB; ++b) {
-            if (t + b * 32 + 31 < first) continue;  // all earlier than this wavefront's keys
-            f32x16 s = zero16(), ds = zero16();
-#pragma unroll
-            for (int d = 0; d < D / 16; ++d) {
-                s = att_mfma<T>(read.along(lds, b * 32, d), k.k[d], s);
-                ds = att_mfma<T>(read.along(lds + Stage::LEN, b * 32, d), v.k[d], ds);
-            }
-            const bool edge = t + b * 32 < first + 31;
-            const int from = (int)(mine - t) - b * 32;  // the first of the rows that sees this key
+            // (sums that begin at -L / scale and -D: the exponent and do v - D without further instructions)
             const float *m = most + b * 32 + 4 * (lane >> 5), *dot = dots + b * 32 + 4 * (lane >> 5);
+            f32x16 s, ds;
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                const float p = __builtin_amdgcn_exp2f(fmaf(s[r], c, -m[8 * (r >> 2) + (r & 3)]));
-                const bool seen = !edge || att_row(r, lane) >= from;
-                s[r] = seen ? p : 0.f;
-                ds[r] = seen ? p * (ds[r] - dot[8 * (r >> 2) + (r & 3)]) : 0.f;
+                s[r] = m[8 * (r >> 2) + (r & 3)];
+                ds[r] = dot[8 * (r >> 2) + (r & 3)];
+            }
+#pragma unroll
+            for (int d = 0; d < D / 16; ++d) {
+                s = att_mfma<T>(read.along(tq, b * 32, d), k.k[d], s);
+                ds = att_mfma<T>(read.along(tg, b * 32, d), v.k[d], ds);
+            }
+            const int from = mine - t - b * 32;  // the first of the rows that sees this key
+            if (t + b * 32 < first + 31)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[r] = att_row(r, lane) >= from ? s[r] : -INFINITY;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                s[r] = __builtin_amdgcn_exp2f(s[r] * c);
+                ds[r] *= s[r];
             }
             scaled.fit(ds, dk);
+            AttFrag<T> w[2], z[2];
 #pragma unroll
-            for (int r = 0; r < 16; r += 8) {
+            for (int h = 0; h < 2; ++h) {
                 float x[8], y[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    x[j] = s[r + j];
-                    y[j] = ds[r + j];
+                    x[j] = s[8 * h + j];
+                    y[j] = ds[8 * h + j];
                 }
-                AttFrag<T> w, z;
-                w.set(x);
-                z.set(y);
+                w[h].set(x);
+                z[h].set(y);
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const AttAcrossBoth<T, D, STEP, DIRECT> rows(read, tq, tg, b * 32 + h * 16);
 #pragma unroll
                 for (int d = 0; d < DB; ++d) {
-                    dv[d] = att_mfma<T>(read.across(lds + Stage::LEN, b * 32 + r * 2, d), w, dv[d]);
-                    dk[d] = att_mfma<T>(read.across(lds, b * 32 + r * 2, d), z, dk[d]);
+                    dv[d] = att_mfma<T>(rows.get_b(d), w[h], dv[d]);
+                    dk[d] = att_mfma<T>(rows.get_a(d), z[h], dk[d]);
                 }
             }
         }

@@ -213,18 +213,29 @@ int by_head_dim(int64_t dim, F &&f) {
     return f(std::integral_constant<int, 128>{});
 }
 
-// launch(examples' rows, heads, grid) for as many examples at a time as a grid holds; `members`: a workgroup per head of queries
-template <typename F>
-void by_examples(const TokenRows &tok, int64_t q_heads, int64_t kv_heads, int64_t dim, float scale, bool members, F &&launch) {
-    const int64_t tiles = (std::min(tok.tokens, tok.rows) + kAttRows - 1) / kAttRows, group = q_heads / kv_heads;
-    const int64_t per = std::max<int64_t>(1, kMaxGroups / q_heads);
-    for (int64_t e0 = 0; e0 < tok.examples; e0 += per) {
-        TokenRows part = tok;
-        part.examples = std::min(per, tok.examples - e0);
-        part.base = e0;
-        const AttHeads a{part.examples * kv_heads, (int)kv_heads, (int)group, (int)dim, scale};
-        launch(part, a, dim3((unsigned)(round_up(a.pairs, 8) * (members ? group : 1)), (unsigned)tiles));
+// Rows that go to LDS in whole pieces of 16 bytes, 64 of them within 2 GB; f(whether all of the arrays are such).
+struct Pieces {
+    const void *p;
+    int64_t stride;
+};
+template <typename T, typename F>
+int by_pieces(int64_t dim, std::initializer_list<Pieces> arrays, F &&f) {
+    if constexpr (sizeof(T) == 2) {
+        bool whole = dim % 8 == 0;
+        for (const Pieces &a : arrays)
+            whole = whole && reinterpret_cast<uintptr_t>(a.p) % 16 == 0 && a.stride % 8 == 0 && a.stride < ((int64_t)1 << 24);
+        if (whole) return f(std::true_type{});
     }
+    return f(std::false_type{});
+}
+
+// launch(heads, workgroups) for as many workgroups at a time as a grid holds; `members`: one per tile and head of queries, else of keys
+template <typename F>
+void by_units(const TokenRows &tok, int64_t q_heads, int64_t kv_heads, int64_t dim, float scale, bool members, F &&launch) {
+    const int64_t tiles = (std::min(tok.tokens, tok.rows) + kAttRows - 1) / kAttRows, group = q_heads / kv_heads, pairs = tok.examples * kv_heads;
+    const int64_t units = round_up(pairs, 8) * tiles * (members ? group : 1);
+    for (int64_t u = 0; u < units; u += kMaxGroups)  // (a multiple of eight)
+        launch(AttHeads{pairs, u, (int)tiles, (int)kv_heads, (int)group, (int)dim, scale}, dim3((unsigned)std::min(kMaxGroups, units - u)));
 }
 
 }  // namespace
@@ -342,25 +353,25 @@ extern "C" int cdgrab_attention(cdgrab_handle *h, const cdgrab_token_rows *t, in
     if (!Q || !K || !V || !O) return fail(h, CDGRAB_EINVAL, "%s: null pointer", who);
     const int64_t size = elem_size(type), qw = q_heads * dim, kw = kv_heads * dim, rows = t->rows;
     if (bad_rows(Q, rows, qw, q_stride, size) || bad_rows(K, rows, kw, k_stride, size) || bad_rows(V, rows, kw, v_stride, size) ||
-        bad_rows(O, rows, qw, o_stride, size) || bad_rows(lse, rows, q_heads, q_heads, 4))
+        bad_rows(O, rows, qw, o_stride, size) || bad_rows(lse, q_heads, rows, rows, 4))
         return fail(h, CDGRAB_EINVAL, "%s: a stride below the width, or a misaligned or too long array", who);
     rc = check_apart(h, who, {{"Q", Q, rows, qw * size, q_stride * size}, {"K", K, rows, kw * size, k_stride * size},
                               {"V", V, rows, kw * size, v_stride * size}},
-                     {{"O", O, rows, qw * size, o_stride * size}, {"lse", lse, rows, q_heads * 4, q_heads * 4}});
+                     {{"O", O, rows, qw * size, o_stride * size}, {"lse", lse, 1, rows * q_heads * 4, rows * q_heads * 4}});
     if (rc) return rc;
     const OnDevice on(h->device);
     HIP_TRY(h, on.err);
     const TokenRows tok{t->examples, rows, t->tokens, t->first, t->count, 0};
     return by_elem(type, [&](auto elem) {
         typedef decltype(elem) T;
-        return by_head_dim(dim, [&](auto room) {
-            by_examples(tok, q_heads, kv_heads, dim, scale, true, [&](const TokenRows &part, const AttHeads &a, dim3 grid) {
-                hipLaunchKernelGGL((attention_forward<T, decltype(room)::value>), grid, dim3(kAttThreads), 0, h->stream, part, a, (const T *)Q,
-                                   q_stride, (const T *)K, k_stride, (const T *)V, v_stride, (T *)O, o_stride, lse, q_heads);
+        return by_head_dim(dim, [&](auto room) { return by_pieces<T>(dim, {{K, k_stride}, {V, v_stride}}, [&](auto direct) {
+            by_units(tok, q_heads, kv_heads, dim, scale, true, [&](const AttHeads &a, dim3 grid) {
+                hipLaunchKernelGGL((attention_forward<T, decltype(room)::value, decltype(direct)::value>), grid, dim3(kAttThreads), 0, h->stream, tok, a, (const T *)Q,
+                                   q_stride, (const T *)K, k_stride, (const T *)V, v_stride, (T *)O, o_stride, lse);
             });
             HIP_TRY(h, hipGetLastError());
             return (int)CDGRAB_OK;
-        });
+        }); });
     });
 }
 
@@ -377,12 +388,12 @@ extern "C" int cdgrab_attention_backward(cdgrab_handle *h, const cdgrab_token_ro
     if (!Q || !K || !V || !O || !lse || !DO || !DQ || !DK || !DV) return fail(h, CDGRAB_EINVAL, "%s: null pointer", who);
     const int64_t size = elem_size(type), qw = q_heads * dim, kw = kv_heads * dim, rows = t->rows;
     if (bad_rows(Q, rows, qw, q_stride, size) || bad_rows(K, rows, kw, k_stride, size) || bad_rows(V, rows, kw, v_stride, size) ||
-        bad_rows(O, rows, qw, o_stride, size) || bad_rows(DO, rows, qw, do_stride, size) || bad_rows(lse, rows, q_heads, q_heads, 4) ||
+        bad_rows(O, rows, qw, o_stride, size) || bad_rows(DO, rows, qw, do_stride, size) || bad_rows(lse, q_heads, rows, rows, 4) ||
         bad_rows(DQ, rows, qw, dq_stride, size) || bad_rows(DK, rows, kw, dk_stride, size) || bad_rows(DV, rows, kw, dv_stride, size))
         return fail(h, CDGRAB_EINVAL, "%s: a stride below the width, or a misaligned or too long array", who);
     rc = check_apart(h, who, {{"Q", Q, rows, qw * size, q_stride * size}, {"K", K, rows, kw * size, k_stride * size},
                               {"V", V, rows, kw * size, v_stride * size}, {"O", O, rows, qw * size, o_stride * size},
-                              {"DO", DO, rows, qw * size, do_stride * size}, {"lse", lse, rows, q_heads * 4, q_heads * 4}},
+                              {"DO", DO, rows, qw * size, do_stride * size}, {"lse", lse, 1, rows * q_heads * 4, rows * q_heads * 4}},
                      {{"DQ", DQ, rows, qw * size, dq_stride * size}, {"DK", DK, rows, kw * size, dk_stride * size},
                       {"DV", DV, rows, kw * size, dv_stride * size}});
     if (rc) return rc;
@@ -395,15 +406,21 @@ extern "C" int cdgrab_attention_backward(cdgrab_handle *h, const cdgrab_token_ro
         typedef decltype(elem) T;
         return by_head_dim(dim, [&](auto room) {
             constexpr int D = decltype(room)::value;
-            by_examples(tok, q_heads, kv_heads, dim, scale, true, [&](const TokenRows &part, const AttHeads &a, dim3 grid) {
-                hipLaunchKernelGGL((attention_backward_q<T, D>), grid, dim3(kAttThreads), 0, h->stream, part, a, (const T *)Q, q_stride,
-                                   (const T *)K, k_stride, (const T *)V, v_stride, (const T *)O, o_stride, lse, (const T *)DO, do_stride,
-                                   (T *)DQ, dq_stride, delta, q_heads);
+            by_pieces<T>(dim, {{K, k_stride}, {V, v_stride}}, [&](auto direct) {
+                by_units(tok, q_heads, kv_heads, dim, scale, true, [&](const AttHeads &a, dim3 grid) {
+                    hipLaunchKernelGGL((attention_backward_q<T, D, decltype(direct)::value>), grid, dim3(kAttThreads), 0, h->stream, tok, a,
+                                       (const T *)Q, q_stride, (const T *)K, k_stride, (const T *)V, v_stride, (const T *)O, o_stride, lse,
+                                       (const T *)DO, do_stride, (T *)DQ, dq_stride, delta);
+                });
+                return 0;
             });
-            by_examples(tok, q_heads, kv_heads, dim, scale, false, [&](const TokenRows &part, const AttHeads &a, dim3 grid) {
-                hipLaunchKernelGGL((attention_backward_kv<T, D>), grid, dim3(kAttThreads), 0, h->stream, part, a, (const T *)Q, q_stride,
-                                   (const T *)K, k_stride, (const T *)V, v_stride, lse, (const T *)DO, do_stride, delta, (T *)DK, dk_stride,
-                                   (T *)DV, dv_stride, q_heads);
+            by_pieces<T>(dim, {{Q, q_stride}, {DO, do_stride}}, [&](auto direct) {
+                by_units(tok, q_heads, kv_heads, dim, scale, false, [&](const AttHeads &a, dim3 grid) {
+                    hipLaunchKernelGGL((attention_backward_kv<T, D, decltype(direct)::value>), grid, dim3(kAttThreads), 0, h->stream, tok, a,
+                                       (const T *)Q, q_stride, (const T *)K, k_stride, (const T *)V, v_stride, lse, (const T *)DO, do_stride,
+                                       delta, (T *)DK, dk_stride, (T *)DV, dv_stride);
+                });
+                return 0;
             });
             HIP_TRY(h, hipGetLastError());
             return (int)CDGRAB_OK;

@@ -102,7 +102,7 @@ def test_attention(p):
     q, k, v = qkv.split([32, 16, 16], -1)
     o, lse = p.cdgrab_attention(h, q, k, v, q_heads=4, kv_heads=2)
     a = h.last
-    assert a[2:7] == [4, 2, 8, 1, 8 ** -0.5] and o.shape == q.shape and lse.shape == (2, 7, 4) and lse.dtype == torch.float32
+    assert a[2:7] == [4, 2, 8, 1, 8 ** -0.5] and o.shape == q.shape and lse.shape == (4, 2, 7) and lse.dtype == torch.float32
     assert a[7:13] == [qkv.data_ptr(), 64, qkv.data_ptr() + 64, 64, qkv.data_ptr() + 96, 64] and a[14:] == [32, lse.data_ptr()]
     assert p.cdgrab_attention(h, q, k, v, q_heads=4, kv_heads=2, scale=0.5, want_lse=False)[1] is None and h.last[6] == 0.5
     dqkv = torch.zeros_like(qkv)
@@ -117,4 +117,4 @@ def test_attention(p):
         with pytest.raises((TypeError, ValueError)):
             p.cdgrab_attention(h, **{"Q": q, "K": k, "V": v, "q_heads": 4, "kv_heads": 2, **bad})
     with pytest.raises(ValueError):
-        p.cdgrab_attention_backward(h, q, k, v, o, lse[..., :3], o, q_heads=4, kv_heads=2)
+        p.cdgrab_attention_backward(h, q, k, v, o, lse[:3], o, q_heads=4, kv_heads=2)
