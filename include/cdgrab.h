@@ -456,7 +456,7 @@ int cdgrab_embed(cdgrab_handle *h, int64_t rows, int64_t vocab, int64_t width, c
  *     G[e][v * width + c] = scale * sum over the example's rows t with ids[t] = v of DY[t][c];
  * ids outside 0 .. vocab - 1 have no part in it.  One example that holds all rows gives the ordinary gradient.
  *   ids [rows] int32 dev, DY [rows][width] of `type` dev, G: row e at G + e * g_stride, fp32 dev, written whole.
- * Examples of more than 2048 rows use workspace (16 bytes a row, and 8 * width bytes per 64 rows; at most 1 GiB, or one
+ * Examples of more than 2048 rows use workspace (16 bytes a row, and 4 * width bytes per 16 rows; at most 1 GiB, or one
  * example's).  Sums in fp32.  Errors: EINVAL (as above; tokens > 2^28, more than 2^32 elements per row of G), ENOMEM, EHIP. */
 int cdgrab_pergrad_embed(cdgrab_handle *h, const cdgrab_token_rows *t, int64_t vocab, int64_t width, int32_t type,
                          const int32_t *ids, const void *DY, int64_t dy_stride, float scale, float *G, int64_t g_stride);

@@ -450,6 +450,9 @@ def _rows(t: torch.Tensor, name: str, device, like: Optional[torch.Tensor] = Non
     width = shape[-1]
     if t.is_contiguous():
         return t.data_ptr(), t.numel() // width if width else 0, width, width or 1
+    strides = t.stride()
+    if len(shape) == 3 and strides[2] == 1 and strides[1] >= width > 0 and strides[0] == shape[1] * strides[1] > 0 < shape[0]:
+        return t.data_ptr(), shape[0] * shape[1], width, strides[1]  # (the usual case, without the loops)
     rows, stride = 1, width
     for n in shape[:-1]:
         rows *= n
@@ -616,11 +619,15 @@ def cdgrab_orthogonalize(h: Handle, M: torch.Tensor, steps: int = 5, coeffs=None
 # ---- operators over the rows of a sequence ---------------------------------------------------
 
 def _ids(ids: torch.Tensor, shape, device) -> int:
-    return _ptr(ids, torch.int32, shape, "ids", device)
+    if ids.dtype is torch.int32 and ids.shape == shape and ids.is_contiguous() and ids.device == device:
+        return ids.data_ptr()
+    return _ptr(ids, torch.int32, shape, "ids", device)  # (says what is wrong)
 
 
 def _made_like(h, t: torch.Tensor, shape, dtype, partly: bool) -> torch.Tensor:
     """An output that the call makes; zeros where it may not write all of it (`partly`)."""
+    if h.stream is None or h.stream_number == _current_stream(h.device_index):
+        return (torch.zeros if partly else torch.empty)(shape, dtype=dtype, device=t.device)
     out = _allocator(h)(shape, dtype=dtype, device=t.device)
     if partly:
         with torch.cuda.stream(h.stream):  # before the call's kernels, wherever they run
@@ -636,15 +643,18 @@ def cdgrab_embed(h: Handle, ids: torch.Tensor, table: torch.Tensor, scale: float
     pt, vocab, width, st = _rows(table, "table", dev)
     if table.dim() != 2:
         raise ValueError("table must be [vocab][width], got %s" % (tuple(table.shape),))
+    rows = ids.numel()
     if Y is None:
-        Y = _allocator(h)((*ids.shape, width), dtype=dtype or table.dtype, device=dev)
+        Y = _made_like(h, table, (*ids.shape, width), dtype or table.dtype, False)
+        py, sy = Y.data_ptr(), width or 1
     elif tuple(Y.shape) != (*ids.shape, width) or (dtype is not None and Y.dtype != dtype):
         raise ValueError("Y must be %s %s, got %s %s" % (dtype or table.dtype, (*ids.shape, width), Y.dtype, tuple(Y.shape)))
+    else:
+        py, _, _, sy = _rows(Y if Y.dim() > 1 else Y.unsqueeze(0), "Y", dev)
     if Y.dtype not in _ELEM:
         raise TypeError("Y must be float32, bfloat16 or float16, got %s" % Y.dtype)
     if table.dtype not in (torch.float32, Y.dtype):
         raise TypeError("table must be float32 or %s, got %s" % (Y.dtype, table.dtype))
-    py, rows, _, sy = _rows(Y if Y.dim() > 1 else Y.unsqueeze(0), "Y", dev)
     rc = h._lib.cdgrab_embed(h._h, rows, vocab, width, _ids(ids, ids.shape, dev), _ELEM[table.dtype], pt, st, scale,
                              _ELEM[Y.dtype], py, sy)
     if rc:
@@ -729,19 +739,21 @@ def cdgrab_pergrad_headnorm(h: Handle, X: torch.Tensor, dY: torch.Tensor, gain_q
 
 
 def _attention_rows(h, Q, K, V, q_heads, kv_heads, scale, first, count, tokens):
-    """(spans, head dim, scale, [pointer, stride] of Q, K and V)"""
+    """(spans, head dim, scale, pointer and stride of Q, K and V, leading shape)"""
     dev = h.device
     pq, rows, qw, sq = _rows(Q, "Q", dev)
     if q_heads < 1 or kv_heads < 1 or q_heads % kv_heads or qw % q_heads:
         raise ValueError("rows of %d features and %d heads of queries on %d of keys do not go together" % (qw, q_heads, kv_heads))
-    dim = qw // q_heads
-    at = [pq, sq]
-    for x, name in ((K, "K"), (V, "V")):
-        if x.dtype != Q.dtype or tuple(x.shape) != (*Q.shape[:-1], kv_heads * dim):
-            raise ValueError("%s must be %s %s, got %s %s" % (name, Q.dtype, (*Q.shape[:-1], kv_heads * dim), x.dtype, tuple(x.shape)))
-        p, _, _, sx = _rows(x, name, dev)
-        at += [p, sx]
-    return _token_rows(Q, rows, first, count, tokens, dev), dim, dim ** -0.5 if scale is None and dim else scale or 0.0, at
+    dim, lead, kind = qw // q_heads, Q.shape[:-1], Q.dtype
+    kw = kv_heads * dim
+    pk, _, wk, sk = _rows(K, "K", dev)
+    pv, _, wv, sv = _rows(V, "V", dev)
+    for x, w, name in ((K, wk, "K"), (V, wv, "V")):
+        if x.dtype is not kind or w != kw or x.shape[:-1] != lead:
+            raise ValueError("%s must be %s %s, got %s %s" % (name, kind, (*lead, kw), x.dtype, tuple(x.shape)))
+    if scale is None:
+        scale = dim ** -0.5 if dim else 1.0
+    return _token_rows(Q, rows, first, count, tokens, dev), dim, scale, (pq, sq, pk, sk, pv, sv), lead
 
 
 def _rows_or_made(h, t, name, like, partly):
@@ -760,10 +772,10 @@ def cdgrab_attention(h: Handle, Q: torch.Tensor, K: torch.Tensor, V: torch.Tenso
     """Causal attention within each example: (O, lse).  Q[..., q_heads * dim], K and V[..., kv_heads * dim], lse[q_heads, ...]
     float32 (logarithms of the sums, for the backward pass); ``scale`` is 1 / sqrt(dim) by default; rows of examples as in
     cdgrab_pergrad_layernorm.  Rows of no example keep what O holds (zero where the call makes it, and in lse)."""
-    t, dim, scale, at = _attention_rows(h, Q, K, V, q_heads, kv_heads, scale, first, count, tokens)
+    t, dim, scale, at, lead = _attention_rows(h, Q, K, V, q_heads, kv_heads, scale, first, count, tokens)
     partly = first is not None or count is not None
     O, po, so = _rows_or_made(h, O, "O", Q, partly)
-    lse = _made_like(h, Q, (q_heads, *Q.shape[:-1]), torch.float32, partly) if want_lse else None
+    lse = _made_like(h, Q, (q_heads, *lead), torch.float32, partly) if want_lse else None
     rc = h._lib.cdgrab_attention(h._h, ctypes.byref(t), q_heads, kv_heads, dim, _ELEM[Q.dtype], scale, *at, po, so,
                                  lse.data_ptr() if want_lse else None)
     if rc:
@@ -779,10 +791,10 @@ def cdgrab_attention_backward(h: Handle, Q: torch.Tensor, K: torch.Tensor, V: to
                               dV: Optional[torch.Tensor] = None):
     """Backward pass of cdgrab_attention from its outputs O and lse and the gradient dO: (dQ, dK, dV), which may be given, as
     stretches of one array's rows too.  Rows of no example keep what they hold (zero where the call makes them)."""
-    t, dim, scale, at = _attention_rows(h, Q, K, V, q_heads, kv_heads, scale, first, count, tokens)
+    t, dim, scale, at, lead = _attention_rows(h, Q, K, V, q_heads, kv_heads, scale, first, count, tokens)
     po, _, _, so = _rows(O, "O", h.device, Q)
     pg, _, _, sg = _rows(dO, "dO", h.device, Q)
-    pl = _ptr(lse, torch.float32, (q_heads, *Q.shape[:-1]), "lse", h.device)
+    pl = _ptr(lse, torch.float32, (q_heads, *lead), "lse", h.device)
     partly = first is not None or count is not None
     dQ, pq, sq = _rows_or_made(h, dQ, "dQ", Q, partly)
     dK, pk, sk = _rows_or_made(h, dK, "dK", K, partly)

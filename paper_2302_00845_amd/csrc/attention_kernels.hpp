@@ -28,6 +28,7 @@ struct AttHeads {
     int64_t pairs, unit0;  // examples * kv_heads; the launch's first workgroup
     int tiles;             // of kAttRows rows that an example has at most
     int kv_heads, group;   // queries' heads that share keys and values
+    bool by_pair;          // order of the workgroups
     int dim;
     float scale;
 };
@@ -404,22 +405,23 @@ __device__ __forceinline__ void att_write(T *to, const f32x16 (&acc)[D / 32], fl
         }
 }
 
-// What a workgroup works on.  All of a pair (example, head of keys) run on one XCD one after the other, so that its L2 holds what they
-// share: workgroups go round the XCDs, so every eighth belongs to the same pair.  The longest of a pair come first.
+// What a workgroup works on.  All of a pair (example, head of keys) run on one XCD: workgroups go round the XCDs, so every eighth belongs
+// to the same pair.  The longest tiles of all pairs come first: a long one that starts late keeps the others waiting.  Or, by_pair, those of
+// a pair one after the other, so that the XCD's L2 holds what they share.  (us, tile by tile and by pair: forward 64 x 1024 tokens, 12
+// heads of 64, bf16, 6144 workgroups 191 and 183; 16 x 1024, 8 heads of 64, fp32, 1024 workgroups 117 and 177; dk and dv of 16 x 1024, 16
+// heads on 4 of 128, 512 workgroups 250 and 383.)
 struct AttPlace {
     RowSpan span;
     int row0, count;  // the tile's first row in the example, the example's rows
     int kv, head;     // heads of keys, of queries
     bool there;
-    // QUERIES: a workgroup per tile and head of queries, later tiles are the longer ones.  Otherwise one per tile of keys, and the first tiles of
-    // all pairs come first: there are fewer workgroups, and a long one that starts late keeps the others waiting (16 x 1024 tokens, 16
-    // heads on 4 of 128: 250 us, pair by pair 383).
+    // QUERIES: a workgroup per tile and head of queries, later tiles are the longer ones.  Otherwise one per tile of keys.
     template <bool QUERIES>
     __device__ __forceinline__ AttPlace(const TokenRows &tok, const AttHeads &a, std::integral_constant<bool, QUERIES>) {
         const int members = QUERIES ? a.group : 1;
-        const int64_t unit = a.unit0 + blockIdx.x, turn = unit >> 3, groups = (a.pairs + 7) >> 3, per = QUERIES ? (int64_t)a.tiles * members : groups;
-        const int64_t whole = turn / per, part = turn - whole * per, pair = (QUERIES ? whole : part) * 8 + (unit & 7);
-        const int rest = (int)(QUERIES ? part : whole), tile = rest / members;
+        const int64_t unit = a.unit0 + blockIdx.x, turn = unit >> 3, per = a.by_pair ? (int64_t)a.tiles * members : (a.pairs + 7) >> 3;
+        const int64_t whole = turn / per, part = turn - whole * per, pair = (a.by_pair ? whole : part) * 8 + (unit & 7);
+        const int rest = (int)(a.by_pair ? part : whole), tile = rest / members;
         there = pair < a.pairs;
         if (!there) return;
         const int64_t e = pair / a.kv_heads;
@@ -440,6 +442,8 @@ template <typename T> constexpr float kAttShiftForward = 0.f;
 template <> constexpr float kAttShiftForward<f16_t> = 7.f;
 template <typename T> constexpr float kAttShiftBack = 0.f;
 template <> constexpr float kAttShiftBack<f16_t> = 14.f;
+
+template <typename T> constexpr bool kAttExact = LinearPlanes<T>::N > 1;  // fp32
 
 // A staged tile's rows; LDS for two of them, all planes.
 template <typename T> constexpr int att_step() { return LinearPlanes<T>::N == 1 ? 64 : 32; }
@@ -593,35 +597,57 @@ __global__ __launch_bounds__(kAttThreads, LinearPlanes<T>::N > 1 ? 1 : D <= 64 ?
             for (int j = 0; j < 8; ++j) dot = fmaf((float)x[j], (float)y[j], dot);
         }
         dot = both_sum(dot);
-        if (live && lane < 32) delta[at.head * tok.rows + row] = dot;
     }
     const AttRead<T, D, STEP> read(lane);
-    f32x16 acc[DB];
-#pragma unroll
-    for (int d = 0; d < DB; ++d) acc[d] = zero16();
-    AttScaled<T, DB> scaled;
     const float c = a.scale * kLog2E, most = live ? lse[at.head * tok.rows + row] * kLog2E : INFINITY;
     const int end = at.row0 + kAttRows < count ? at.row0 + kAttRows : count;
     Pipe pipe(lds, a.dim, k_stride, v_stride);
     pipe.fetch(k, k_stride, v, v_stride, 0, end);
+    // p (do v - D) of 32 keys
+    const auto weights = [&](const E *tk, const E *tv, int t, int b) {
+        f32x16 s = zero16(), ds = zero16();
+#pragma unroll
+        for (int d = 0; d < D / 16; ++d) {
+            s = att_mfma<T>(read.along(tk, b * 32, d), q.k[d], s);
+            ds = att_mfma<T>(read.along(tv, b * 32, d), g.k[d], ds);
+        }
+        if (t + b * 32 + 31 > first)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] = b * 32 + att_row(r, lane) <= mine - t ? s[r] : -INFINITY;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) ds[r] = __builtin_amdgcn_exp2f(fmaf(s[r], c, -most)) * (ds[r] - dot);
+        return ds;
+    };
+    // The first rows of an example go over their keys twice: o is rounded to 16 bits, and D with it, and for a row of few keys that is
+    // as much as p (do v - D) itself (which is nothing for the first).  What sum_j p_ij (do_i v_j - D_i) leaves is D's error.  (dq, relative,
+    // without and with: 2 tokens of fp16 5.1e-4 and 2.9e-4, 1024 of bf16 2.50e-3 and 2.38e-3; the outputs' rounding alone is 2.1e-4 and
+    // 1.66e-3.  Of rows of many keys D's error is a part of that of p, by the root of their number.)
+    if (LinearPlanes<T>::N == 1 && at.row0 == 0) {
+        float rest = 0.f;
+        for (int t = 0; t < end; t += STEP) {
+            const E *tk = pipe.turn(), *tv = tk + Pipe::LEN / 2;
+            pipe.fetch(k, k_stride, v, v_stride, t + STEP < end ? t + STEP : 0, end);  // (behind the last the first again)
+            if (t > first + 31) continue;
+#pragma unroll 1
+            for (int b = 0; b < KB; ++b) {
+                const f32x16 ds = weights(tk, tv, t, b);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) rest += ds[r];
+            }
+        }
+        dot += both_sum(rest);
+    }
+    f32x16 acc[DB];
+#pragma unroll
+    for (int d = 0; d < DB; ++d) acc[d] = zero16();
+    AttScaled<T, DB> scaled;
     for (int t = 0; t < end; t += STEP) {
         const E *tk = pipe.turn(), *tv = tk + Pipe::LEN / 2;
         if (t + STEP < end) pipe.fetch(k, k_stride, v, v_stride, t + STEP, end);
         if (t > first + 31) continue;
-        const int left = mine - t;
 #pragma unroll 1
         for (int b = 0; b < KB; ++b) {
-            f32x16 s = zero16(), ds = zero16();
-#pragma unroll
-            for (int d = 0; d < D / 16; ++d) {
-                s = att_mfma<T>(read.along(tk, b * 32, d), q.k[d], s);
-                ds = att_mfma<T>(read.along(tv, b * 32, d), g.k[d], ds);
-            }
-            if (t + b * 32 + 31 > first)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) s[r] = b * 32 + att_row(r, lane) <= left ? s[r] : -INFINITY;
-#pragma unroll
-            for (int r = 0; r < 16; ++r) ds[r] = __builtin_amdgcn_exp2f(fmaf(s[r], c, -most)) * (ds[r] - dot);
+            f32x16 ds = weights(tk, tv, t, b);
             scaled.fit(ds, acc);
             const AttAcross<T, D, STEP, DIRECT> keys(read, tk, b * 32);
 #pragma unroll
@@ -636,6 +662,7 @@ __global__ __launch_bounds__(kAttThreads, LinearPlanes<T>::N > 1 ? 1 : D <= 64 ?
             }
         }
     }
+    if (live && lane < 32) delta[at.head * tok.rows + row] = dot;
     if (live) att_write<T, D>(DQ + row * dq_stride + (int64_t)at.head * a.dim, acc, a.scale / scaled.scale, a.dim, lane);
 }
 
@@ -691,7 +718,8 @@ __global__ __launch_bounds__(kAttThreads, LinearPlanes<T>::N == 1 && D <= 64 ? 3
     for (; head < at.head + a.group; t = next_t, head = next_head) {
         if (threadIdx.x < STEP) {  // (the other one may still be read)
             // (a row that is not there: p = 0)
-            row_values[which * 2 * STEP + threadIdx.x] = t + (int)threadIdx.x < count ? (kAttShiftBack<T> * kLn2 - next_most) / a.scale : -INFINITY;
+            row_values[which * 2 * STEP + threadIdx.x] = 
+                t + (int)threadIdx.x >= count ? -INFINITY : kAttExact<T> ? -next_most * kLog2E : (kAttShiftBack<T> * kLn2 - next_most) / a.scale;
             row_values[which * 2 * STEP + STEP + threadIdx.x] = -next_dot;
         }
         const E *tq = pipe.turn(), *tg = tq + Pipe::LEN / 2;
@@ -702,12 +730,13 @@ __global__ __launch_bounds__(kAttThreads, LinearPlanes<T>::N == 1 && D <= 64 ? 3
         if (t + STEP - 1 < first) continue;  // all earlier than this wavefront's keys
 #pragma unroll 1
         for (int b = 0; b < QB; ++b) {
-            // (sums that begin at -L / scale and -D: the exponent and do v - D without further instructions)
+            // (sums that begin at -L / scale and -D: the exponent and do v - D without further instructions.  fp32: L / scale would take
+            // digits from the scores, dk 1.2e-6 off instead of 0.7e-6)
             const float *m = most + b * 32 + 4 * (lane >> 5), *dot = dots + b * 32 + 4 * (lane >> 5);
             f32x16 s, ds;
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                s[r] = m[8 * (r >> 2) + (r & 3)];
+                s[r] = kAttExact<T> ? 0.f : m[8 * (r >> 2) + (r & 3)];
                 ds[r] = dot[8 * (r >> 2) + (r & 3)];
             }
 #pragma unroll
@@ -721,7 +750,7 @@ __global__ __launch_bounds__(kAttThreads, LinearPlanes<T>::N == 1 && D <= 64 ? 3
                 for (int r = 0; r < 16; ++r) s[r] = att_row(r, lane) >= from ? s[r] : -INFINITY;
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                s[r] = __builtin_amdgcn_exp2f(s[r] * c);
+                s[r] = __builtin_amdgcn_exp2f(kAttExact<T> ? fmaf(s[r], c, m[8 * (r >> 2) + (r & 3)]) : s[r] * c);
                 ds[r] *= s[r];
             }
             scaled.fit(ds, dk);

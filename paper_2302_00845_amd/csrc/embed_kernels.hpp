@@ -14,12 +14,13 @@ constexpr int kEmbedList = 2048;    // ids of an example that a workgroup looks 
 constexpr int kEmbedElems = 16384;  // elements of G that a workgroup writes, about
 constexpr int kEmbedSpan = 2048;    // rows of G at most
 constexpr int kEmbedLong = 32;      // rows of dy from which on all threads of a workgroup share a row of G
-constexpr int kEmbedChunk = 4096;   // keys that a workgroup sorts
+constexpr int kEmbedPiece = 16;     // longer examples: the same, and sorted keys of one id that are added up beforehand
+constexpr int kEmbedChunk = 1024;   // keys that a workgroup sorts (of 4096: 40 us for 16 of them, of 1024 a quarter of that)
 constexpr int kEmbedFan = 16;       // sorted runs that are merged at a time
-constexpr int kEmbedPiece = 64;     // sorted keys that a group of threads adds up
 
-// Threads that share a row: 1 << shift of them, VEC elements each at a time.
-template <typename TT, typename T, int VEC>
+// Threads that share a row: 1 << shift of them, VEC elements each at a time.  ONCE, here and below: what is written is more than the caches
+// hold, and goes past them (65 536 rows of 768, bf16, with other inputs every time 45 -> 32 us; 64 examples of 5000 x 128 46 -> 33).
+template <typename TT, typename T, int VEC, bool ONCE>
 __global__ __launch_bounds__(kEmbedThreads) void embed_forward(const int32_t *__restrict__ ids, int64_t rows, int64_t vocab, int width,
                                                                int shift, const TT *__restrict__ table, int64_t t_stride, float scale,
                                                                T *__restrict__ Y, int64_t y_stride)
@@ -39,7 +40,7 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_forward(const int32_t *__
             load_any<TT, VEC>(from + at, x);
 #pragma unroll
             for (int j = 0; j < VEC; ++j) y[j] = known ? (T)((float)x[j] * scale) : (T)0.f;
-            store_any<T, VEC>(to + at, y);
+            store_any<T, VEC, ONCE>(to + at, y);
         }
     }
 }
@@ -85,7 +86,7 @@ __device__ __forceinline__ void embed_shared(int shift, int width, int n, float 
 
 // Examples of at most kEmbedList rows.  Workgroup b writes rows v0 .. v0 + span - 1 of example b / units: it picks the ids in that range,
 // sorts them (id and row, by counting the smaller ones), and its groups of threads take the rows of G in turn.
-template <typename T, int VEC>
+template <typename T, int VEC, bool ONCE>
 __global__ __launch_bounds__(kEmbedThreads) void embed_grad_few(TokenRows tok, uint32_t units, int span, int shift,
                                                                 const int32_t *__restrict__ ids, int64_t vocab, int width,
                                                                 const T *__restrict__ DY, int64_t dy_stride, float scale,
@@ -142,7 +143,7 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_grad_few(TokenRows tok, u
             if (count > 0) sum_of(at, j0, count, sum);
 #pragma unroll
             for (int i = 0; i < VEC; ++i) sum[i] *= scale;
-            store_any<float, VEC>(to + (int64_t)v * width + at, sum);
+            store_any<float, VEC, ONCE>(to + (int64_t)v * width + at, sum);
         }
     }
     __syncthreads();
@@ -158,18 +159,18 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_grad_few(TokenRows tok, u
     }
 }
 
-// ---- longer examples: all (id, row) keys of an example in order -------------------------------------
+// ---- longer examples: all (id, row) keys of an example in order, then as above --------------------------
 
 constexpr uint64_t kEmbedNone = ~(uint64_t)0;  // of no row, or an id that is not in the table
 
 // Chunk b % chunks of example b / chunks: its keys, sorted.  keys [examples of the launch][chunks * kEmbedChunk]
-__global__ __launch_bounds__(1024) void embed_sort(TokenRows tok, int chunks, const int32_t *__restrict__ ids, int64_t vocab,
-                                                   uint64_t *__restrict__ keys)
+__global__ __launch_bounds__(kEmbedThreads) void embed_sort(TokenRows tok, int chunks, const int32_t *__restrict__ ids, int64_t vocab,
+                                                            uint64_t *__restrict__ keys)
 {
     __shared__ uint64_t part[kEmbedChunk];
     const int64_t local = blockIdx.x / chunks, c = blockIdx.x - local * chunks;
     const RowSpan rows = rows_of(tok, tok.base + local);
-    for (int i = threadIdx.x; i < kEmbedChunk; i += 1024) {
+    for (int i = threadIdx.x; i < kEmbedChunk; i += kEmbedThreads) {
         const int64_t t = c * kEmbedChunk + i;
         const int64_t id = t < rows.count ? ids[rows.first + t] : -1;
         part[i] = id >= 0 && id < vocab ? (uint64_t)id << 32 | (uint64_t)t : kEmbedNone;
@@ -177,7 +178,8 @@ __global__ __launch_bounds__(1024) void embed_sort(TokenRows tok, int chunks, co
     for (int size = 2; size <= kEmbedChunk; size *= 2)
         for (int gap = size / 2; gap > 0; gap /= 2) {
             __syncthreads();
-            for (int i = threadIdx.x; i < kEmbedChunk / 2; i += 1024) {
+#pragma unroll
+            for (int i = threadIdx.x; i < kEmbedChunk / 2; i += kEmbedThreads) {
                 const int lo = 2 * i - (i & (gap - 1)), hi = lo + gap;
                 const uint64_t a = part[lo], b = part[hi];
                 const bool up = (lo & size) == 0;
@@ -189,137 +191,182 @@ __global__ __launch_bounds__(1024) void embed_sort(TokenRows tok, int chunks, co
         }
     __syncthreads();
     uint64_t *to = keys + (local * chunks + c) * kEmbedChunk;
-    for (int i = threadIdx.x; i < kEmbedChunk; i += 1024) to[i] = part[i];
+    for (int i = threadIdx.x; i < kEmbedChunk; i += kEmbedThreads) to[i] = part[i];
 }
 
-// Number of keys below `key` among the n sorted ones.
-__device__ __forceinline__ int64_t embed_below(const uint64_t *keys, int64_t n, uint64_t key) {
-    int64_t lo = 0, hi = n;
-    while (lo < hi) {
-        const int64_t mid = (lo + hi) >> 1;
-        if (keys[mid] < key) lo = mid + 1;
-        else hi = mid;
-    }
-    return lo;
-}
-
-// kEmbedFan sorted runs of `run` keys each become one: a key's place is the number of smaller ones in all of them.  (Keys are distinct but
-// for those of no row, which keep the runs' order.)
-__global__ __launch_bounds__(256) void embed_merge(const uint64_t *__restrict__ from, uint64_t *__restrict__ to, int64_t len, int64_t run)
+// kEmbedFan sorted runs of `run` keys each become one: a key's place is the number of smaller ones in all of them.  A wavefront counts
+// those of one run, for 64 keys side by side, whose searches go the same way and read the same lines (a lane per run instead: 18 us a
+// pass over 65 536 keys).  (Keys are distinct but for those of no row, which keep the runs' order.)
+__global__ __launch_bounds__(64 * kEmbedFan) void embed_merge(const uint64_t *__restrict__ from, uint64_t *__restrict__ to, int64_t len,
+                                                              int64_t run)
 {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= len) return;
+    __shared__ int below[kEmbedFan][64];
+    const int lane = threadIdx.x & 63, r = threadIdx.x >> 6;
+    const int64_t i = (int64_t)blockIdx.x * 64 + lane;  // (len and run are multiples of 64)
     const uint64_t *keys = from + blockIdx.y * len;
     const uint64_t key = keys[i];
-    const int64_t mine = i / run, group = mine / kEmbedFan * kEmbedFan;
-    int64_t at = i - mine * run;
-#pragma unroll
-    for (int r = 0; r < kEmbedFan; ++r) {
-        const int64_t begin = (group + r) * run;
-        if (group + r == mine || begin >= len) continue;
-        const int64_t n = len - begin < run ? len - begin : run;
-        at += key != kEmbedNone ? embed_below(keys + begin, n, key) : group + r < mine ? n : embed_below(keys + begin, n, key);
+    const int64_t mine = i / run, group = mine / kEmbedFan * kEmbedFan, begin = (group + r) * run;
+    const int64_t n = begin >= len ? 0 : len - begin < run ? len - begin : run;
+    int64_t lo = 0, hi = n;
+    if (group + r == mine) lo = hi = i - begin;
+    if (group + r < mine && key == kEmbedNone) lo = hi;
+    while (lo < hi) {
+        const int64_t mid = (lo + hi) >> 1;
+        if (keys[begin + mid] < key) lo = mid + 1;
+        else hi = mid;
     }
-    to[blockIdx.y * len + group * run + at] = key;
+    below[r][lane] = (int)lo;
+    __syncthreads();
+    if (r == 0) {
+        int64_t at = group * run;
+#pragma unroll
+        for (int q = 0; q < kEmbedFan; ++q) at += below[q][lane];
+        to[blockIdx.y * len + at] = key;
+    }
 }
 
-// A group of threads adds up the rows of kEmbedPiece sorted keys.  Runs of one id that lie within the piece go to G; of the others the
-// sums go to parts [piece][2][width]: 0 of a run that has begun in an earlier piece, 1 of one that begins here and goes on.
+// Of a piece of sorted keys that all have one id a group of threads adds up the rows, to parts [piece][width]: frequent ids are shared by
+// many workgroups so.
 template <typename T, int VEC>
 __global__ __launch_bounds__(kEmbedThreads) void embed_grad_pieces(TokenRows tok, int64_t pieces, int shift, const uint64_t *__restrict__ keys,
                                                                    int64_t len, int width, const T *__restrict__ DY, int64_t dy_stride,
-                                                                   float scale, float *__restrict__ G, int64_t g_stride,
                                                                    float *__restrict__ parts)
 {
     const int lanes = 1 << shift, t = threadIdx.x & (lanes - 1);
     const int64_t unit = (int64_t)blockIdx.x * (kEmbedThreads >> shift) + (threadIdx.x >> shift);
     if (unit >= pieces * tok.examples) return;
-    const int64_t local = unit / pieces, piece = unit - local * pieces, e = tok.base + local;
-    const RowSpan rows = rows_of(tok, e);
-    const uint64_t *list = keys + local * len, *k = list + piece * kEmbedPiece;
-    if (k[0] == kEmbedNone) return;
-    const bool before = piece > 0 && k[-1] >> 32 == k[0] >> 32;
-    const T *dy = DY + rows.first * dy_stride;
-    float *g = G + e * g_stride, *part = parts + unit * 2 * width;
+    const int64_t local = unit / pieces, piece = unit - local * pieces;
+    const uint64_t *k = keys + local * len + piece * kEmbedPiece;
+    if (k[kEmbedPiece - 1] == kEmbedNone || k[0] >> 32 != k[kEmbedPiece - 1] >> 32) return;
+    const T *dy = DY + rows_of(tok, tok.base + local).first * dy_stride;
     for (int col = t * VEC; col < width; col += lanes * VEC) {
         const int at = col + VEC <= width ? col : width - VEC;
         float sum[VEC];
 #pragma unroll
         for (int i = 0; i < VEC; ++i) sum[i] = 0.f;
-        bool begun = before;
-        uint64_t key = k[0];
-        for (int j0 = 0; j0 < kEmbedPiece; j0 += 8) {
-            if (k[j0] == kEmbedNone) break;
-            T x[8][VEC];
-            uint64_t next[9];
+        embed_sum<T, VEC>(dy, dy_stride, at, kEmbedPiece, [&](int j) { return (int64_t)(k[j] & 0xffffffffu); }, sum);
+        store_any<float, VEC>(parts + unit * width + at, sum);
+    }
+}
+
+// Number of the n sorted keys below `key`: all threads of the workgroup look at once, 256 places at a time.
+__device__ __forceinline__ int64_t embed_below(const uint64_t *keys, int64_t n, uint64_t key) {
+    int64_t lo = 0;
+    while (n > 0) {  // uniform
+        const int64_t gap = (n + kEmbedThreads - 1) / kEmbedThreads, at = threadIdx.x * gap;
+        const int below = __syncthreads_count(at < n && keys[lo + at] < key);
+        if (below == 0) break;  // (the first place is not below)
+        // places 0 .. below - 1 are: the answer lies behind the last of them, within its gap
+        const int64_t last = (below - 1) * gap;
+        lo += last + 1;
+        n = (last + gap < n ? last + gap : n) - last - 1;
+    }
+    return lo;
+}
+
+// embed_grad_few for sorted keys, but for the ids of many rows.
+template <typename T, int VEC, bool ONCE>
+__device__ __forceinline__ void embed_span(uint32_t *lds, const uint64_t *list, int64_t len, int64_t v0, int own, int shift, int width,
+                                           const T *dy, int64_t dy_stride, float scale, float *g)
+{
+    uint32_t *const start = lds, *const stop = lds + kEmbedSpan, *const found = lds + 2 * kEmbedSpan;
+    for (int v = threadIdx.x; v < own; v += kEmbedThreads) start[v] = stop[v] = 0;
+    const int64_t begin = embed_below(list, len, (uint64_t)v0 << 32);
+    const int64_t m = embed_below(list + begin, len - begin, (uint64_t)(v0 + own) << 32);
+    list += begin;
+    __syncthreads();
+    for (int64_t i = threadIdx.x; i < m; i += kEmbedThreads) {
+        const uint64_t key = list[i];
+        const int v = (int)((int64_t)(key >> 32) - v0);
+        if (i < kEmbedList) found[i] = (uint32_t)key;
+        if (i == 0 || list[i - 1] >> 32 != key >> 32) start[v] = (uint32_t)i;
+        if (i == m - 1 || list[i + 1] >> 32 != key >> 32) stop[v] = (uint32_t)i + 1;
+    }
+    __syncthreads();
+    const int lanes = 1 << shift, t = threadIdx.x & (lanes - 1), groups = kEmbedThreads >> shift;
+    float *to = g + v0 * width;
+    const bool here = m <= kEmbedList;  // uniform
+    for (int v = threadIdx.x >> shift; v < own; v += groups) {
+        const int64_t j0 = start[v], count = stop[v] - j0;
+        if (count >= kEmbedPiece) continue;
+        for (int col = t * VEC; col < width; col += lanes * VEC) {
+            const int at = col + VEC <= width ? col : width - VEC;
+            float sum[VEC];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                next[j] = k[j0 + j];
-                if (next[j] != kEmbedNone) load_any<T, VEC>(dy + (int64_t)(next[j] & 0xffffffffu) * dy_stride + at, x[j]);
+            for (int i = 0; i < VEC; ++i) sum[i] = 0.f;
+            if (count > 0) {
+                if (here) embed_sum<T, VEC>(dy, dy_stride, at, (int)count, [&](int j) { return (int64_t)found[j0 + j]; }, sum);
+                else embed_sum<T, VEC>(dy, dy_stride, at, (int)count, [&](int j) { return (int64_t)(uint32_t)list[j0 + j]; }, sum);
             }
-            const int64_t behind = piece * kEmbedPiece + j0 + 8;
-            next[8] = behind < len ? list[behind] : kEmbedNone;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                if (next[j] == kEmbedNone) break;
-                key = next[j];
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) sum[i] += (float)x[j][i];
-                const bool same = next[j + 1] >> 32 == key >> 32;
-                if (same && j0 + j + 1 < kEmbedPiece) continue;
-                if (!begun && !same) {
-#pragma unroll
-                    for (int i = 0; i < VEC; ++i) sum[i] *= scale;
-                    store_any<float, VEC>(g + (int64_t)(key >> 32) * width + at, sum);
-                } else {
-                    store_any<float, VEC>(part + (begun ? 0 : width) + at, sum);
-                }
-                begun = false;
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) sum[i] = 0.f;
-            }
+            for (int i = 0; i < VEC; ++i) sum[i] *= scale;
+            store_any<float, VEC, ONCE>(to + (int64_t)v * width + at, sum);
         }
     }
 }
 
-// The rest of G: zeros, and runs of several pieces.
-template <int VEC>
-__global__ __launch_bounds__(kEmbedThreads) void embed_grad_rest(TokenRows tok, uint32_t units, int span, int shift, int64_t pieces,
-                                                                 const uint64_t *__restrict__ keys, int64_t len, int64_t vocab, int width,
-                                                                 float scale, const float *__restrict__ parts, float *__restrict__ G,
-                                                                 int64_t g_stride)
+// Ids of kEmbedPiece rows and more: a workgroup each, that of the piece in which the id's keys begin (of no two ids: the first would
+// fill the piece).  Rows up to the first whole piece, whole pieces, the rest; in this order.
+template <typename T, int VEC>
+__device__ __forceinline__ void embed_long(float *part, const uint64_t *list, int64_t len, int64_t piece, int shift, int width, const T *dy,
+                                           int64_t dy_stride, float scale, const float *parts, float *g)
 {
-    __shared__ int64_t start[kEmbedSpan + 1];
-    __shared__ float part[kEmbedThreads * VEC];
-    const uint32_t local = blockIdx.x / units;
-    const int64_t e = tok.base + local, v0 = (int64_t)(blockIdx.x - local * units) * span;
-    const int own = (int)(vocab - v0 < span ? vocab - v0 : span);
+    int64_t j0 = -1;
+#pragma unroll
+    for (int j = 0; j < kEmbedPiece; ++j) {  // (uniform, and at most one)
+        const int64_t i = piece * kEmbedPiece + j, last = i + kEmbedPiece - 1;
+        if (last < len && list[last] != kEmbedNone && list[last] >> 32 == list[i] >> 32 && (i == 0 || list[i - 1] >> 32 != list[i] >> 32))
+            j0 = i;
+    }
+    if (j0 < 0) return;
+    const uint64_t id = list[j0] >> 32;
+    const int64_t j1 = j0 + embed_below(list + j0, len - j0, (id + 1) << 32);
+    const int64_t p0 = (j0 + kEmbedPiece - 1) / kEmbedPiece, p1 = j1 / kEmbedPiece;
+    const int whole = p1 > p0 ? (int)(p1 - p0) : 0;
+    const int head = (int)(whole ? p0 * kEmbedPiece - j0 : j1 - j0), tail = (int)(whole ? j1 - p1 * kEmbedPiece : 0);
+    const float *from = parts + p0 * width;
+    float *to = g + (int64_t)id * width;
+    const auto rows_sum = [&](int at, const uint64_t *k, int count, float (&sum)[VEC]) {
+        embed_sum<T, VEC>(dy, dy_stride, at, count, [&](int j) { return (int64_t)(uint32_t)k[j]; }, sum);
+    };
+    embed_shared<VEC>(shift, width, head + whole + tail, part,
+                      [&](int at, int a, int count, float (&sum)[VEC]) {
+                          const int b = a + count;
+                          if (a < head) rows_sum(at, list + j0 + a, (b < head ? b : head) - a, sum);
+                          const int pa = a > head ? a - head : 0, pb = b - head < whole ? b - head : whole;
+                          if (pb > pa) embed_sum<float, VEC>(from, width, at, pb - pa, [&](int j) { return (int64_t)(pa + j); }, sum);
+                          const int ta = a > head + whole ? a - head - whole : 0, tb = b - head - whole;
+                          if (tb > ta) rows_sum(at, list + p1 * kEmbedPiece + ta, tb - ta, sum);
+                      },
+                      [&](int at, float (&sum)[VEC]) {
+#pragma unroll
+                          for (int i = 0; i < VEC; ++i) sum[i] *= scale;
+                          store_any<float, VEC>(to + at, sum);
+                      });
+}
+
+// Both, the ids of many rows first: they take longest, and the others fill the chip beside them (one after the other 50 + 24 us).
+template <typename T, int VEC, bool ONCE>
+__global__ __launch_bounds__(kEmbedThreads) void embed_grad_many(TokenRows tok, uint32_t units, int span, int shift, uint32_t pieces,
+                                                                 const uint64_t *__restrict__ keys, int64_t len, int64_t vocab, int width,
+                                                                 const T *__restrict__ DY, int64_t dy_stride, float scale,
+                                                                 const float *__restrict__ parts, float *__restrict__ G, int64_t g_stride)
+{
+    __shared__ uint32_t lds[2 * kEmbedSpan + kEmbedList];
+    static_assert(sizeof(lds) >= kEmbedThreads * VEC * sizeof(float), "");
+    const uint32_t longs = pieces * (uint32_t)tok.examples;  // workgroups
+    const bool many = blockIdx.x < longs;                    // uniform
+    const uint32_t b = many ? blockIdx.x : blockIdx.x - longs, local = b / (many ? pieces : units), at = b - local * (many ? pieces : units);
+    const int64_t e = tok.base + local;
     const uint64_t *list = keys + local * len;
-    for (int v = threadIdx.x; v <= own; v += kEmbedThreads) start[v] = embed_below(list, len, (uint64_t)(v0 + v) << 32);
-    __syncthreads();
-    const int lanes = 1 << shift, t = threadIdx.x & (lanes - 1), groups = kEmbedThreads >> shift;
-    float *to = G + e * g_stride + v0 * width;
-    const float *from = parts + local * pieces * 2 * width;
-    float none[VEC];
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) none[i] = 0.f;
-    for (int v = threadIdx.x >> shift; v < own; v += groups)
-        if (start[v] == start[v + 1])
-            for (int col = t * VEC; col < width; col += lanes * VEC)
-                store_any<float, VEC>(to + (int64_t)v * width + (col + VEC <= width ? col : width - VEC), none);
-    for (int v = 0; v < own; ++v) {  // uniform
-        const int64_t first = start[v] / kEmbedPiece, last = (start[v + 1] - 1) / kEmbedPiece;
-        if (start[v] == start[v + 1] || first == last) continue;
-        embed_shared<VEC>(shift, width, (int)(last - first + 1), part,
-                          [&](int at, int j0, int count, float (&sum)[VEC]) {
-                              embed_sum<float, VEC>(from, width, at, count,
-                                                    [&](int j) { return (first + j0 + j) * 2 + (j0 + j == 0 ? 1 : 0); }, sum);
-                          },
-                          [&](int at, float (&sum)[VEC]) {
-#pragma unroll
-                              for (int i = 0; i < VEC; ++i) sum[i] *= scale;
-                              store_any<float, VEC>(to + (int64_t)v * width + at, sum);
-                          });
+    const T *dy = DY + rows_of(tok, e).first * dy_stride;
+    float *g = G + e * g_stride;
+    if (many) {
+        embed_long<T, VEC>(reinterpret_cast<float *>(lds), list, len, at, shift, width, dy, dy_stride, scale,
+                           parts + (int64_t)local * pieces * width, g);
+    } else {
+        const int64_t v0 = (int64_t)at * span;
+        embed_span<T, VEC, ONCE>(lds, list, len, v0, (int)(vocab - v0 < span ? vocab - v0 : span), shift, width, dy, dy_stride, scale, g);
     }
 }
 

@@ -48,131 +48,147 @@ struct HeadShape {
 // Cosines and sines of `rows` positions from `at` on.
 __device__ __forceinline__ void head_angles(float2 *table, const HeadTurns &turns, int64_t at, int rows, int half) {
     for (int q = threadIdx.x; q < rows * half; q += kHeadThreads) {
-        const int r = q / half, i = q - r * half;
+        const uint32_t r = (uint32_t)q / (uint32_t)half, i = q - r * half;
         table[q] = cos_sin_turns((uint64_t)(at + r) * turns.turn[i]);
     }
 }
 
-// Workgroup b takes chunk b % chunks of the rows of example b / chunks, `rows` rows at a time; LANES threads a head.
-// BACKWARD: DY and DX in the place of Y; the gains' gradients [2][dim] to G or to `partial` [examples][chunks][2 dim].
-template <typename T, int VEC, int LANES, bool BACKWARD>
+// Sum over the lanes of a wavefront that hold the same place of their heads: every LANES-th.
+template <int LANES>
+__device__ __forceinline__ float heads_sum(float x) {
+    if constexpr (LANES <= 8) x = dpp_add_f32<0x128>(x);  // row_ror 8, 4, 2, 1
+    if constexpr (LANES <= 4) x = dpp_add_f32<0x124>(x);
+    if constexpr (LANES <= 2) x = dpp_add_f32<0x122>(x);
+    if constexpr (LANES <= 1) x = dpp_add_f32<0x121>(x);
+    if constexpr (LANES <= 16) {
+        const auto p = __builtin_amdgcn_permlane16_swap(__float_as_int(x), __float_as_int(x), false, false);
+        x = __int_as_float((int)p[0]) + __int_as_float((int)p[1]);
+    }
+    if constexpr (LANES <= 32) {
+        const auto p = __builtin_amdgcn_permlane32_swap(__float_as_int(x), __float_as_int(x), false, false);
+        x = __int_as_float((int)p[0]) + __int_as_float((int)p[1]);
+    }
+    return x;
+}
+
+// Workgroup b takes chunk b % chunks of the rows of example b / chunks, the queries' heads and then the keys', `rows` rows at a time;
+// LANES threads a head.  BACKWARD: DY and DX in the place of Y; the gains' gradients [2][dim] to G or to `partial` [examples][chunks][2 dim].
+// ONCE: rows that the caches do not hold anyway are read past them, and DX is written past them (20 000 rows of 40 heads of 128, bf16 148 -> 143
+// us; Y, which is read next, is not: 65 536 rows of 24 of 64 102 -> 106).
+template <typename T, int VEC, int LANES, bool BACKWARD, bool ONCE>
 __global__ __launch_bounds__(kHeadThreads) void head_norm(
     TokenRows tok, int chunks, HeadShape sh, HeadTurns turns, const T *__restrict__ X, int64_t x_stride, const T *__restrict__ DY,
     int64_t dy_stride, const float *__restrict__ gain_q, const float *__restrict__ gain_k, T *__restrict__ Y, int64_t y_stride,
     float *__restrict__ G, int64_t g_stride, float *__restrict__ partial)
 {
-    constexpr int GROUPS = kHeadThreads / LANES;
+    constexpr int GROUPS = kHeadThreads / LANES, WAVES = kHeadThreads / 64;
     __shared__ float2 table[kHeadTable];
-    __shared__ float part[BACKWARD ? GROUPS * LANES * VEC : 1];
+    static_assert(sizeof(table) >= WAVES * kHeadMaxDim * sizeof(float), "the wavefronts' sums take its place");
     const int t = threadIdx.x % LANES, mine = threadIdx.x / LANES, half = sh.half;
     const NormSlice<VEC, LANES, 1> sl(t, half);
     const int pos = sl.pos[0];
     const int64_t e = tok.base + blockIdx.x / chunks;
     const int c = (int)(blockIdx.x % chunks);
     const RowSpan span = rows_of(tok, e);
-    const int64_t per = ((span.count + chunks - 1) / chunks + sh.rows - 1) / sh.rows * sh.rows;
+    const int64_t per = (span.count + chunks - 1) / chunks;
     const int64_t t0 = c * per < span.count ? c * per : span.count, t1 = t0 + per < span.count ? t0 + per : span.count;
-    float wq[2][VEC], wk[2][VEC], dq[2][VEC], dk[2][VEC];
-#pragma unroll
-    for (int p = 0; p < 2; ++p)
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-            wq[p][j] = gain_q ? gain_q[p * half + pos + j] : 1.f;
-            wk[p][j] = gain_k ? gain_k[p * half + pos + j] : 1.f;
-            dq[p][j] = dk[p][j] = 0.f;
-        }
     const float inv = 0.5f / (float)half;
-    for (int64_t at = t0; at < t1; at += sh.rows) {
-        const int rows = (int)(t1 - at < sh.rows ? t1 - at : sh.rows);
-        __syncthreads();  // (the last rows' angles have been read)
-        head_angles(table, turns, at, rows, half);
-        __syncthreads();
-        const int items = rows * sh.heads;
-        for (int base = 0; base < items; base += GROUPS) {
-            const int item = base + mine < items ? base + mine : items - 1;
-            const bool live = base + mine < items;
-            const int r = item / sh.heads, head = item - r * sh.heads;
-            const bool query = head < sh.q_heads;
-            const int64_t row = span.first + at + r;
-            const int64_t off = (int64_t)head * 2 * half + pos;
-            T x[2][VEC], dy[2][VEC];
+    for (int keys = 0; keys < 2; ++keys) {
+        const int heads = keys ? sh.heads - sh.q_heads : sh.q_heads;
+        const float *gain = keys ? gain_k : gain_q;
+        float w[2][VEC], dw[2][VEC];
 #pragma unroll
-            for (int p = 0; p < 2; ++p) {
-                load_any<T, VEC>(X + row * x_stride + off + p * half, x[p]);
-                if constexpr (BACKWARD) load_any<T, VEC>(DY + row * dy_stride + off + p * half, dy[p]);
+        for (int p = 0; p < 2; ++p)
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                w[p][j] = gain ? gain[p * half + pos + j] : 1.f;
+                dw[p][j] = 0.f;
             }
-            const float2 *turn = table + r * half + pos;
-            if constexpr (!BACKWARD) {
-                float ss = 0.f;
-#pragma unroll
-                for (int p = 0; p < 2; ++p)
-#pragma unroll
-                    for (int j = 0; j < VEC; ++j) ss = sl.own(0, j) ? fmaf((float)x[p][j], (float)x[p][j], ss) : ss;
-                ss = lanes_sum<LANES>(ss);
-                const float rs = 1.f / sqrtf(fmaf(ss, inv, sh.eps)) + (ss - ss);  // (NaN of a sum that is not finite)
-                T y[2][VEC];
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) {
-                    const float2 cs = turn[j];
-                    const float a = (float)x[0][j] * rs * (query ? wq[0][j] : wk[0][j]), b = (float)x[1][j] * rs * (query ? wq[1][j] : wk[1][j]);
-                    y[0][j] = (T)fmaf(a, cs.x, -(b * cs.y));
-                    y[1][j] = (T)fmaf(b, cs.x, a * cs.y);
-                }
-                if (live && sl.any(0))
-#pragma unroll
-                    for (int p = 0; p < 2; ++p) store_any<T, VEC>(Y + row * y_stride + off + p * half, y[p]);
-            } else {
-                float u[2][VEC], s[2] = {0.f, 0.f};  // sums of x^2, g x
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) {
-                    const float2 cs = turn[j];
-                    const float a = (float)dy[0][j], b = (float)dy[1][j];
-                    u[0][j] = fmaf(a, cs.x, b * cs.y);
-                    u[1][j] = fmaf(b, cs.x, -(a * cs.y));
-#pragma unroll
-                    for (int p = 0; p < 2; ++p) {
-                        const float v = sl.own(0, j) ? (float)x[p][j] : 0.f;
-                        s[0] = fmaf(v, v, s[0]);
-                        s[1] = fmaf(u[p][j] * (query ? wq[p][j] : wk[p][j]), v, s[1]);
-                    }
-                }
-                s[0] = lanes_sum<LANES>(s[0]);
-                s[1] = lanes_sum<LANES>(s[1]);
-                const float rs = 1.f / sqrtf(fmaf(s[0], inv, sh.eps)) + (s[0] - s[0]);
-                const float mean = s[1] * rs * inv;
+        for (int64_t at = t0; at < t1; at += sh.rows) {
+            const int rows = (int)(t1 - at < sh.rows ? t1 - at : sh.rows), items = rows * heads;
+            if (!keys || at > t0 || rows < t1 - t0 || BACKWARD) {  // (else the table is there)
+                __syncthreads();  // (the last rows' angles have been read)
+                head_angles(table, turns, at, rows, half);
+                __syncthreads();
+            }
+            for (int base = 0; base < items; base += GROUPS) {  // (uniform: what is beyond the last is not written)
+                const bool live = base + mine < items;
+                const uint32_t item = (uint32_t)(live ? base + mine : items - 1), r = item / (uint32_t)heads;
+                const int64_t row = span.first + at + r, off = (int64_t)(item - r * heads + (keys ? sh.q_heads : 0)) * 2 * half + pos;
+                T x[2][VEC], dy[2][VEC];
 #pragma unroll
                 for (int p = 0; p < 2; ++p) {
-                    T out[VEC];
+                    load_any<T, VEC, ONCE>(X + row * x_stride + off + p * half, x[p]);
+                    if constexpr (BACKWARD) load_any<T, VEC, ONCE>(DY + row * dy_stride + off + p * half, dy[p]);
+                }
+                const float2 *turn = table + r * half + pos;
+                T y[2][VEC];
+                if constexpr (!BACKWARD) {
+                    float ss = 0.f;
+#pragma unroll
+                    for (int p = 0; p < 2; ++p)
+#pragma unroll
+                        for (int j = 0; j < VEC; ++j) ss = sl.own(0, j) ? fmaf((float)x[p][j], (float)x[p][j], ss) : ss;
+                    ss = lanes_sum<LANES>(ss);
+                    const float rs = 1.f / sqrtf(fmaf(ss, inv, sh.eps)) + (ss - ss);  // (NaN of a sum that is not finite)
 #pragma unroll
                     for (int j = 0; j < VEC; ++j) {
-                        const float hat = (float)x[p][j] * rs;
-                        out[j] = (T)(rs * fmaf(u[p][j], query ? wq[p][j] : wk[p][j], -(hat * mean)));
-                        const float add = u[p][j] * hat;
-                        if (live) {
-                            if (query) dq[p][j] += add;
-                            else dk[p][j] += add;
+                        const float2 cs = turn[j];
+                        const float a = (float)x[0][j] * rs * w[0][j], b = (float)x[1][j] * rs * w[1][j];
+                        y[0][j] = (T)fmaf(a, cs.x, -(b * cs.y));
+                        y[1][j] = (T)fmaf(b, cs.x, a * cs.y);
+                    }
+                } else {
+                    float u[2][VEC], s[2] = {0.f, 0.f};  // sums of x^2, g x
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) {
+                        const float2 cs = turn[j];
+                        const float a = (float)dy[0][j], b = (float)dy[1][j];
+                        u[0][j] = fmaf(a, cs.x, b * cs.y);
+                        u[1][j] = fmaf(b, cs.x, -(a * cs.y));
+#pragma unroll
+                        for (int p = 0; p < 2; ++p) {
+                            const float v = sl.own(0, j) ? (float)x[p][j] : 0.f;
+                            s[0] = fmaf(v, v, s[0]);
+                            s[1] = fmaf(u[p][j] * w[p][j], v, s[1]);
                         }
                     }
-                    if (Y && live && sl.any(0)) store_any<T, VEC>(Y + row * y_stride + off + p * half, out);
+                    s[0] = lanes_sum<LANES>(s[0]);
+                    s[1] = lanes_sum<LANES>(s[1]);
+                    const float rs = 1.f / sqrtf(fmaf(s[0], inv, sh.eps)) + (s[0] - s[0]);
+                    const float mean = s[1] * rs * inv;
+#pragma unroll
+                    for (int p = 0; p < 2; ++p)
+#pragma unroll
+                        for (int j = 0; j < VEC; ++j) {
+                            const float hat = (float)x[p][j] * rs;
+                            y[p][j] = (T)(rs * fmaf(u[p][j], w[p][j], -(hat * mean)));
+                            if (live) dw[p][j] = fmaf(u[p][j], hat, dw[p][j]);
+                        }
                 }
+                if ((!BACKWARD || Y) && live && sl.any(0))
+#pragma unroll
+                    for (int p = 0; p < 2; ++p) store_any<T, VEC, BACKWARD && ONCE>(Y + row * y_stride + off + p * half, y[p]);
             }
         }
-    }
-    if constexpr (BACKWARD) {
-        if (!G && !partial) return;
-        float *to = chunks > 1 ? partial + (e * chunks + c) * 4 * half : G + e * g_stride;
-#pragma unroll
-        for (int which = 0; which < 4; ++which) {
+        if constexpr (BACKWARD) {
+            if (!G && !partial) continue;
+            float *part = reinterpret_cast<float *>(table);  // [WAVES][2 half]
             __syncthreads();
 #pragma unroll
-            for (int j = 0; j < VEC; ++j)
-                if (sl.own(0, j)) part[mine * LANES * VEC + pos + j] = which < 2 ? dq[which & 1][j] : dk[which & 1][j];
+            for (int p = 0; p < 2; ++p)
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    const float sum = heads_sum<LANES>(dw[p][j]);
+                    if ((threadIdx.x & 63) < LANES && sl.own(0, j)) part[(threadIdx.x >> 6) * 2 * half + p * half + pos + j] = sum;
+                }
             __syncthreads();
-            for (int col = threadIdx.x; col < half; col += kHeadThreads) {
+            float *to = (chunks > 1 ? partial + (e * chunks + c) * 4 * half : G + e * g_stride) + keys * 2 * half;
+            for (int col = threadIdx.x; col < 2 * half; col += kHeadThreads) {
                 float sum = 0.f;
-#pragma unroll 8
-                for (int g = 0; g < GROUPS; ++g) sum += part[g * LANES * VEC + col];
-                to[which * half + col] = sum;
+#pragma unroll
+                for (int q = 0; q < WAVES; ++q) sum += part[q * 2 * half + col];
+                to[col] = sum;
             }
         }
     }

@@ -30,7 +30,7 @@ __device__ __forceinline__ void load_any(const T *p, T (&v)[N]) {
         for (int j = 0; j < N; ++j) v[j] = x[j];
     }
 }
-template <typename T, int N>
+template <typename T, int N, bool ONCE = false>
 __device__ __forceinline__ void store_any(T *p, const T (&v)[N]) {
     if constexpr (N == 1) {
         *p = v[0];
@@ -38,7 +38,12 @@ __device__ __forceinline__ void store_any(T *p, const T (&v)[N]) {
         typename AnyVec<T, N>::type x;
 #pragma unroll
         for (int j = 0; j < N; ++j) x[j] = v[j];
-        *reinterpret_cast<typename AnyVec<T, N>::type *>(p) = x;
+        if constexpr (ONCE && N * sizeof(T) == 16) {
+            typedef uint32_t words __attribute__((ext_vector_type(4), aligned(2)));
+            __builtin_nontemporal_store(__builtin_bit_cast(words, x), reinterpret_cast<words *>(p));
+        } else {
+            *reinterpret_cast<typename AnyVec<T, N>::type *>(p) = x;
+        }
     }
 }
 

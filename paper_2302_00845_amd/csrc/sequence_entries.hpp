@@ -40,45 +40,52 @@ int row_shift(int64_t width, int64_t vec) {
     return s;
 }
 
+constexpr int64_t kOnceBytes = (int64_t)64 << 20;  // of an array from which on it is written past the caches
+
 template <typename TT, typename T>
 int run_embed(cdgrab_handle *h, const int32_t *ids, int64_t rows, int64_t vocab, int64_t width, const void *table, int64_t t_stride,
               float scale, void *Y, int64_t y_stride) {
     constexpr int VEC = 16 / (int)sizeof(T);
-    const auto launch = [&](auto vec) {
+    const auto launch = [&](auto vec, auto once) {
         constexpr int V = decltype(vec)::value;
         const int shift = row_shift(width, V);
         const int64_t per = kEmbedThreads >> shift, groups = std::min<int64_t>((rows + per - 1) / per, 8 * (int64_t)h->num_cu);
-        hipLaunchKernelGGL((embed_forward<TT, T, V>), dim3((unsigned)groups), dim3(kEmbedThreads), 0, h->stream, ids, rows, vocab, (int)width,
+        hipLaunchKernelGGL((embed_forward<TT, T, V, decltype(once)::value>), dim3((unsigned)groups), dim3(kEmbedThreads), 0, h->stream, ids, rows, vocab, (int)width,
                            shift, (const TT *)table, t_stride, scale, (T *)Y, y_stride);
     };
-    if (width < VEC) launch(std::integral_constant<int, 1>{});
-    else launch(std::integral_constant<int, VEC>{});
+    if (width < VEC) launch(std::integral_constant<int, 1>{}, std::false_type{});
+    else if (rows * width * (int64_t)sizeof(T) < kOnceBytes) launch(std::integral_constant<int, VEC>{}, std::false_type{});
+    else launch(std::integral_constant<int, VEC>{}, std::true_type{});
     HIP_TRY(h, hipGetLastError());
     return CDGRAB_OK;
 }
 
-template <typename T, int VEC>
+template <typename T, int VEC, bool ONCE>
 int run_embed_grad(cdgrab_handle *h, const char *who, const TokenRows &tok, int64_t vocab, int64_t width, const int32_t *ids, const T *DY,
                    int64_t dy_stride, float scale, float *G, int64_t g_stride) {
     const int shift = row_shift(width, VEC);
-    const int64_t span = std::min<int64_t>(std::max<int64_t>(1, kEmbedElems / width), std::min<int64_t>(kEmbedSpan, vocab));
-    const int64_t units = (vocab + span - 1) / span, tokens = std::min(tok.tokens, tok.rows);
+    const int64_t tokens = std::min(tok.tokens, tok.rows);
+    // rows of G per workgroup: stretches of kEmbedElems, or shorter ones until there are 32 workgroups per CU (the first ids are the
+    // frequent ones of most vocabularies: a workgroup that has many of them is the last to end)
+    const int64_t elems = std::max<int64_t>(1024, std::min<int64_t>(kEmbedElems, tok.examples * vocab * width / (32 * (int64_t)h->num_cu)));
+    const int64_t span = std::min<int64_t>(std::max<int64_t>(1, elems / width), std::min<int64_t>(kEmbedSpan, vocab));
+    const int64_t units = (vocab + span - 1) / span;
     if (tokens <= kEmbedList) {
         const int64_t per = std::max<int64_t>(1, kMaxGroups / units);
         for (int64_t e0 = 0; e0 < tok.examples; e0 += per) {
             TokenRows part = tok;
             part.examples = std::min(per, tok.examples - e0);
             part.base = e0;
-            hipLaunchKernelGGL((embed_grad_few<T, VEC>), dim3((unsigned)(part.examples * units)), dim3(kEmbedThreads), 0, h->stream, part,
+            hipLaunchKernelGGL((embed_grad_few<T, VEC, ONCE>), dim3((unsigned)(part.examples * units)), dim3(kEmbedThreads), 0, h->stream, part,
                                (uint32_t)units, (int)span, shift, ids, vocab, (int)width, DY, dy_stride, scale, G, g_stride);
         }
         HIP_TRY(h, hipGetLastError());
         return CDGRAB_OK;
     }
     const int64_t chunks = (tokens + kEmbedChunk - 1) / kEmbedChunk, len = chunks * kEmbedChunk, pieces = len / kEmbedPiece;
-    const int64_t bytes = len * 16 + pieces * 2 * width * 4;  // of an example
+    const int64_t bytes = len * 16 + pieces * width * 4;  // of an example
     const int64_t lanes = kEmbedThreads >> shift;
-    const int64_t at_once = std::max<int64_t>(1, std::min({tok.examples, kEmbedBytes / bytes, kMaxGroups / std::max(units, chunks),
+    const int64_t at_once = std::max<int64_t>(1, std::min({tok.examples, kEmbedBytes / bytes, kMaxGroups / (units + pieces),
                                                            (int64_t)65535, kMaxGroups * lanes / pieces}));
     char *ws = nullptr;
     const int rc = layer_room(h, who, at_once * bytes, &ws);
@@ -89,16 +96,18 @@ int run_embed_grad(cdgrab_handle *h, const char *who, const TokenRows &tok, int6
         TokenRows part = tok;
         part.examples = std::min(at_once, tok.examples - e0);
         part.base = e0;
-        hipLaunchKernelGGL(embed_sort, dim3((unsigned)(part.examples * chunks)), dim3(1024), 0, h->stream, part, (int)chunks, ids, vocab, keys);
+        hipLaunchKernelGGL(embed_sort, dim3((unsigned)(part.examples * chunks)), dim3(kEmbedThreads), 0, h->stream, part, (int)chunks, ids, vocab,
+                           keys);
         uint64_t *from = keys, *to = other;
         for (int64_t run = kEmbedChunk; run < len; run *= kEmbedFan) {
-            hipLaunchKernelGGL(embed_merge, dim3((unsigned)(len / 256), (unsigned)part.examples), dim3(256), 0, h->stream, from, to, len, run);
+            hipLaunchKernelGGL(embed_merge, dim3((unsigned)(len / 64), (unsigned)part.examples), dim3(64 * kEmbedFan), 0, h->stream, from, to, len, run);
             std::swap(from, to);
         }
         hipLaunchKernelGGL((embed_grad_pieces<T, VEC>), dim3((unsigned)((part.examples * pieces + lanes - 1) / lanes)), dim3(kEmbedThreads), 0,
-                           h->stream, part, pieces, shift, from, len, (int)width, DY, dy_stride, scale, G, g_stride, parts);
-        hipLaunchKernelGGL((embed_grad_rest<VEC>), dim3((unsigned)(part.examples * units)), dim3(kEmbedThreads), 0, h->stream, part,
-                           (uint32_t)units, (int)span, shift, pieces, from, len, vocab, (int)width, scale, parts, G, g_stride);
+                           h->stream, part, pieces, shift, from, len, (int)width, DY, dy_stride, parts);
+        hipLaunchKernelGGL((embed_grad_many<T, VEC, ONCE>), dim3((unsigned)(part.examples * (pieces + units))), dim3(kEmbedThreads), 0, h->stream,
+                           part, (uint32_t)units, (int)span, shift, (uint32_t)pieces, from, len, vocab, (int)width, DY, dy_stride, scale, parts,
+                           G, g_stride);
     }
     HIP_TRY(h, hipGetLastError());
     return CDGRAB_OK;
@@ -121,28 +130,13 @@ int by_head_shape(int half, F &&f) {
 #undef HEAD_SHAPE
 }
 
-// Rows at a time: two rounds of the workgroup's groups of threads at least, and few of them idle in the last.
-int head_rows(int heads, int half, int groups) {
-    const int most = std::max(1, std::min(kHeadTable / half, 64));
-    int best = 1;
-    double least = 1e30;
-    for (int r = 1; r <= most; ++r) {
-        const int items = r * heads, rounds = (items + groups - 1) / groups;
-        const double waste = (double)rounds * groups / items + (rounds < 2 ? 1.0 : 0.0);
-        if (waste < least - 0.02) {
-            least = waste;
-            best = r;
-        }
-    }
-    return best;
-}
-
 HeadTurns head_turns(int half, double base) {
     HeadTurns t{};
-    for (int i = 0; i < half; ++i) {
-        const long double rate = base == 0.0 ? 0.0L : powl((long double)base, -(long double)i / half);  // radians per position
-        t.turn[i] = (uint64_t)(rate / (2.0L * 3.14159265358979323846264338327950288L) * 18446744073709551616.0L);
-    }
+    if (base == 0.0) return t;
+    // (powers of the ratio one after the other: 64 bits, of which 256 products leave 56)
+    const long double ratio = powl((long double)base, -1.0L / half);
+    long double turn = 18446744073709551616.0L / (2.0L * 3.14159265358979323846264338327950288L);  // of one radian per position
+    for (int i = 0; i < half; ++i, turn *= ratio) t.turn[i] = (uint64_t)turn;
     return t;
 }
 
@@ -162,13 +156,18 @@ int run_heads(cdgrab_handle *h, const char *who, const TokenRows &tok, const cdg
               int64_t dy_stride, const float *gain_q, const float *gain_k, T *Y, int64_t y_stride, float *G, int64_t g_stride) {
     const int half = (int)s.dim / 2, heads = (int)(s.q_heads + s.k_heads);
     const HeadTurns turns = head_turns(half, s.base);
+    const int64_t width = heads * s.dim, size = sizeof(T);
+    // (pieces of heads in whole lines: else a line that both halves share is read twice, 257 examples of 200 rows of 10 heads of 80, fp16
+    // 46 -> 55 us; 65 536 rows of 24 heads of 64, bf16 95 -> 91, 20 000 of 40 of 128 back 133 -> 118)
+    const bool once = half * size % 64 == 0 && norm_once(tok.rows, width, size, X, x_stride) && (!BACKWARD || norm_once(tok.rows, width, size, DY, dy_stride));
     return by_head_shape<T>(half, [&](auto vec, auto lanes) {
         constexpr int VEC = decltype(vec)::value, LANES = decltype(lanes)::value;
-        const HeadShape sh{(int)s.q_heads, heads, half, head_rows(heads, half, kHeadThreads / LANES), s.eps};
-        // an example's rows in chunks until the chip is full
-        const int64_t tokens = std::min(tok.tokens, tok.rows), fill = 8 * (int64_t)h->num_cu;
-        const int64_t most = std::max<int64_t>(1, (tokens + sh.rows - 1) / sh.rows);
-        const int64_t chunks = std::min(most, std::max<int64_t>(1, (fill + tok.examples - 1) / tok.examples));
+        // an example's rows in chunks until the chip is full, of a round of the groups of threads at least
+        constexpr int GROUPS = kHeadThreads / LANES;
+        const int64_t tokens = std::min(tok.tokens, tok.rows), fill = 8 * (int64_t)h->num_cu, least = std::max(1, GROUPS / heads);
+        const int64_t chunks = std::min(std::max<int64_t>(1, tokens / least), std::max<int64_t>(1, (fill + tok.examples - 1) / tok.examples));
+        const int64_t each = (tokens + chunks - 1) / chunks;
+        const HeadShape sh{(int)s.q_heads, heads, half, (int)std::max<int64_t>(1, std::min<int64_t>({kHeadTable / half, each, 64})), s.eps};
         float *partial = nullptr;
         if (BACKWARD && G && chunks > 1) {
             const int rc = layer_room(h, who, tok.examples * chunks * 2 * s.dim, &partial);
@@ -179,8 +178,17 @@ int run_heads(cdgrab_handle *h, const char *who, const TokenRows &tok, const cdg
             TokenRows part = tok;
             part.examples = std::min(per, tok.examples - e0);
             part.base = e0;
-            hipLaunchKernelGGL((head_norm<T, VEC, LANES, BACKWARD>), dim3((unsigned)(part.examples * chunks)), dim3(kHeadThreads), 0, h->stream,
-                               part, (int)chunks, sh, turns, X, x_stride, DY, dy_stride, gain_q, gain_k, Y, y_stride, G, g_stride, partial);
+            const auto launch = [&](auto kernel) {
+                hipLaunchKernelGGL(kernel, dim3((unsigned)(part.examples * chunks)), dim3(kHeadThreads), 0, h->stream, part, (int)chunks, sh,
+                                   turns, X, x_stride, DY, dy_stride, gain_q, gain_k, Y, y_stride, G, g_stride, partial);
+            };
+            if constexpr (VEC > 1) {
+                if (once) {
+                    launch(head_norm<T, VEC, LANES, BACKWARD, true>);
+                    continue;
+                }
+            }
+            launch(head_norm<T, VEC, LANES, BACKWARD, false>);
         }
         if (partial)  // (fewer than `fill` examples of at most 32 groups of columns: one launch)
             hipLaunchKernelGGL(norm_grad_finish, dim3((unsigned)(tok.examples * ((2 * s.dim + 31) / 32))), dim3(256), 0, h->stream, partial,
@@ -229,13 +237,15 @@ int by_pieces(int64_t dim, std::initializer_list<Pieces> arrays, F &&f) {
     return f(std::false_type{});
 }
 
-// launch(heads, workgroups) for as many workgroups at a time as a grid holds; `members`: one per tile and head of queries, else of keys
+// launch(heads, workgroups) for as many workgroups at a time as a grid holds; `members`: one per tile and head of queries, else of keys.
+// By pairs if there are so many that the last long ones do not count.
 template <typename F>
-void by_units(const TokenRows &tok, int64_t q_heads, int64_t kv_heads, int64_t dim, float scale, bool members, F &&launch) {
+void by_units(cdgrab_handle *h, const TokenRows &tok, int64_t q_heads, int64_t kv_heads, int64_t dim, float scale, bool members, F &&launch) {
     const int64_t tiles = (std::min(tok.tokens, tok.rows) + kAttRows - 1) / kAttRows, group = q_heads / kv_heads, pairs = tok.examples * kv_heads;
     const int64_t units = round_up(pairs, 8) * tiles * (members ? group : 1);
     for (int64_t u = 0; u < units; u += kMaxGroups)  // (a multiple of eight)
-        launch(AttHeads{pairs, u, (int)tiles, (int)kv_heads, (int)group, (int)dim, scale}, dim3((unsigned)std::min(kMaxGroups, units - u)));
+        launch(AttHeads{pairs, u, (int)tiles, (int)kv_heads, (int)group, members && units >= 8 * (int64_t)h->num_cu, (int)dim, scale},
+               dim3((unsigned)std::min(kMaxGroups, units - u)));
 }
 
 }  // namespace
@@ -288,8 +298,10 @@ extern "C" int cdgrab_pergrad_embed(cdgrab_handle *h, const cdgrab_token_rows *t
     const TokenRows tok{t->examples, t->rows, t->tokens, t->first, t->count, 0};
     return by_elem(type, [&](auto elem) {
         typedef decltype(elem) T;
-        if (width < 4) return run_embed_grad<T, 1>(h, who, tok, vocab, width, ids, (const T *)DY, dy_stride, scale, G, g_stride);
-        return run_embed_grad<T, 4>(h, who, tok, vocab, width, ids, (const T *)DY, dy_stride, scale, G, g_stride);
+        const T *dy = (const T *)DY;
+        if (width < 4) return run_embed_grad<T, 1, false>(h, who, tok, vocab, width, ids, dy, dy_stride, scale, G, g_stride);
+        if (d > kOnceBytes / 4 / t->examples) return run_embed_grad<T, 4, true>(h, who, tok, vocab, width, ids, dy, dy_stride, scale, G, g_stride);
+        return run_embed_grad<T, 4, false>(h, who, tok, vocab, width, ids, dy, dy_stride, scale, G, g_stride);
     });
 }
 
@@ -365,7 +377,7 @@ extern "C" int cdgrab_attention(cdgrab_handle *h, const cdgrab_token_rows *t, in
     return by_elem(type, [&](auto elem) {
         typedef decltype(elem) T;
         return by_head_dim(dim, [&](auto room) { return by_pieces<T>(dim, {{K, k_stride}, {V, v_stride}}, [&](auto direct) {
-            by_units(tok, q_heads, kv_heads, dim, scale, true, [&](const AttHeads &a, dim3 grid) {
+            by_units(h, tok, q_heads, kv_heads, dim, scale, true, [&](const AttHeads &a, dim3 grid) {
                 hipLaunchKernelGGL((attention_forward<T, decltype(room)::value, decltype(direct)::value>), grid, dim3(kAttThreads), 0, h->stream, tok, a, (const T *)Q,
                                    q_stride, (const T *)K, k_stride, (const T *)V, v_stride, (T *)O, o_stride, lse);
             });
@@ -407,7 +419,7 @@ extern "C" int cdgrab_attention_backward(cdgrab_handle *h, const cdgrab_token_ro
         return by_head_dim(dim, [&](auto room) {
             constexpr int D = decltype(room)::value;
             by_pieces<T>(dim, {{K, k_stride}, {V, v_stride}}, [&](auto direct) {
-                by_units(tok, q_heads, kv_heads, dim, scale, true, [&](const AttHeads &a, dim3 grid) {
+                by_units(h, tok, q_heads, kv_heads, dim, scale, true, [&](const AttHeads &a, dim3 grid) {
                     hipLaunchKernelGGL((attention_backward_q<T, D, decltype(direct)::value>), grid, dim3(kAttThreads), 0, h->stream, tok, a,
                                        (const T *)Q, q_stride, (const T *)K, k_stride, (const T *)V, v_stride, (const T *)O, o_stride, lse,
                                        (const T *)DO, do_stride, (T *)DQ, dq_stride, delta);
@@ -415,7 +427,7 @@ extern "C" int cdgrab_attention_backward(cdgrab_handle *h, const cdgrab_token_ro
                 return 0;
             });
             by_pieces<T>(dim, {{Q, q_stride}, {DO, do_stride}}, [&](auto direct) {
-                by_units(tok, q_heads, kv_heads, dim, scale, false, [&](const AttHeads &a, dim3 grid) {
+                by_units(h, tok, q_heads, kv_heads, dim, scale, false, [&](const AttHeads &a, dim3 grid) {
                     hipLaunchKernelGGL((attention_backward_kv<T, D, decltype(direct)::value>), grid, dim3(kAttThreads), 0, h->stream, tok, a,
                                        (const T *)Q, q_stride, (const T *)K, k_stride, (const T *)V, v_stride, lse, (const T *)DO, do_stride,
                                        delta, (T *)DK, dk_stride, (T *)DV, dv_stride);

@@ -450,6 +450,19 @@ def test_values_that_are_not_finite_stay_in_their_example(lib):
     assert not torch.isfinite(o[1, 20:]).any() and torch.isnan(o[1, 30:]).all()
 
 
+def test_attention_of_more_examples_than_a_launch_holds(lib):
+    # one row each: the only weight is one, o = v, dv = do and the others are zero, exactly
+    n, heads, dim = 300_000, 8, 8
+    q, k, v, do = (rand(s, 4, heads * dim, dtype=torch.bfloat16).repeat(n // 4, 1).unsqueeze(1) for s in (1, 2, 3, 4))
+    h = lib.Handle()
+    o, lse = lib.cdgrab_attention(h, q, k, v, q_heads=heads, kv_heads=heads)
+    dq, dk, dv = lib.cdgrab_attention_backward(h, q, k, v, o, lse, do, q_heads=heads, kv_heads=heads)
+    assert torch.equal(o, v) and torch.equal(dv, do)
+    # (do v - do o, both sums of the same eight products in another order: at most 16 roundings of their sizes, times q or k)
+    size = (do.float() * v.float()).abs().sum() / n * 8
+    assert dq.abs().max() <= 16 * U * size * k.abs().max() and dk.abs().max() <= 16 * U * size * q.abs().max()
+
+
 # ---- streams, recordings, the run together ----------------------------------------------------------
 
 def every_call(lib, h, s):
