@@ -457,7 +457,7 @@ int cdgrab_embed(cdgrab_handle *h, int64_t rows, int64_t vocab, int64_t width, c
  * ids outside 0 .. vocab - 1 have no part in it.  One example that holds all rows gives the ordinary gradient.
  *   ids [rows] int32 dev, DY [rows][width] of `type` dev, G: row e at G + e * g_stride, fp32 dev, written whole.
  * Examples of more than 2048 rows use workspace (16 bytes a row, and 4 * width bytes per 16 rows; at most 1 GiB, or one
- * example's).  Sums in fp32.  Errors: EINVAL (as above; tokens > 2^28, more than 2^32 elements per row of G), ENOMEM, EHIP. */
+ * example's).  Sums in fp32.  Errors: EINVAL (as above; tokens > 2^26, more than 2^32 elements per row of G), ENOMEM, EHIP. */
 int cdgrab_pergrad_embed(cdgrab_handle *h, const cdgrab_token_rows *t, int64_t vocab, int64_t width, int32_t type,
                          const int32_t *ids, const void *DY, int64_t dy_stride, float scale, float *G, int64_t g_stride);
 
@@ -496,7 +496,7 @@ int cdgrab_pergrad_headnorm(cdgrab_handle *h, const cdgrab_token_rows *t, const 
  * (fp32: to 2^-24) where they are multiplied with V, sums are fp32.  An element that is not finite makes the results it enters infinite
  * or NaN, and may do so to those of up to 127 rows before it in its example.
  * Errors: EINVAL (sizes, dim > 128, more than 4096 heads, q_heads no multiple of kv_heads, more than 2^22 tokens, type,
- * scale not positive and finite, null, strides, overlap), EHIP. */
+ * scale not within 1e-30 .. 1e30, null, strides, overlap), EHIP. */
 int cdgrab_attention(cdgrab_handle *h, const cdgrab_token_rows *t, int64_t q_heads, int64_t kv_heads, int64_t dim, int32_t type,
                      float scale, const void *Q, int64_t q_stride, const void *K, int64_t k_stride, const void *V,
                      int64_t v_stride, void *O, int64_t o_stride, float *lse);
@@ -505,7 +505,8 @@ int cdgrab_attention(cdgrab_handle *h, const cdgrab_token_rows *t, int64_t q_hea
  *     DQ_i = scale sum_j ds_ij K_j,   DK_j = scale sum_i ds_ij Q_i,   DV_j = sum_i p_ij DO_i,
  * the last two over the heads that share K_j and V_j.
  *   Q, K, V, scale: the forward pass's; O, lse: its outputs; DO as O; DQ as Q, DK and DV as K.
- * p and ds are rounded to `type` (fp32: to 2^-24) where they are multiplied.  Workspace: 4 * rows * q_heads bytes.
+ * p and ds are rounded to `type` (fp32: to 2^-24) where they are multiplied.  Elements that are not finite: as there, and here also for
+ * up to 127 rows behind.  Workspace: 4 * rows * q_heads bytes.
  * Errors: EINVAL (as above), ENOMEM, EHIP. */
 int cdgrab_attention_backward(cdgrab_handle *h, const cdgrab_token_rows *t, int64_t q_heads, int64_t kv_heads, int64_t dim,
                               int32_t type, float scale, const void *Q, int64_t q_stride, const void *K, int64_t k_stride,

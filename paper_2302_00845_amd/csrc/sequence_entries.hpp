@@ -203,9 +203,9 @@ int check_attention(cdgrab_handle *h, const char *who, const cdgrab_token_rows *
     const int rc = check_tokens(h, who, t);
     if (rc) return rc;
     if (q_heads < 1 || kv_heads < 1 || q_heads > kMaxHeads || q_heads % kv_heads != 0 || dim < 1 || dim > kAttMaxDim || bad_type(type) ||
-        !(scale > 0.f && std::isfinite(scale)))
+        !(scale >= 1e-30f && scale <= 1e30f))
         return fail(h, CDGRAB_EINVAL, "%s: bad arguments q_heads=%lld (a multiple of kv_heads, at most %lld) kv_heads=%lld dim=%lld (1 .. %d) "
-                    "type=%d scale=%g (above 0)", who, (long long)q_heads, (long long)kMaxHeads, (long long)kv_heads, (long long)dim,
+                    "type=%d scale=%g (1e-30 .. 1e30)", who, (long long)q_heads, (long long)kMaxHeads, (long long)kv_heads, (long long)dim,
                     kAttMaxDim, (int)type, (double)scale);
     if (std::min(t->tokens, t->rows) > kAttMaxTokens)
         return fail(h, CDGRAB_EINVAL, "%s: %lld tokens of an example, and at most 2^22", who, (long long)std::min(t->tokens, t->rows));
@@ -282,8 +282,8 @@ extern "C" int cdgrab_pergrad_embed(cdgrab_handle *h, const cdgrab_token_rows *t
     int rc = check_tokens(h, who, t);
     if (rc) return rc;
     if (vocab < 1 || vocab > INT32_MAX || width < 1 || width > (1 << 20) || vocab * width > kMaxCells || bad_type(type) || !std::isfinite(scale) ||
-        std::min(t->tokens, t->rows) > ((int64_t)1 << 28))
-        return fail(h, CDGRAB_EINVAL, "%s: bad arguments vocab=%lld width=%lld (1 .. 2^20, 2^32 elements) type=%d scale=%g tokens=%lld (2^28)", who,
+        std::min(t->tokens, t->rows) > ((int64_t)1 << 26))
+        return fail(h, CDGRAB_EINVAL, "%s: bad arguments vocab=%lld width=%lld (1 .. 2^20, 2^32 elements) type=%d scale=%g tokens=%lld (2^26)", who,
                     (long long)vocab, (long long)width, (int)type, (double)scale, (long long)t->tokens);
     if (t->examples == 0) return CDGRAB_OK;
     if (!G || (t->rows > 0 && t->tokens > 0 && (!ids || !DY))) return fail(h, CDGRAB_EINVAL, "%s: null pointer", who);

@@ -388,6 +388,15 @@ def test_attention_of_growing_scores(lib, dtype):
     check_attention(lib, [(0, n)], n, {}, "dense", 1, n, q, k.flip(0).contiguous(), v, do, 1, 1)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("scale", [1e-6, 3.0])
+def test_attention_at_other_scales(lib, scale, dtype):
+    # (all weights alike; and one weight that is nearly everything)
+    n, dim = 150, 40
+    q, k, v, do = (rand(s, n, dim, dtype=dtype) for s in (1, 2, 3, 4))
+    check_attention(lib, [(0, n)], n, {}, "dense", 1, n, q, k, v, do, 1, 1, scale=scale)
+
+
 def test_attention_of_small_fp16_gradients(lib):
     # (ds of these is 1e-9 and less, far below fp16's numbers; the gradients are not)
     n, dim = 700, 64
@@ -620,7 +629,8 @@ def test_refusals(lib):
     o, lse = lib.cdgrab_attention(h, x, x.clone(), x.clone(), **kw)
     refused(lambda: lib.cdgrab_attention(h, x, x, x, O=x, **kw))                     # O on its inputs
     refused(lambda: lib.cdgrab_attention(h, x, x, x, scale=-1.0, **kw))
-    refused(lambda: lib.cdgrab_attention(h, x, x, x, scale=float("inf"), **kw))
+    for scale in (float("inf"), float("nan"), 1e-31, 1e31):
+        refused(lambda: lib.cdgrab_attention(h, x, x, x, scale=scale, **kw))
     wide = torch.zeros(1, 4, 129, device="cuda")
     refused(lambda: lib.cdgrab_attention(h, wide, wide, wide, **kw))                 # a head of 129
     refused(lambda: lib.cdgrab_attention_backward(h, x, x, x, o, lse, x, dQ=x.clone(), dK=o, **kw))
