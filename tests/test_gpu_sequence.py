@@ -371,6 +371,26 @@ def test_attention(lib, n, tokens, hq, hk, dim, kind, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("dim", [8, 24, 40, 72, 104, 120])
+def test_attention_of_heads_narrower_than_their_tiles(lib, dim, dtype):
+    attention_case(lib, 2, 150, 2, 1, dim, "padded", dtype)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("dim", [32, 64, 96, 128])
+def test_attention_of_rows_at_any_element(lib, dim, dtype):
+    """Whole heads, but no row or head at a multiple of sixteen bytes."""
+    spans, rows, kw = layout("packed", [130, 0, 70], 140)
+    every = rand(3, rows, 4 * dim + 3, dtype=dtype)
+    do = rand(4, rows, 2 * dim + 5, scale=0.01, dtype=dtype)
+    mask = owned(spans, rows)
+    every[~mask] = float("nan")
+    do[~mask] = float("nan")
+    q, k, v = every[:, 1:2 * dim + 1], every[:, 2 * dim + 1:3 * dim + 1], every[:, 3 * dim + 2:4 * dim + 2]
+    check_attention(lib, spans, rows, kw, "packed", 3, 140, q, k, v, do[:, 3:2 * dim + 3], 2, 1)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("tokens,hq,hk,dim", [(1000, 2, 1, 128), (1537, 1, 1, 64), (2050, 1, 1, 40)])
 def test_attention_over_many_tiles(lib, tokens, hq, hk, dim, dtype):
     attention_case(lib, 1, tokens, hq, hk, dim, "dense", dtype)
