@@ -443,8 +443,8 @@ int cdgrab_orthogonalize(cdgrab_handle *h, int64_t batch, int64_t rows, int64_t 
  * What a transformer has beside layer norm and linear layers: the embedding of token ids, the norms of queries and keys
  * with the position rotation, and causal attention within each example.  Rows, types, strides, capture and errors as above;
  * cdgrab_token_rows says which rows an example has, and a row's position is its place in its example.  Rows of no example are
- * neither read nor written.  Of examples that share rows, outputs of those rows (Y, DX, O, lse, DQ, DK, DV) are those of any one of
- * them, or of several in part; gradients of parameters (G) are right for every one. */
+ * neither read nor written.  Of examples that share rows, outputs of those rows (Y, DX) are those of any one of them, or of several in
+ * part, and what attention leaves in its outputs for such examples is not defined; gradients of parameters (G) are right for every one. */
 
 /* Embedding:  Y[t] = scale * table[ids[t]], rounded once; a row of zeros for an id outside 0 .. vocab - 1.
  *   ids [rows] int32 dev, table [vocab][width] of `table_type` (fp32 or `type`) dev, Y [rows][width] of `type` dev.
@@ -492,11 +492,12 @@ int cdgrab_pergrad_headnorm(cdgrab_handle *h, const cdgrab_token_rows *t, const 
  *     s_ij = scale * Q_i . K_j,   lse_i = ln sum_j exp(s_ij),   O_i = sum_j exp(s_ij - lse_i) V_j;
  * q_heads / kv_heads consecutive heads of queries share a head of keys and values.
  *   Q, O [rows][q_heads * dim], K, V [rows][kv_heads * dim] of `type` dev; lse [q_heads][rows] fp32 dev, or NULL: not wanted.
+ * With `count` and lengths that differ much: workspace of 8 bytes per example and per 128 rows (a list of what there is).
  * Products of bf16 and fp16 elements are exact, those of fp32 elements good to 2^-23; exponentials are rounded to `type`
  * (fp32: to 2^-24) where they are multiplied with V, sums are fp32.  An element that is not finite makes the results it enters infinite
  * or NaN, and may do so to those of up to 127 rows before it in its example.
  * Errors: EINVAL (sizes, dim > 128, more than 4096 heads, q_heads no multiple of kv_heads, more than 2^22 tokens, type,
- * scale not within 1e-30 .. 1e30, null, strides, overlap), EHIP. */
+ * scale not within 1e-30 .. 1e30, null, strides, overlap), ENOMEM, EHIP. */
 int cdgrab_attention(cdgrab_handle *h, const cdgrab_token_rows *t, int64_t q_heads, int64_t kv_heads, int64_t dim, int32_t type,
                      float scale, const void *Q, int64_t q_stride, const void *K, int64_t k_stride, const void *V,
                      int64_t v_stride, void *O, int64_t o_stride, float *lse);
@@ -506,7 +507,8 @@ int cdgrab_attention(cdgrab_handle *h, const cdgrab_token_rows *t, int64_t q_hea
  * the last two over the heads that share K_j and V_j.
  *   Q, K, V, scale: the forward pass's; O, lse: its outputs; DO as O; DQ as Q, DK and DV as K.
  * p and ds are rounded to `type` (fp32: to 2^-24) where they are multiplied.  Elements that are not finite: as there, and here also for
- * up to 127 rows behind.  Workspace: 4 * rows * q_heads bytes.
+ * up to 127 rows behind.  Workspace: 4 * rows * q_heads bytes, and
+ * the list.
  * Errors: EINVAL (as above), ENOMEM, EHIP. */
 int cdgrab_attention_backward(cdgrab_handle *h, const cdgrab_token_rows *t, int64_t q_heads, int64_t kv_heads, int64_t dim,
                               int32_t type, float scale, const void *Q, int64_t q_stride, const void *K, int64_t k_stride,

@@ -34,6 +34,7 @@ struct AttHeads {
     int tiles;             // of kAttRows rows that an example has at most
     int kv_heads, group;   // queries' heads that share keys and values
     bool by_pair;          // order of the workgroups
+    const uint64_t *list;  // or NULL: the number of tiles that there are, and then example and number in it of each
     int dim;
     float scale;
 };
@@ -411,6 +412,49 @@ __device__ __forceinline__ void att_write(T *to, const f32x16 (&acc)[D / 32], fl
         }
 }
 
+// The tiles of examples of uneven length, the longest first: list[0] of them, list[1 ..] = example << 32 | number in the example.  One
+// workgroup: it counts the tiles of each number and hands out places behind those of higher ones (which tile of a number gets which place
+// is open: it is only the order in which they run).
+__global__ __launch_bounds__(1024) void attention_list(TokenRows tok, int tiles, int64_t room, uint64_t *__restrict__ list)
+{
+    extern __shared__ int place[];  // [tiles]
+    __shared__ int sums[1024];
+    for (int j = threadIdx.x; j < tiles; j += 1024) place[j] = 0;
+    __syncthreads();
+    const auto each = [&](auto &&f) {
+        for (int64_t e = threadIdx.x; e < tok.examples; e += 1024) {
+            const int mine = (int)((rows_of(tok, e).count + kAttRows - 1) / kAttRows);  // (at most `tiles`)
+            for (int j = 0; j < mine; ++j) f(e, j);
+        }
+    };
+    each([&](int64_t, int j) { atomicAdd(place + j, 1); });
+    __syncthreads();
+    // a thread's share of the numbers, from the highest on: its sum, the sums before it, its places
+    const int per = (tiles + 1023) / 1024, hi = tiles - threadIdx.x * per;
+    int sum = 0;
+    for (int j = hi - 1; j >= 0 && j >= hi - per; --j) sum += place[j];
+    sums[threadIdx.x] = sum;
+    __syncthreads();
+    for (int gap = 1; gap < 1024; gap *= 2) {
+        const int before = (int)threadIdx.x >= gap ? sums[threadIdx.x - gap] : 0;
+        __syncthreads();
+        sums[threadIdx.x] += before;
+        __syncthreads();
+    }
+    int at = sums[threadIdx.x] - sum;
+    for (int j = hi - 1; j >= 0 && j >= hi - per; --j) {
+        const int n = place[j];
+        place[j] = at;
+        at += n;
+    }
+    if (threadIdx.x == 1023) list[0] = (uint64_t)(sums[1023] < room ? sums[1023] : room);
+    __syncthreads();
+    each([&](int64_t e, int j) {
+        const int to = atomicAdd(place + j, 1);
+        if (to < room) list[1 + to] = (uint64_t)e << 32 | (uint64_t)j;
+    });
+}
+
 // What a workgroup works on.  All of a pair (example, head of keys) run on one XCD: workgroups go round the XCDs, so every eighth belongs
 // to the same pair.  The longest tiles of all pairs come first: a long one that starts late keeps the others waiting.  Or, by_pair, those of
 // a pair one after the other, so that the XCD's L2 holds what they share.  (us, tile by tile and by pair: forward 64 x 1024 tokens, 12
@@ -425,6 +469,19 @@ struct AttPlace {
     template <bool QUERIES>
     __device__ __forceinline__ AttPlace(const TokenRows &tok, const AttHeads &a, std::integral_constant<bool, QUERIES>) {
         const int members = QUERIES ? a.group : 1;
+        if (a.list) {  // uniform: the heads of a tile side by side
+            const int64_t unit = a.unit0 + blockIdx.x, heads = (int64_t)a.kv_heads * members, slot = unit / heads;
+            there = slot < (int64_t)a.list[0];
+            if (!there) return;
+            const uint64_t entry = a.list[1 + slot];
+            const int which = (int)(unit - slot * heads), j = (int)(uint32_t)entry;
+            span = rows_of(tok, (int64_t)(entry >> 32));
+            count = (int)span.count;
+            kv = which / members;
+            head = kv * a.group + (which - kv * members);
+            row0 = (QUERIES ? j : (count + kAttRows - 1) / kAttRows - 1 - j) * kAttRows;
+            return;
+        }
         const int64_t unit = a.unit0 + blockIdx.x, turn = unit >> 3, per = a.by_pair ? (int64_t)a.tiles * members : (a.pairs + 7) >> 3;
         const int64_t whole = turn / per, part = turn - whole * per, pair = (a.by_pair ? whole : part) * 8 + (unit & 7);
         const int rest = (int)(a.by_pair ? part : whole), tile = rest / members;

@@ -479,6 +479,32 @@ def test_values_that_are_not_finite_stay_in_their_example(lib):
     assert not torch.isfinite(o[1, 20:]).any() and torch.isnan(o[1, 30:]).all()
 
 
+@pytest.mark.parametrize("kind", ["padded", "packed"])
+@pytest.mark.parametrize("counts", [[3] * 200 + [900], [900, 0] + [1, 129, 0, 257] * 80, [0] * 300 + [700]])
+def test_attention_of_examples_of_very_different_lengths(lib, kind, counts):
+    n, tokens, hq, hk, dim = len(counts), 900, 2, 1, 32
+    spans, rows, kw = layout(kind, counts, tokens)
+    q, k, v, do = attention_inputs(5, spans, rows, hq, hk, dim, torch.bfloat16)
+    q, k, v, do = (x.contiguous() for x in (q, k, v, do))
+    kw = dict(kw, q_heads=hq, kv_heads=hk)
+    h = lib.Handle()
+    x = [shaped(kind, t, n, tokens) for t in (q, k, v, do)]
+    o, lse = lib.cdgrab_attention(h, *x[:3], **kw)
+    grads = lib.cdgrab_attention_backward(h, *x[:3], o, lse, x[3], **kw)
+    again = lib.cdgrab_attention_backward(h, *x[:3], o, lse, x[3], **kw)
+    assert all(torch.equal(a, b) for a, b in zip(grads, again))
+    got = [t.reshape(rows, -1) for t in (o, *grads)] + [lse.reshape(hq, rows).t()]
+    mask = owned(spans, rows)
+    assert all((t[~mask] == 0).all() for t in got)
+    for at, count in {(a, c) for a, c in spans if c}:  # the same numbers as of the example by itself
+        part = [t[at:at + count].unsqueeze(0) for t in (q, k, v, do)]
+        o1, l1 = lib.cdgrab_attention(h, *part[:3], q_heads=hq, kv_heads=hk)
+        g1 = lib.cdgrab_attention_backward(h, *part[:3], o1, l1, part[3], q_heads=hq, kv_heads=hk)
+        for t, want in zip(got, [o1, *g1]):
+            assert torch.equal(t[at:at + count], want.reshape(count, -1))
+        assert torch.equal(got[4][at:at + count], l1.reshape(hq, count).t())
+
+
 def test_attention_of_more_examples_than_a_launch_holds(lib):
     # one row each: the only weight is one, o = v, dv = do and the others are zero, exactly
     n, heads, dim = 300_000, 8, 8
@@ -545,6 +571,42 @@ def test_recorded_calls(lib):
             graph.replay()
             stream.synchronize()
             assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_recorded_attention_of_other_lengths(lib):
+    """What an example has is read when the recording is replayed, the list of tiles is made anew."""
+    n, tokens, rows = 300, 500, 3000
+    stream = torch.cuda.Stream()
+    h = lib.Handle(stream=stream)
+
+    def counts(seed):
+        c = torch.randint(0, 8, (n,), generator=torch.Generator().manual_seed(seed))
+        c[seed % n] = tokens
+        first = c.cumsum(0) - c
+        return first.cuda(), c.int().cuda()
+
+    with torch.cuda.stream(stream):
+        first, count = counts(1)
+        q, do = rand(1, rows, 64, dtype=torch.bfloat16), rand(2, rows, 64, dtype=torch.bfloat16)
+        k, v = rand(3, rows, 32, dtype=torch.bfloat16), rand(4, rows, 32, dtype=torch.bfloat16)
+        kw = dict(q_heads=2, kv_heads=1, first=first, count=count, tokens=tokens)
+
+        def both():
+            o, lse = lib.cdgrab_attention(h, q, k, v, **kw)
+            return [o, lse, *lib.cdgrab_attention_backward(h, q, k, v, o, lse, do, **kw)]
+        both()
+        stream.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            got = both()
+        for seed in (7, 8, 9):
+            for t, new in zip((first, count), counts(seed)):
+                t.copy_(new)
+            want = both()
+            stream.synchronize()
+            graph.replay()
+            stream.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(got, want)) and (want[0] != 0).any()
 
 
 def test_a_recording_needs_its_workspace_beforehand(lib):
