@@ -494,8 +494,9 @@ int cdgrab_pergrad_headnorm(cdgrab_handle *h, const cdgrab_token_rows *t, const 
  *   Q, O [rows][q_heads * dim], K, V [rows][kv_heads * dim] of `type` dev; lse [q_heads][rows] fp32 dev, or NULL: not wanted.
  * With `count` and lengths that differ much: workspace of 8 bytes per example and per 128 rows (a list of what there is).
  * Products of bf16 and fp16 elements are exact, those of fp32 elements good to 2^-23; exponentials are rounded to `type`
- * (fp32: to 2^-24) where they are multiplied with V, sums are fp32.  An element that is not finite makes the results it enters infinite
- * or NaN, and may do so to those of up to 127 rows before it in its example.
+ * (fp32: to 2^-24) where they are multiplied with V, sums are fp32.  Scores may be of any size that fp32 holds, at any scale.  An element
+ * that is not finite, or a product Q_i . K_j beyond fp32, makes the results it enters infinite or NaN, and may do so to those of up to
+ * 127 rows before it in its example.  What fp32 elements beyond 3.38e38 and below 2^-110 in size give is as in cdgrab_pergrad_linear.
  * Errors: EINVAL (sizes, dim > 128, more than 4096 heads, q_heads no multiple of kv_heads, more than 2^22 tokens, type,
  * scale not within 1e-30 .. 1e30, null, strides, overlap), ENOMEM, EHIP. */
 int cdgrab_attention(cdgrab_handle *h, const cdgrab_token_rows *t, int64_t q_heads, int64_t kv_heads, int64_t dim, int32_t type,
@@ -506,9 +507,9 @@ int cdgrab_attention(cdgrab_handle *h, const cdgrab_token_rows *t, int64_t q_hea
  *     DQ_i = scale sum_j ds_ij K_j,   DK_j = scale sum_i ds_ij Q_i,   DV_j = sum_i p_ij DO_i,
  * the last two over the heads that share K_j and V_j.
  *   Q, K, V, scale: the forward pass's; O, lse: its outputs; DO as O; DQ as Q, DK and DV as K.
- * p and ds are rounded to `type` (fp32: to 2^-24) where they are multiplied.  Elements that are not finite: as there, and here also for
- * up to 127 rows behind.  Workspace: 4 * rows * q_heads bytes, and
- * the list.
+ * p and ds are rounded to `type` (fp32: to 2^-24) where they are multiplied.  Of large scores p has the error of lse, an fp32 number, besides:
+ * up to 2^-18 (|s_ij| + |lse_i|) relative, as an exponent, for |s_ij| up to 65 536; gradients of larger scores are not defined.
+ * Elements that are not finite: as there, and here also for up to 127 rows behind.  Workspace: 4 * rows * q_heads bytes, and the list.
  * Errors: EINVAL (as above), ENOMEM, EHIP. */
 int cdgrab_attention_backward(cdgrab_handle *h, const cdgrab_token_rows *t, int64_t q_heads, int64_t kv_heads, int64_t dim,
                               int32_t type, float scale, const void *Q, int64_t q_stride, const void *K, int64_t k_stride,

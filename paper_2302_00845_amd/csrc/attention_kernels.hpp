@@ -511,6 +511,13 @@ template <typename T> constexpr bool kAttExact = LinearPlanes<T>::N > 1;  // fp3
 // A staged tile's rows; LDS for two of them, all planes.
 template <typename T> constexpr int att_step() { return LinearPlanes<T>::N == 1 ? 64 : 32; }
 
+// Exponents of the forward pass: s c - most, where most is the rounded product of c and the row's maximum.  That all of a row are off by half a
+// step of `most` is nothing while it is small, since a factor of all weights goes out with their sum, but from 2^24 on it takes them out
+// of fp16 and from 2^31 on out of fp32.  So where it would pass kAttFar a wavefront goes over to (s - ref) c - most for the rest of its rows,
+// ref the maximum in the scores' units and most the shift alone: a difference of scores is as exact as they are, at any scale.
+// (One branch a tile: 64 x 1024 tokens, 12 heads of 64, bf16 196 -> 198 us, 2 x 8192, 32 heads on 8 of 128 1264 -> 1272 on the same card.)
+constexpr float kAttFar = 0x1p20f;
+
 template <typename T, int D, bool DIRECT>
 __global__ __launch_bounds__(kAttThreads, LinearPlanes<T>::N == 1 ? 2 : 1) void attention_forward(
     TokenRows tok, AttHeads a, const T *__restrict__ Q, int64_t q_stride, const T *__restrict__ K, int64_t k_stride,
@@ -532,8 +539,9 @@ __global__ __launch_bounds__(kAttThreads, LinearPlanes<T>::N == 1 ? 2 : 1) void 
     f32x16 acc[DB];
 #pragma unroll
     for (int d = 0; d < DB; ++d) acc[d] = zero16();
-    float most = -INFINITY, sum = 0.f;  // (of the lane's own rows)
+    float most = -INFINITY, sum = 0.f, ref = 0.f;  // (`sum` of the lane's own rows)
     const float c = a.scale * kLog2E;
+    bool far = false;  // uniform
     const int end = at.row0 + kAttRows < count ? at.row0 + kAttRows : count;  // keys
     Pipe pipe(lds, a.dim, k_stride, v_stride);
     pipe.fetch(k, k_stride, v, v_stride, 0, end);
@@ -560,10 +568,23 @@ __global__ __launch_bounds__(kAttThreads, LinearPlanes<T>::N == 1 ? 2 : 1) void 
         for (int b = 0; b < KB; ++b)
 #pragma unroll
             for (int r = 0; r < 16; ++r) top = fmaxf(top, s[b][r]);
-        top = fmaf(both_max(top), c, -kAttShiftForward<T>);
+        const float raw = both_max(top);
+        top = fmaf(raw, c, -kAttShiftForward<T>);
         // (The maximum may lag behind by 2^8, the sums have room for that: they are seldom scaled.)
-        if (__any(top > most + 8.f)) {
-            const float next = fmaxf(most, top), down = __builtin_amdgcn_exp2f(most - next);
+        if (__any(far ? (raw - ref) * c > 8.f : top > most + 8.f)) {
+            float next = fmaxf(most, top), down = __builtin_amdgcn_exp2f(most - next);
+            if (far || __any(fabsf(next) > kAttFar)) {
+                float by = 0.f;  // what the exponents of the sums change by for the other form
+                if (!far) {
+                    far = true;
+                    ref = most / c;
+                    by = most > -INFINITY ? fmaf(-ref, c, most) + kAttShiftForward<T> : 0.f;
+                }
+                next = -kAttShiftForward<T>;
+                const float peak = fmaxf(ref, raw);
+                down = __builtin_amdgcn_exp2f(fmaf(ref - peak, c, by));
+                ref = peak;
+            }
             most = next;
             sum *= down;
 #pragma unroll
@@ -571,6 +592,11 @@ __global__ __launch_bounds__(kAttThreads, LinearPlanes<T>::N == 1 ? 2 : 1) void 
 #pragma unroll
                 for (int r = 0; r < 16; ++r) acc[d][r] *= down;
         }
+        if (far)
+#pragma unroll
+            for (int b = 0; b < KB; ++b)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[b][r] -= ref;
 #pragma unroll
         for (int b = 0; b < KB; ++b) {
             const AttAcross<T, D, STEP, DIRECT> values(read, tv, b * 32);
@@ -592,7 +618,8 @@ __global__ __launch_bounds__(kAttThreads, LinearPlanes<T>::N == 1 ? 2 : 1) void 
     sum = both_sum(sum);
     if (mine < count) {
         att_write<T, D>(O + (at.span.first + mine) * o_stride + (int64_t)at.head * a.dim, acc, 1.f / sum, a.dim, lane);
-        if (lse && lane < 32) lse[at.head * tok.rows + at.span.first + mine] = (most + __builtin_amdgcn_logf(sum)) * kLn2;
+        if (lse && lane < 32)
+            lse[at.head * tok.rows + at.span.first + mine] = fmaf(ref, a.scale, (most + __builtin_amdgcn_logf(sum)) * kLn2);
     }
 }
 
