@@ -492,7 +492,7 @@ int cdgrab_pergrad_headnorm(cdgrab_handle *h, const cdgrab_token_rows *t, const 
  *     s_ij = scale * Q_i . K_j,   lse_i = ln sum_j exp(s_ij),   O_i = sum_j exp(s_ij - lse_i) V_j;
  * q_heads / kv_heads consecutive heads of queries share a head of keys and values.
  *   Q, O [rows][q_heads * dim], K, V [rows][kv_heads * dim] of `type` dev; lse [q_heads][rows] fp32 dev, or NULL: not wanted.
- * With `count` and lengths that differ much: workspace of 8 bytes per example and per 128 rows (a list of what there is).
+ * With `count` and lengths that differ much: workspace of 8 bytes per example and 12 per 128 rows (a list of what there is).
  * Products of bf16 and fp16 elements are exact, those of fp32 elements good to 2^-23; exponentials are rounded to `type`
  * (fp32: to 2^-24) where they are multiplied with V, sums are fp32.  Scores may be of any size that fp32 holds, at any scale.  An element
  * that is not finite, or a product Q_i . K_j beyond fp32, makes the results it enters infinite or NaN, and may do so to those of up to

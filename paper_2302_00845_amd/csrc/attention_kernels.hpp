@@ -415,41 +415,78 @@ __device__ __forceinline__ void att_write(T *to, const f32x16 (&acc)[D / 32], fl
 // The tiles of examples of uneven length, the longest first: list[0] of them, list[1 ..] = example << 32 | number in the example.  One
 // workgroup: it counts the tiles of each number and hands out places behind those of higher ones (which tile of a number gets which place
 // is open: it is only the order in which they run).
-__global__ __launch_bounds__(1024) void attention_list(TokenRows tok, int tiles, int64_t room, uint64_t *__restrict__ list)
+// Examples that share no rows have at most rows / kAttRows + 1 whole tiles and one that is not whole each, which is the list's room.  Where
+// there are more, some share rows, and outputs of those are not defined: each whole tile claims the multiple of kAttRows among its
+// rows, the first example that claims one keeps its tile, and other tiles are left out.  A tile of an example that shares no rows is never
+// one of them, and there is room for what is left.  claims [rows / kAttRows + 1].
+__global__ __launch_bounds__(1024) void attention_list(TokenRows tok, int tiles, int64_t room, uint64_t *__restrict__ list,
+                                                       uint32_t *__restrict__ claims)
 {
     extern __shared__ int place[];  // [tiles]
     __shared__ int sums[1024];
-    for (int j = threadIdx.x; j < tiles; j += 1024) place[j] = 0;
-    __syncthreads();
+    // f(example, its rows, tile's number)
     const auto each = [&](auto &&f) {
         for (int64_t e = threadIdx.x; e < tok.examples; e += 1024) {
-            const int mine = (int)((rows_of(tok, e).count + kAttRows - 1) / kAttRows);  // (at most `tiles`)
-            for (int j = 0; j < mine; ++j) f(e, j);
+            const RowSpan span = rows_of(tok, e);
+            const int mine = (int)((span.count + kAttRows - 1) / kAttRows);  // (at most `tiles`)
+            for (int j = 0; j < mine; ++j) f(e, span, j);
         }
     };
-    each([&](int64_t, int j) { atomicAdd(place + j, 1); });
-    __syncthreads();
-    // a thread's share of the numbers, from the highest on: its sum, the sums before it, its places
-    const int per = (tiles + 1023) / 1024, hi = tiles - threadIdx.x * per;
-    int sum = 0;
-    for (int j = hi - 1; j >= 0 && j >= hi - per; --j) sum += place[j];
-    sums[threadIdx.x] = sum;
-    __syncthreads();
-    for (int gap = 1; gap < 1024; gap *= 2) {
-        const int before = (int)threadIdx.x >= gap ? sums[threadIdx.x - gap] : 0;
+    const auto claim = [&](const RowSpan &span, int j) -> uint32_t * {  // (NULL: not a whole tile)
+        return (j + 1) * kAttRows <= span.count ? claims + (span.first + j * kAttRows + kAttRows - 1) / kAttRows : nullptr;
+    };
+    bool shared = false;  // uniform
+    const auto kept = [&](int64_t e, const RowSpan &span, int j) {
+        if (!shared) return true;
+        const uint32_t *c = claim(span, j);
+        return !c || __hip_atomic_load(c, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)e;
+    };
+    // The first place of each number, into `place`; how many there are.
+    const auto hand_out = [&]() {
+        for (int j = threadIdx.x; j < tiles; j += 1024) place[j] = 0;
         __syncthreads();
-        sums[threadIdx.x] += before;
+        each([&](int64_t e, const RowSpan &span, int j) {
+            if (kept(e, span, j)) atomicAdd(place + j, 1);
+        });
         __syncthreads();
+        // a thread's share of the numbers, from the highest on: its sum, the sums before it, its places
+        const int per = (tiles + 1023) / 1024, hi = tiles - threadIdx.x * per;
+        int sum = 0;
+        for (int j = hi - 1; j >= 0 && j >= hi - per; --j) sum += place[j];
+        sums[threadIdx.x] = sum;
+        __syncthreads();
+        for (int gap = 1; gap < 1024; gap *= 2) {
+            const int before = (int)threadIdx.x >= gap ? sums[threadIdx.x - gap] : 0;
+            __syncthreads();
+            sums[threadIdx.x] += before;
+            __syncthreads();
+        }
+        int at = sums[threadIdx.x] - sum;
+        for (int j = hi - 1; j >= 0 && j >= hi - per; --j) {
+            const int n = place[j];
+            place[j] = at;
+            at += n;
+        }
+        const int total = sums[1023];
+        __syncthreads();
+        return total;
+    };
+    int total = hand_out();  // uniform
+    if (total > room) {
+        for (int64_t i = threadIdx.x; i < tok.rows / kAttRows + 1; i += 1024) claims[i] = ~0u;
+        __threadfence();
+        __syncthreads();
+        each([&](int64_t e, const RowSpan &span, int j) {
+            if (uint32_t *c = claim(span, j)) atomicMin(c, (uint32_t)e);
+        });
+        __threadfence();
+        __syncthreads();
+        shared = true;
+        total = hand_out();
     }
-    int at = sums[threadIdx.x] - sum;
-    for (int j = hi - 1; j >= 0 && j >= hi - per; --j) {
-        const int n = place[j];
-        place[j] = at;
-        at += n;
-    }
-    if (threadIdx.x == 1023) list[0] = (uint64_t)(sums[1023] < room ? sums[1023] : room);
-    __syncthreads();
-    each([&](int64_t e, int j) {
+    if (threadIdx.x == 0) list[0] = (uint64_t)(total < room ? total : room);
+    each([&](int64_t e, const RowSpan &span, int j) {
+        if (!kept(e, span, j)) return;
         const int to = atomicAdd(place + j, 1);
         if (to < room) list[1 + to] = (uint64_t)e << 32 | (uint64_t)j;
     });

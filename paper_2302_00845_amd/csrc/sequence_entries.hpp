@@ -240,25 +240,27 @@ int by_pieces(int64_t dim, std::initializer_list<Pieces> arrays, F &&f) {
 
 int64_t att_tiles(const TokenRows &tok) { return (std::min(tok.tokens, tok.rows) + kAttRows - 1) / kAttRows; }
 
-// Tiles that examples which share no rows can have at most, if a list of them pays (else 0): where the longest example is much longer
+// Room of the list of tiles: what examples that share no rows can have at most, if a list pays (else 0): where the longest example is much longer
 // than the others most of [examples][tiles] is empty, and a workgroup that finds nothing costs about a nanosecond (1000 examples of 100 tokens and
 // one of 8192, 12 heads of 64, bf16: forward 1141 -> 342 us, back 2855 -> 966).
 int64_t att_list(const TokenRows &tok) {
     const int64_t tiles = att_tiles(tok), most = tok.rows / kAttRows + tok.examples;
     const bool pays = tok.count && tiles > 1 && tiles <= kAttListTiles && tok.examples < INT32_MAX / tiles && most < INT32_MAX / 2 &&
                       tok.examples >= 2 * most / tiles + 64;
-    return pays ? most : 0;
+    return pays ? most + 1 : 0;
 }
 
+// The list, and what its kernel takes besides (claims), whole words of eight bytes.
 int64_t att_list_bytes(const TokenRows &tok) {
     const int64_t most = att_list(tok);
-    return most ? (most + 1) * 8 : 0;
+    return most ? (most + 1) * 8 + round_up((tok.rows / kAttRows + 1) * 4, 8) : 0;
 }
 
 void make_att_list(cdgrab_handle *h, const TokenRows &tok, uint64_t *list) {
     const int64_t most = att_list(tok), tiles = att_tiles(tok);
     if (most)
-        hipLaunchKernelGGL(attention_list, dim3(1), dim3(1024), (size_t)tiles * sizeof(int), h->stream, tok, (int)tiles, most, list);
+        hipLaunchKernelGGL(attention_list, dim3(1), dim3(1024), (size_t)tiles * sizeof(int), h->stream, tok, (int)tiles, most, list,
+                           reinterpret_cast<uint32_t *>(list + most + 1));
 }
 
 // launch(heads, workgroups) for as many workgroups at a time as a grid holds; `members`: one per tile and head of queries, else of keys.
