@@ -42,6 +42,12 @@ __device__ __forceinline__ float2 cos_sin_turns(uint64_t turns) {
     return make_float2((quarter + 1) & 2 ? -a : a, quarter & 2 ? -b : b);
 }
 
+// Without eps, or with next to none, a head of small elements is as long as any other, but their squares are below fp32's numbers: where
+// a head's sum is below kHeadSmall its elements are taken kHeadUp times as large, and eps by the square of that.  (From kHeadTiny on eps
+// is what counts beside such a sum, and fp16 has no elements as small: kernels of their own, RAISE, so that the others keep their
+// registers; with a branch in one kernel 121 of them became 132, three wavefronts per SIMD instead of four.)
+constexpr float kHeadTiny = 0x1p-80f, kHeadSmall = 0x1p-90f, kHeadUp = 0x1p100f;
+
 struct HeadShape {
     int q_heads, heads, half;  // queries' heads, queries' and keys', half of a head's features
     int rows;                  // rows at a time
@@ -78,7 +84,7 @@ __device__ __forceinline__ float heads_sum(float x) {
 // LANES threads a head.  BACKWARD: DY and DX in the place of Y; the gains' gradients [2][dim] to G or to `partial` [examples][chunks][2 dim].
 // ONCE: rows that the caches do not hold anyway are read past them, and DX is written past them (20 000 rows of 40 heads of 128, bf16 148 -> 143
 // us; Y, which is read next, is not: 65 536 rows of 24 of 64 102 -> 106).
-template <typename T, int VEC, int LANES, bool BACKWARD, bool ONCE>
+template <typename T, int VEC, int LANES, bool BACKWARD, bool ONCE, bool RAISE>
 __global__ __launch_bounds__(kHeadThreads) void head_norm(
     TokenRows tok, int chunks, HeadShape sh, HeadTurns turns, const T *__restrict__ X, int64_t x_stride, const T *__restrict__ DY,
     int64_t dy_stride, const float *__restrict__ gain_q, const float *__restrict__ gain_k, T *__restrict__ Y, int64_t y_stride,
@@ -126,6 +132,22 @@ __global__ __launch_bounds__(kHeadThreads) void head_norm(
                 }
                 const float2 *turn = table + r * half + pos;
                 T y[2][VEC];
+                float eps = sh.eps, up = 1.f;
+                if constexpr (RAISE) {
+                    float ss = 0.f;
+#pragma unroll
+                    for (int p = 0; p < 2; ++p)
+#pragma unroll
+                        for (int j = 0; j < VEC; ++j) ss = sl.own(0, j) ? fmaf((float)x[p][j], (float)x[p][j], ss) : ss;
+                    if (lanes_sum<LANES>(ss) < kHeadSmall) {
+                        up = kHeadUp;
+                        eps = eps * kHeadUp * kHeadUp;
+                    }
+#pragma unroll
+                    for (int p = 0; p < 2; ++p)
+#pragma unroll
+                        for (int j = 0; j < VEC; ++j) x[p][j] = (T)((float)x[p][j] * up);
+                }
                 if constexpr (!BACKWARD) {
                     float ss = 0.f;
 #pragma unroll
@@ -133,7 +155,7 @@ __global__ __launch_bounds__(kHeadThreads) void head_norm(
 #pragma unroll
                         for (int j = 0; j < VEC; ++j) ss = sl.own(0, j) ? fmaf((float)x[p][j], (float)x[p][j], ss) : ss;
                     ss = lanes_sum<LANES>(ss);
-                    const float rs = 1.f / sqrtf(fmaf(ss, inv, sh.eps)) + (ss - ss);  // (NaN of a sum that is not finite)
+                    const float rs = 1.f / sqrtf(fmaf(ss, inv, eps)) + (ss - ss);  // (NaN of a sum that is not finite)
 #pragma unroll
                     for (int j = 0; j < VEC; ++j) {
                         const float2 cs = turn[j];
@@ -158,14 +180,16 @@ __global__ __launch_bounds__(kHeadThreads) void head_norm(
                     }
                     s[0] = lanes_sum<LANES>(s[0]);
                     s[1] = lanes_sum<LANES>(s[1]);
-                    const float rs = 1.f / sqrtf(fmaf(s[0], inv, sh.eps)) + (s[0] - s[0]);
+                    const float rs = 1.f / sqrtf(fmaf(s[0], inv, eps)) + (s[0] - s[0]);
                     const float mean = s[1] * rs * inv;
 #pragma unroll
                     for (int p = 0; p < 2; ++p)
 #pragma unroll
                         for (int j = 0; j < VEC; ++j) {
                             const float hat = (float)x[p][j] * rs;
-                            y[p][j] = (T)(rs * fmaf(u[p][j], w[p][j], -(hat * mean)));
+                            float d = rs * fmaf(u[p][j], w[p][j], -(hat * mean));
+                            if constexpr (RAISE) d *= up;
+                            y[p][j] = (T)d;
                             if (live) dw[p][j] = fmaf(u[p][j], hat, dw[p][j]);
                         }
                 }

@@ -183,13 +183,19 @@ int run_heads(cdgrab_handle *h, const char *who, const TokenRows &tok, const cdg
                 hipLaunchKernelGGL(kernel, dim3((unsigned)(part.examples * chunks)), dim3(kHeadThreads), 0, h->stream, part, (int)chunks, sh,
                                    turns, X, x_stride, DY, dy_stride, gain_q, gain_k, Y, y_stride, G, g_stride, partial);
             };
-            if constexpr (VEC > 1) {
-                if (once) {
-                    launch(head_norm<T, VEC, LANES, BACKWARD, true>);
+            if constexpr (!std::is_same<T, f16_t>::value) {
+                if (s.eps < kHeadTiny) {
+                    launch(head_norm<T, VEC, LANES, BACKWARD, false, true>);
                     continue;
                 }
             }
-            launch(head_norm<T, VEC, LANES, BACKWARD, false>);
+            if constexpr (VEC > 1) {
+                if (once) {
+                    launch(head_norm<T, VEC, LANES, BACKWARD, true, false>);
+                    continue;
+                }
+            }
+            launch(head_norm<T, VEC, LANES, BACKWARD, false, false>);
         }
         if (partial)  // (fewer than `fill` examples of at most 32 groups of columns: one launch)
             hipLaunchKernelGGL(norm_grad_finish, dim3((unsigned)(tok.examples * ((2 * s.dim + 31) / 32))), dim3(256), 0, h->stream, partial,
