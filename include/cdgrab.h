@@ -446,7 +446,7 @@ int cdgrab_orthogonalize(cdgrab_handle *h, int64_t batch, int64_t rows, int64_t 
  * neither read nor written.  Of examples that share rows, outputs of those rows (Y, DX) are those of any one of them, or of several in
  * part, and what attention leaves in its outputs for such examples is not defined; gradients of parameters (G) are right for every one. */
 
-/* Embedding:  Y[t] = scale * table[ids[t]], rounded once; a row of zeros for an id outside 0 .. vocab - 1.
+/* Embedding:  Y[t] = scale * table[ids[t]], in fp32 and then rounded to `type`; a row of zeros for an id outside 0 .. vocab - 1.
  *   ids [rows] int32 dev, table [vocab][width] of `table_type` (fp32 or `type`) dev, Y [rows][width] of `type` dev.
  * Errors: EINVAL (sizes, width > 2^20, types, scale not finite, null, strides, overlap), EHIP. */
 int cdgrab_embed(cdgrab_handle *h, int64_t rows, int64_t vocab, int64_t width, const int32_t *ids, int32_t table_type,
@@ -473,7 +473,7 @@ typedef struct cdgrab_heads {
  * a_i = position * base^(-2 i / dim), i < dim / 2,
  *     Y[i] = u[i] cos a_i - u[i + dim/2] sin a_i,    Y[i + dim/2] = u[i + dim/2] cos a_i + u[i] sin a_i.
  *   X, Y [rows][(q_heads + k_heads) * dim] of `type` dev; gain_q (queries), gain_k (keys) [dim] fp32 dev, or NULL: one.
- * Angles are good to 2^-27 of a turn at any position.  A head with an element that is not finite, or whose squares add up beyond fp32
+ * Angles are good to 2^-27 of a turn at positions up to 2^32.  A head with an element that is not finite, or whose squares add up beyond fp32
  * (elements beyond about 1e19), becomes NaN, and with eps 0 a head of zeros.
  * Errors: EINVAL (sizes, dim odd or > 512, more than 4096 heads, type, eps < 0, base, null, strides, overlap), EHIP. */
 int cdgrab_headnorm(cdgrab_handle *h, const cdgrab_token_rows *t, const cdgrab_heads *s, int32_t type, const void *X,

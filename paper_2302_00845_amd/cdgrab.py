@@ -790,7 +790,8 @@ def cdgrab_attention_backward(h: Handle, Q: torch.Tensor, K: torch.Tensor, V: to
                               dQ: Optional[torch.Tensor] = None, dK: Optional[torch.Tensor] = None,
                               dV: Optional[torch.Tensor] = None):
     """Backward pass of cdgrab_attention from its outputs O and lse and the gradient dO: (dQ, dK, dV), which may be given, as
-    stretches of one array's rows too.  Rows of no example keep what they hold (zero where the call makes them)."""
+    stretches of one array's rows too.  Rows of no example keep what they hold (zero where the call makes them).  Gradients are
+    good where scores (scale * Q . K) are at most 65 536 in size."""
     t, dim, scale, at, lead = _attention_rows(h, Q, K, V, q_heads, kv_heads, scale, first, count, tokens)
     po, _, _, so = _rows(O, "O", h.device, Q)
     pg, _, _, sg = _rows(dO, "dO", h.device, Q)

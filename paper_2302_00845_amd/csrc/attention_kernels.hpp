@@ -16,10 +16,17 @@
 // (LinearPlanes), p and ds too.  A backward pass in two kernels, dq by queries and dk, dv by keys, takes seven products
 // instead of five but adds everything up in registers in a fixed order.
 //
-// Measured: forward 2 x 8192 tokens, 32 heads on 8 of 128, bf16 1110 us, 990 TFLOP/s (a large product reaches 1100 to 1150); with heads of
-// 64, where there is one exponential for half as many products, 64 x 1024 tokens, 12 heads 190 us, 540 TFLOP/s: VALU 67 % of the cycles, MFMA
-// 31 %.  Back, the same: dq 270 us, dk and dv 300, 575 and 685 TFLOP/s of the products that they take; half of the wavefronts' time is waiting,
-// and registers allow no more of them (dk, dv: one, two, three per SIMD 668, 420, 400 us).  fp32 64 x 128 tokens, 4 heads of 32 11 us.
+// Measured: forward 2 x 8192 tokens, 32 heads on 8 of 128, bf16 1110 to 1270 us by the card, 990 to 870 TFLOP/s (a large product reaches 1100
+// to 1150); with heads of 64, where there is one exponential for half as many products, 64 x 1024 tokens, 12 heads 190 to 198 us, 530 TFLOP/s:
+// VALU 66 % of the cycles, MFMA 30 %.  Back, the same: dq 270 us, dk and dv 300, 575 and 685 TFLOP/s of the products that they take; half of
+// the wavefronts' time is waiting, and registers allow no more of them (dk, dv: one, two, three per SIMD 668, 420, 400 us).  fp32 64 x 128
+// tokens, 4 heads of 32 11 us, dq 14, dk and dv 16; 16 x 1024, 8 heads of 64 121, 207 and 252 us; 8 x 1024, 16 heads on 4 of 128 290, 400 and 870.
+//
+// What is far from that: dk and dv where keys are shared or examples are few or uneven, since a workgroup goes over all heads of the group and all
+// later queries of its 128 keys by itself (24 examples of up to 1500 tokens, 8 heads on 2 of 80, fp16 250 us, CUs busy for 60 % of it; 1 x 2048,
+// 32 heads on 1 of 128, bf16, 16 workgroups, 2500 us for what its products take 60), and at more than 64 features, of which one workgroup
+// fits a CU; forward and dq of fewer than eight pairs (example, head of keys), each of which runs on one XCD: 1 x 8192, 32 heads on 1 of 128
+// forward 4100 us, on 4 of 128 1110, on 8 all XCDs are in use.
 #pragma once
 #include "linear_kernels.hpp"
 
@@ -794,7 +801,7 @@ __global__ __launch_bounds__(kAttThreads, LinearPlanes<T>::N > 1 ? 1 : D <= 64 ?
 }
 
 // dk and dv by keys, over all heads that share them.  A block of 32 queries at a time: two at a time need registers that are not there (620 us
-// against 430 for the case above).
+// against 430 for the case above).  Spilled: 62 registers of fp32 at 128 features, at 64 of 16 bits 3 (whole pieces; dq too) or 4 to 15.
 template <typename T, int D, bool DIRECT>
 __global__ __launch_bounds__(kAttThreads, LinearPlanes<T>::N == 1 && D <= 64 ? 3 : 1) void attention_backward_kv(
     TokenRows tok, AttHeads a, const T *__restrict__ Q, int64_t q_stride, const T *__restrict__ K, int64_t k_stride,

@@ -10,7 +10,7 @@
 // computes those of its rows once, into LDS.  Sums in fp32, results are rounded once.  Queries' heads first and then the keys': one kind's
 // gains and their sums are in registers at a time (backward 145 -> 121 of them, 141 -> 131 us for the case below).  65 536 rows of 24 heads
 // of 64, bf16: 102 us, 4.0 TB/s, and back 138 us, 4.4 TB/s.  Heads whose half is no power of two of pieces leave threads idle: back, 25 700 rows
-// of 10 heads of 80, fp16 54 us, 2.3 TB/s, VALU 89 % of the cycles.
+// of 10 heads of 80, fp16 54 us, 2.3 TB/s, VALU 90 % of the cycles.
 #pragma once
 #include "norm_kernels.hpp"
 

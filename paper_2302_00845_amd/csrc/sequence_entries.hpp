@@ -248,7 +248,8 @@ int64_t att_tiles(const TokenRows &tok) { return (std::min(tok.tokens, tok.rows)
 
 // Room of the list of tiles: what examples that share no rows can have at most, if a list pays (else 0): where the longest example is much longer
 // than the others most of [examples][tiles] is empty, and a workgroup that finds nothing costs about a nanosecond (1000 examples of 100 tokens and
-// one of 8192, 12 heads of 64, bf16: forward 1141 -> 342 us, back 2855 -> 966).
+// one of 8192, 12 heads of 64, bf16: forward 1141 -> 342 us, back 2855 -> 966).  Of packed rows only: with the rows of a padded batch there
+// may be as many tiles as there are workgroups, and `count` is not known here.
 int64_t att_list(const TokenRows &tok) {
     const int64_t tiles = att_tiles(tok), most = tok.rows / kAttRows + tok.examples;
     const bool pays = tok.count && tiles > 1 && tiles <= kAttListTiles && tok.examples < INT32_MAX / tiles && most < INT32_MAX / 2 &&
