@@ -617,7 +617,7 @@ __global__ __launch_bounds__(kAttThreads, LinearPlanes<T>::N == 1 ? 2 : 1) void 
         // (The maximum may lag behind by 2^8, the sums have room for that: they are seldom scaled.)
         if (__any(far ? (raw - ref) * c > 8.f : top > most + 8.f)) {
             float next = fmaxf(most, top), down = __builtin_amdgcn_exp2f(most - next);
-            if (far || __any(fabsf(next) > kAttFar)) {
+            if (far || __any(fabsf(next) > kAttFar && next > -INFINITY)) {  // (-inf: a row that is NaN so far)
                 float by = 0.f;  // what the exponents of the sums change by for the other form
                 if (!far) {
                     far = true;

@@ -129,3 +129,20 @@ def test_gradients_of_large_scores(lib, most, dim, dtype):
     for name, got, want, tol in (("dq", dq, ds @ k * scale, scale * eds @ k.abs()), ("dk", dk, ds.t() @ q * scale, scale * eds.t() @ q.abs()),
                                  ("dv", dv, p.t() @ do, (p * (ep + half * (1 + ep) + (n + 4) * U) + low).t() @ do.abs())):
         close(got, want, tol + half * want.abs() * 1.01 + tiny(dtype), name)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_rows_beside_a_query_that_is_not_finite(lib, dtype):
+    """Queries share nothing but their keys: the others' rows are as good as without it, at large scores too."""
+    n, dim = 330, 40
+    q, k, v = whole(1, n, dim, dtype=dtype), whole(2, n, dim, dtype=dtype), rand(3, n, dim, dtype=dtype)
+    q[0], q[140] = float("nan"), float("inf")
+    others = torch.ones(n, dtype=torch.bool, device="cuda")
+    others[0] = others[140] = False
+    for scale in (0.5, 1e9):
+        o, lse = lib.cdgrab_attention(lib.Handle(), q.unsqueeze(0), k.unsqueeze(0), v.unsqueeze(0), q_heads=1, kv_heads=1, scale=scale)
+        s, want_lse, p = weights64(q, k, float(torch.tensor(scale)))
+        want, size = (p @ v.double())[others], ((p * (4 * 161 * U + (2 * n + 8) * U + step(dtype)) + 2.0 ** -32) @ v.double().abs())[others]
+        close(o[0][others], want, size + step(dtype) * want.abs() * 1.01 + tiny(dtype), "o")
+        close(lse[0, 0][others], want_lse.squeeze(1)[others], 6 * U * want_lse.squeeze(1)[others].abs() + (2 * n + 700) * U, "lse")
+        assert not torch.isfinite(o[0][~others]).any()
